@@ -322,6 +322,71 @@ int longer_input_generation_backward(const longer_config* cfg, const longer_inpu
                                      float* dE_out, float* dtdiff_out, float* grads_out,
                                      void* ws, size_t ws_bytes, void* stream);
 
+/* ---- The training step around the gradients (Section 3.6 trains with them; the paper names no norm of the
+ * inputs, no clipping and no optimizer: these calls are the usual ones, and take part in no call above).
+ *
+ * Layer norm of token rows: Y = (X - mean) / sqrt(var + eps) * ln_g + ln_b over the d values of each row, biased
+ * variance, statistics in fp32 from the centred values.  In front of longer_forward_backward it normalises the
+ * rows of the embeddings (H, G); on the first m rows of each user's Y_out it is the final norm that the pre-norm
+ * stack does not have.
+ *
+ * Rows of a [B, L, d] tensor that need not be dense: value c of row l of user b lies at
+ * data + b user_stride + l row_stride + c, strides in elements, not negative, aligned to the element only.  An
+ * input's rows may coincide (stride 0), an output's may not overlap. */
+typedef struct { void* data; int64_t user_stride, row_stride; int32_t dtype; } longer_rows;
+
+/* x -> y, of one dtype, ln_g / ln_b [d] of that dtype.  lens int32 [B] (device) or NULL: rows l >= lens[b] are
+ * padding, never read and written as exact zeros.  y may be x itself (same data and strides), else the two may not
+ * overlap.  1 <= d <= LONGER_MAX_NORM_WIDTH, B L < 2^31, eps > 0.  Takes no workspace. */
+#define LONGER_MAX_NORM_WIDTH 16384
+int longer_layer_norm(const longer_rows* x, const void* ln_g, const void* ln_b, const int32_t* lens,
+                      int B, int L, int d, float eps, const longer_rows* y, void* stream);
+
+/* Its backward pass: for q = dy ln_g, xh the normalised row and r = 1 / sqrt(var + eps),
+ *   dx = r (q - mean(q) - xh mean(q xh)),   d ln_g = sum over rows of dy xh,   d ln_b = sum over rows of dy.
+ * Nothing is kept from the forward call: statistics are formed again from x, which is read anyway.
+ * x and ln_g as in the forward call; dy and dx in fp32 (what longer_forward_backward writes to dH_out and dG_out)
+ * or both in x's dtype; padding as above: neither x nor dy is read there, dx is zero.  dx may be dy itself.
+ * grads_out fp32 [2][d]: ln_g's gradient, then ln_b's; overwritten, not accumulated into.  The sums over rows are
+ * taken in a fixed order: the same call gives the same bits.
+ * ws: device, 256-byte aligned, at least longer_layer_norm_backward_workspace_bytes(B, L, d) bytes (0 = unsupported). */
+size_t longer_layer_norm_backward_workspace_bytes(int B, int L, int d);
+int longer_layer_norm_backward(const longer_rows* x, const void* ln_g, const longer_rows* dy, const int32_t* lens,
+                               int B, int L, int d, float eps, const longer_rows* dx, float* grads_out,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* A list of dense tensors: HOST array of descriptors of device memory, read during the call only.  n = 0 is allowed
+ * (data may then be NULL).  dtype LONGER_F32 or LONGER_BF16, tensor by tensor; aligned to the element only. */
+typedef struct { void* data; int64_t n; int32_t dtype; } longer_tensor;
+
+/* Global norm of a list of gradients and the factor that bounds it:
+ *   norm_out[0] = sqrt(sum of the squares of all values),
+ *   norm_out[1] = 1 where norm_out[0] <= max_norm, max_norm / norm_out[0] where it is larger and finite, 0 where it is
+ *   an infinity or NaN.
+ * Squares and sums in 64 bits, in a fixed order.  max_norm > 0; infinity: never clips.  norm_out: device, fp32 [2].
+ * ws: device, 256-byte aligned, at least longer_grad_norm_workspace_bytes(grads, count) bytes (0 = a bad list). */
+size_t longer_grad_norm_workspace_bytes(const longer_tensor* grads, int count);
+int longer_grad_norm(const longer_tensor* grads, int count, float max_norm, float* norm_out,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/* out[i] = norm[1] * grads[i], norm as longer_grad_norm wrote it (device); where norm[0] is not finite, zeros.
+ * out[i] has the size and dtype of grads[i] and is either the same memory (out = NULL: all of them; with a factor of
+ * 1 nothing is then read or written) or does not overlap any tensor of the list. */
+int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, int count, const float* norm, void* stream);
+
+/* One tensor of an AdamW update: fp32 master values p and moments m, v; the gradient g (fp32 or bf16); w, the copy
+ * in the model's type that the kernels read (fp32 or bf16), or NULL.  n values each; decay = weight decay of this
+ * tensor (0 for biases and norms).  The five do not overlap, nor do two tensors of a list. */
+typedef struct { float *p, *m, *v; const void* g; void* w; int64_t n; int32_t g_dtype, w_dtype; double decay; } longer_adamw_tensor;
+typedef struct { double lr, beta1, beta2, eps; int64_t step; } longer_adamw;   /* step counts from 1 */
+
+/* With g' = norm[1] g (norm NULL: g' = g), for every value of every tensor, in fp32:
+ *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
+ *   p <- p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + decay p)        w <- p rounded to w_dtype
+ * Clipping is the factor alone: no pass of its own over the gradients, which stay as they are.  A norm that is not
+ * finite leaves p, m, v and w as they were (the batch is dropped).  lr >= 0, 0 <= beta1, beta2 < 1, eps > 0. */
+int longer_adamw_step(const longer_adamw_tensor* tensors, int count, const longer_adamw* how, const float* norm, void* stream);
+
 /* Measurement aid: when enabled, every kernel launch group of the entry points is bracketed
  * by a pair of HIP events recorded on the caller's stream (at most 4096 pairs between two
  * reads; later launches go unrecorded).  enable = 0: off; 1: every stage; any other value:

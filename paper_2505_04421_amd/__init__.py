@@ -17,4 +17,6 @@ from .binding import (  # noqa: F401
     longer_backward_workspace_bytes, longer_block_grad_floats, longer_token_merge_backward, block_grad_views,
     longer_model_grad_floats, longer_forward_backward_workspace_bytes, longer_forward_backward, model_grad_views,
     longer_input_backward_workspace_bytes, longer_input_grad_floats, longer_input_generation_backward, input_grad_views,
+    longer_layer_norm, longer_layer_norm_backward_workspace_bytes, longer_layer_norm_backward,
+    TensorList, AdamWList, longer_grad_norm_workspace_bytes, longer_grad_norm, longer_clip_gradients, longer_adamw_step,
 )

@@ -19,7 +19,9 @@ ENTRY_POINTS = ("longer_workspace_bytes", "longer_kv_cache_bytes", "longer_inner
                 "longer_score_candidates_static", "longer_probe_rate",
                 "longer_backward_workspace_bytes", "longer_block_grad_floats", "longer_token_merge_backward",
                 "longer_model_grad_floats", "longer_forward_backward_workspace_bytes", "longer_forward_backward",
-                "longer_input_backward_workspace_bytes", "longer_input_grad_floats", "longer_input_generation_backward")
+                "longer_input_backward_workspace_bytes", "longer_input_grad_floats", "longer_input_generation_backward",
+                "longer_layer_norm", "longer_layer_norm_backward_workspace_bytes", "longer_layer_norm_backward",
+                "longer_grad_norm_workspace_bytes", "longer_grad_norm", "longer_clip_gradients", "longer_adamw_step")
 
 
 class LongerError(RuntimeError):
@@ -47,6 +49,23 @@ class CWeights(ctypes.Structure):
 
 class CInputWeights(ctypes.Structure):
     _fields_ = [(f, ctypes.c_void_p) for f in ("pos", "w1", "b1", "w2", "b2")]
+
+
+class CRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("user_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class CTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class CAdamWTensor(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in "pmvgw"] + [("n", ctypes.c_int64), ("g_dtype", ctypes.c_int32),
+                                                          ("w_dtype", ctypes.c_int32), ("decay", ctypes.c_double)]
+
+
+class CAdamW(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_double) for f in ("lr", "beta1", "beta2", "eps")] + [("step", ctypes.c_int64)]
 
 
 def library_path() -> str:
@@ -102,6 +121,16 @@ def load_library() -> ctypes.CDLL:
     lib.longer_input_grad_floats.argtypes = [cfgp, i32, i32]
     lib.longer_input_generation_backward.argtypes = [cfgp, ctypes.POINTER(CInputWeights), vp, vp, vp, i32, i32, i32, vp, vp, vp, vp,
                                                      vp, sz, vp]
+    rowsp = ctypes.POINTER(CRows)
+    lib.longer_layer_norm.argtypes = [rowsp, vp, vp, vp, i32, i32, i32, ctypes.c_float, rowsp, vp]
+    lib.longer_layer_norm_backward_workspace_bytes.restype = sz
+    lib.longer_layer_norm_backward_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.longer_layer_norm_backward.argtypes = [rowsp, vp, rowsp, vp, i32, i32, i32, ctypes.c_float, rowsp, vp, vp, sz, vp]
+    lib.longer_grad_norm_workspace_bytes.restype = sz
+    lib.longer_grad_norm_workspace_bytes.argtypes = [ctypes.POINTER(CTensor), i32]
+    lib.longer_grad_norm.argtypes = [ctypes.POINTER(CTensor), i32, ctypes.c_float, vp, vp, sz, vp]
+    lib.longer_clip_gradients.argtypes = [ctypes.POINTER(CTensor), ctypes.POINTER(CTensor), i32, vp, vp]
+    lib.longer_adamw_step.argtypes = [ctypes.POINTER(CAdamWTensor), i32, ctypes.POINTER(CAdamW), vp, vp]
     lib.longer_last_error.restype = ctypes.c_char_p
     lib.longer_probe_mfma_layout.argtypes = [vp, vp]
     lib.longer_stage_timing.argtypes = [i32]
@@ -110,7 +139,8 @@ def load_library() -> ctypes.CDLL:
         if name not in ("longer_workspace_bytes", "longer_kv_cache_bytes", "longer_packed_weights_bytes", "longer_last_error",
                         "longer_backward_workspace_bytes", "longer_block_grad_floats", "longer_model_grad_floats",
                         "longer_forward_backward_workspace_bytes", "longer_input_backward_workspace_bytes",
-                        "longer_input_grad_floats"):
+                        "longer_input_grad_floats", "longer_layer_norm_backward_workspace_bytes",
+                        "longer_grad_norm_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     _LIB = lib
     return lib
@@ -468,3 +498,133 @@ def longer_input_generation_backward(ccfg, weights, E, tdiff, lens, B, L, d_e, d
                                                            _ptr(lens), B, L, d_e, _ptr(dH), _ptr(dE_out), _ptr(dtdiff_out),
                                                            _ptr(grads_out), _ptr(ws), ws.numel(), _stream(stream)),
            "longer_input_generation_backward")
+
+
+# ----------------------------------------------------------------------------- the training step around the gradients
+def _tensor_dtype(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise LongerError("tensors are float32 or bfloat16, not %s" % t.dtype)
+
+
+def _rows(t, B, L, d, name) -> CRows:
+    if not t.is_cuda or t.shape != (B, L, d):
+        raise LongerError("%s must be a device tensor [%d, %d, %d]" % (name, B, L, d))
+    su, sr, sc = t.stride()
+    if d > 1 and sc != 1:
+        raise LongerError("%s: the values of a row must be adjacent" % name)
+    return CRows(t.data_ptr(), su, sr, _tensor_dtype(t))
+
+
+def _vector(t, n, dtype, name):
+    if t.dtype != dtype or t.numel() != n:
+        raise LongerError("%s must hold %d values of %s" % (name, n, dtype))
+    return _ptr(t)
+
+
+def _lens(lens, B):
+    import torch
+    return None if lens is None else _vector(lens, B, torch.int32, "lens")
+
+
+def longer_layer_norm(X, ln_g, ln_b, lens, eps, Y_out, stream=None):
+    """Layer norm of the rows of X [B, L, d] into Y_out (X itself, or a tensor that does not overlap it); values of a row are
+    adjacent, rows and users may have any strides."""
+    _require_gpu()
+    if X.dim() != 3:
+        raise LongerError("X must be a device tensor [B, L, d]")
+    B, L, d = X.shape
+    x, y = _rows(X, B, L, d, "X"), _rows(Y_out, B, L, d, "Y_out")
+    _check(load_library().longer_layer_norm(ctypes.byref(x), _vector(ln_g, d, X.dtype, "ln_g"), _vector(ln_b, d, X.dtype, "ln_b"),
+                                            _lens(lens, B), B, L, d, eps, ctypes.byref(y), _stream(stream)), "longer_layer_norm")
+
+
+def longer_layer_norm_backward_workspace_bytes(B: int, L: int, d: int) -> int:
+    return int(load_library().longer_layer_norm_backward_workspace_bytes(B, L, d))
+
+
+def longer_layer_norm_backward(X, ln_g, dY, lens, eps, dX_out, grads_out, ws, stream=None):
+    """Gradients of longer_layer_norm: dX_out like dY (float32, or X's type), grads_out float32 [2, d] (ln_g, ln_b)."""
+    import torch
+    _require_gpu()
+    if X.dim() != 3:
+        raise LongerError("X must be a device tensor [B, L, d]")
+    B, L, d = X.shape
+    x, dy, dx = _rows(X, B, L, d, "X"), _rows(dY, B, L, d, "dY"), _rows(dX_out, B, L, d, "dX_out")
+    _check(load_library().longer_layer_norm_backward(ctypes.byref(x), _vector(ln_g, d, X.dtype, "ln_g"), ctypes.byref(dy),
+                                                     _lens(lens, B), B, L, d, eps, ctypes.byref(dx),
+                                                     _vector(grads_out, 2 * d, torch.float32, "grads_out"), _ptr(ws),
+                                                     ws.numel() * ws.element_size(), _stream(stream)), "longer_layer_norm_backward")
+
+
+class TensorList:
+    """Dense device tensors (float32 or bfloat16, any shapes) as longer_grad_norm and longer_clip_gradients take them.
+    The list holds the tensors and their addresses: make it once, for buffers that stay."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.array = (CTensor * max(1, len(self.tensors)))(*[CTensor(_ptr(t), t.numel(), _tensor_dtype(t)) for t in self.tensors])
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+class AdamWList:
+    """Parameters as longer_adamw_step takes them: tensor by tensor the float32 master values p and moments m and v, the
+    gradient g, the copy w in the model's type (None: there is none) and its weight decay.  Made once, as a TensorList."""
+
+    def __init__(self, p, m, v, g, w, decay):
+        import torch
+        p, m, v, g = list(p), list(m), list(v), list(g)
+        w = [None] * len(p) if w is None else list(w)
+        decay = list(decay)
+        if not len(p) == len(m) == len(v) == len(g) == len(w) == len(decay):
+            raise LongerError("p, m, v, g, w and decay must have one entry for each parameter")
+        self.tensors = (p, m, v, g, w)
+        self.array = (CAdamWTensor * max(1, len(p)))()
+        for i, (c, a) in enumerate(zip(decay, self.array)):
+            n = p[i].numel()
+            for name, t in zip("pmv", (p[i], m[i], v[i])):
+                setattr(a, name, _vector(t, n, torch.float32, "%s[%d]" % (name, i)))
+            a.g, a.g_dtype = _vector(g[i], n, g[i].dtype, "g[%d]" % i), _tensor_dtype(g[i])
+            if w[i] is not None:
+                a.w, a.w_dtype = _vector(w[i], n, w[i].dtype, "w[%d]" % i), _tensor_dtype(w[i])
+            a.n, a.decay = n, c
+
+    def __len__(self):
+        return len(self.tensors[0])
+
+
+def longer_grad_norm_workspace_bytes(grads: TensorList) -> int:
+    return int(load_library().longer_grad_norm_workspace_bytes(grads.array, len(grads)))
+
+
+def longer_grad_norm(grads: TensorList, max_norm, norm_out, ws, stream=None):
+    """norm_out (float32 [2]) = the global norm of the list, and the factor that bounds it by max_norm."""
+    import torch
+    _require_gpu()
+    _check(load_library().longer_grad_norm(grads.array, len(grads), max_norm, _vector(norm_out, 2, torch.float32, "norm_out"),
+                                           _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "longer_grad_norm")
+
+
+def longer_clip_gradients(grads: TensorList, norm, out: Optional[TensorList] = None, stream=None):
+    """out (None: the gradients themselves) = the gradients times the factor in norm, as longer_grad_norm left it."""
+    import torch
+    _require_gpu()
+    if out is not None and len(out) != len(grads):
+        raise LongerError("out must have a tensor for each gradient")
+    _check(load_library().longer_clip_gradients(grads.array, None if out is None else out.array, len(grads),
+                                                _vector(norm, 2, torch.float32, "norm"), _stream(stream)), "longer_clip_gradients")
+
+
+def longer_adamw_step(params: AdamWList, norm, lr, beta1, beta2, eps, step, stream=None):
+    """One AdamW update of every parameter of the list, its gradient scaled by the factor in norm (None: by 1)."""
+    import torch
+    _require_gpu()
+    how = CAdamW(lr, beta1, beta2, eps, step)
+    _check(load_library().longer_adamw_step(params.array, len(params), ctypes.byref(how),
+                                            None if norm is None else _vector(norm, 2, torch.float32, "norm"), _stream(stream)),
+           "longer_adamw_step")

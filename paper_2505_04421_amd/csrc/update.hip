@@ -1,0 +1,318 @@
+// Behind the gradients: their global norm and clipping, and the AdamW update (longer_grad_norm, longer_clip_gradients,
+// longer_adamw_step).
+#include "../../include/longer.h"
+#include "device.h"
+
+#include <cmath>
+
+namespace longer {
+
+int api_error(int code, const char* fmt, ...);   // longer_api.hip
+
+namespace upd {
+
+// A launch takes its tensors in its arguments (under 4 KB of them), so a call needs no table in device memory and
+// keeps none.  (Arrays of 4 and 8 byte elements only: beside a byte array the compiler takes the others by scalar loads from a base
+// that is off a multiple of 4, and scalar loads drop the two low bits of each part of their address.)  Each tensor is cut into pieces of 2^shift values, numbered over the launch's list; a workgroup takes one.
+struct Piece { int t; int64_t begin; };
+
+// first[i] = number of tensor i's first piece, ascending: the last i with first[i] <= b (an empty tensor has its
+// successor's number and is never the last one)
+template <int N>
+__device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int count, uint32_t b, int shift) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < N; k += 64) {
+    const int i = k + lane;
+    n += __popcll(__ballot(i < count && first[i < N ? i : 0] <= b));
+  }
+  return {n - 1, (int64_t)(b - first[n - 1]) << shift};
+}
+
+constexpr int kNormList = 192, kClipList = 128, kStepList = 64;
+constexpr int64_t kHalf = (int64_t)1 << 62;         // in a tensor's size: its values (an update's gradients) are bf16
+constexpr int64_t kHalfW = (int64_t)1 << 61;        // and the update's copy w is
+constexpr int64_t kCount = kHalfW - 1;
+
+struct NormArgs {
+  const void* data[kNormList];
+  int64_t n[kNormList];
+  uint32_t first[kNormList];
+  int count, shift;
+};
+struct ClipArgs {
+  const void* in[kClipList];
+  void* out[kClipList];
+  int64_t n[kClipList];
+  uint32_t first[kClipList];
+  int count, shift;
+  const float* norm;
+};
+struct StepArgs {
+  float *p[kStepList], *m[kStepList], *v[kStepList];
+  const void* g[kStepList];
+  void* w[kStepList];
+  int64_t n[kStepList];
+  uint32_t first[kStepList];
+  float decay[kStepList];                            // lr * decay
+  int count, shift;
+  const float* norm;
+  float beta1, one_beta1, beta2, one_beta2, rate, root, eps;   // rate = lr / (1 - beta1^t), root = 1 / sqrt(1 - beta2^t)
+};
+
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.;
+  for (unsigned w = 0; w < blockDim.x / 64; ++w) v += lds[w];
+  return v;
+}
+
+__global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
+  __shared__ double lds[4];
+  const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
+  const int64_t n = a.n[w.t] & kCount, end = min(n, w.begin + ((int64_t)1 << a.shift));
+  double s = 0.;
+  if (a.n[w.t] & kHalf) {
+    const __bf16* g = (const __bf16*)a.data[w.t];
+    for (int64_t i = w.begin + threadIdx.x; i < end; i += 256) { const double v = (float)g[i]; s = fma(v, v, s); }
+  } else {
+    const float* g = (const float*)a.data[w.t];
+    for (int64_t i = w.begin + threadIdx.x; i < end; i += 256) { const double v = g[i]; s = fma(v, v, s); }
+  }
+  s = block_sum(s, lds);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(1024) void norm_join_kernel(const double* part, uint32_t n, float max_norm, float* norm) {
+  __shared__ double lds[16];
+  double s = 0.;
+  for (uint32_t i = threadIdx.x; i < n; i += 1024) s += part[i];
+  s = block_sum(s, lds);
+  if (threadIdx.x) return;
+  const float v = (float)sqrt(s);
+  norm[0] = v;
+  norm[1] = !isfinite(v) ? 0.f : v <= max_norm ? 1.f : max_norm / v;
+}
+
+template <typename T>
+__device__ __forceinline__ void clip_piece(const T* in, T* out, int64_t begin, int64_t end, float c, bool finite) {
+  for (int64_t i = begin + threadIdx.x; i < end; i += 256) out[i] = finite ? (T)((float)in[i] * c) : (T)0.f;
+}
+
+__global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
+  const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
+  const float c = a.norm[1];
+  const bool finite = isfinite(a.norm[0]);
+  if (c == 1.f && a.in[w.t] == a.out[w.t]) return;
+  const int64_t n = a.n[w.t] & kCount, end = min(n, w.begin + ((int64_t)1 << a.shift));
+  if (a.n[w.t] & kHalf) clip_piece((const __bf16*)a.in[w.t], (__bf16*)a.out[w.t], w.begin, end, c, finite);
+  else clip_piece((const float*)a.in[w.t], (float*)a.out[w.t], w.begin, end, c, finite);
+}
+
+__global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
+  float c = 1.f;
+  if (a.norm) {
+    if (!isfinite(a.norm[0])) return;
+    c = a.norm[1];
+  }
+  const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
+  const int64_t n = a.n[w.t] & kCount, end = min(n, w.begin + ((int64_t)1 << a.shift));
+  const bool half_g = a.n[w.t] & kHalf, half_w = a.n[w.t] & kHalfW;
+  for (int64_t i = w.begin + threadIdx.x; i < end; i += 256) {
+    const float g = c * (half_g ? (float)((const __bf16*)a.g[w.t])[i] : ((const float*)a.g[w.t])[i]);
+    const float m = a.beta1 * a.m[w.t][i] + a.one_beta1 * g;
+    const float v = a.beta2 * a.v[w.t][i] + a.one_beta2 * (g * g);
+    float p = a.p[w.t][i];
+    p -= a.rate * (m / (sqrtf(v) * a.root + a.eps)) + a.decay[w.t] * p;
+    a.m[w.t][i] = m;
+    a.v[w.t][i] = v;
+    a.p[w.t][i] = p;
+    if (a.w[w.t]) {
+      if (half_w) ((__bf16*)a.w[w.t])[i] = (__bf16)p;
+      else ((float*)a.w[w.t])[i] = p;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ host
+static int size_of(int dtype) { return dtype == LONGER_F32 ? 4 : dtype == LONGER_BF16 ? 2 : 0; }
+
+static int launched(const char* what) {
+  return hipGetLastError() == hipSuccess ? 0 : api_error(LONGER_ERR_HIP, "%s launch failed", what);
+}
+
+constexpr int64_t kMostValues = (int64_t)1 << 44;    // of a list: offsets in bytes, and the piece numbers, stay far inside their types
+
+static int check_tensor(const void* p, int64_t n, int dtype, int i, const char* name) {
+  if (n < 0 || n > kMostValues) return api_error(LONGER_ERR_ARG, "tensor %d: n=%lld out of range", i, (long long)n);
+  if (!size_of(dtype)) return api_error(LONGER_ERR_ARG, "tensor %d: dtype %d of %s unknown", i, dtype, name);
+  if (n && !p) return api_error(LONGER_ERR_ARG, "tensor %d: %s is NULL", i, name);
+  if ((uintptr_t)p % size_of(dtype)) return api_error(LONGER_ERR_ARG, "tensor %d: %s is not aligned to its elements", i, name);
+  return 0;
+}
+
+static int check_list(const longer_tensor* t, int count, int64_t* values) {
+  if (!t || count <= 0) return api_error(LONGER_ERR_ARG, "an empty list of tensors");
+  int64_t sum = 0;
+  for (int i = 0; i < count; ++i) {
+    if (int rc = check_tensor(t[i].data, t[i].n, t[i].dtype, i, "data")) return rc;
+    sum += t[i].n;
+    if (sum > kMostValues) return api_error(LONGER_ERR_ARG, "a list of more than 2^44 values");
+  }
+  *values = sum;
+  return 0;
+}
+
+// piece size: at most 4096 pieces beside one more for each tensor
+static int piece_shift(int64_t values) {
+  int s = 12;
+  while ((values >> s) > 4096) ++s;
+  return s;
+}
+static uint32_t pieces(int64_t n, int shift) { return (uint32_t)((n + ((int64_t)1 << shift) - 1) >> shift); }
+
+static uint32_t list_pieces(const longer_tensor* t, int count, int shift) {
+  uint32_t k = 0;
+  for (int i = 0; i < count; ++i) k += pieces(t[i].n, shift);
+  return k;
+}
+static size_t norm_bytes(uint32_t n) { return ((size_t)(n ? n : 1) * 8 + 255) & ~(size_t)255; }
+
+}  // namespace upd
+}  // namespace longer
+
+using namespace longer;
+
+extern "C" {
+
+size_t longer_grad_norm_workspace_bytes(const longer_tensor* grads, int count) {
+  int64_t values;
+  if (upd::check_list(grads, count, &values)) return 0;
+  return upd::norm_bytes(upd::list_pieces(grads, count, upd::piece_shift(values)));
+}
+
+int longer_grad_norm(const longer_tensor* grads, int count, float max_norm, float* norm_out,
+                     void* ws, size_t ws_bytes, void* stream) {
+  int64_t values;
+  if (int rc = upd::check_list(grads, count, &values)) return rc;
+  if (!norm_out || !ws) return api_error(LONGER_ERR_ARG, "null pointer argument");
+  if ((uintptr_t)norm_out & 3) return api_error(LONGER_ERR_ARG, "norm_out is not aligned");
+  if ((uintptr_t)ws & 255) return api_error(LONGER_ERR_ARG, "ws must be 256-byte aligned");
+  if (!(max_norm > 0.f)) return api_error(LONGER_ERR_ARG, "max_norm must be positive");
+  const int shift = upd::piece_shift(values);
+  const uint32_t all = upd::list_pieces(grads, count, shift);
+  if (ws_bytes < upd::norm_bytes(all)) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, upd::norm_bytes(all));
+  hipStream_t st = (hipStream_t)stream;
+  uint32_t done = 0;
+  for (int i = 0; i < count;) {
+    upd::NormArgs a;
+    a.count = 0;
+    a.shift = shift;
+    uint32_t k = 0;
+    for (; i < count && a.count < upd::kNormList; ++i) {
+      if (!grads[i].n) continue;
+      a.data[a.count] = grads[i].data;
+      a.n[a.count] = grads[i].n | (grads[i].dtype == LONGER_BF16 ? upd::kHalf : 0);
+      a.first[a.count++] = k;
+      k += upd::pieces(grads[i].n, shift);
+    }
+    if (!k) break;
+    upd::norm_kernel<<<k, 256, 0, st>>>(a, (double*)ws + done);
+    done += k;
+  }
+  upd::norm_join_kernel<<<1, 1024, 0, st>>>((const double*)ws, done, max_norm, norm_out);
+  return upd::launched("gradient norm");
+}
+
+int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, int count, const float* norm, void* stream) {
+  int64_t values;
+  if (int rc = upd::check_list(grads, count, &values)) return rc;
+  if (out) {
+    if (int rc = upd::check_list(out, count, &values)) return rc;
+    for (int i = 0; i < count; ++i)
+      if (out[i].n != grads[i].n || out[i].dtype != grads[i].dtype) return api_error(LONGER_ERR_ARG, "tensor %d: out has another size or dtype", i);
+  }
+  if (!norm || ((uintptr_t)norm & 3)) return api_error(LONGER_ERR_ARG, "norm is NULL or not aligned");
+  const int shift = upd::piece_shift(values);
+  hipStream_t st = (hipStream_t)stream;
+  for (int i = 0; i < count;) {
+    upd::ClipArgs a;
+    a.count = 0;
+    a.shift = shift;
+    a.norm = norm;
+    uint32_t k = 0;
+    for (; i < count && a.count < upd::kClipList; ++i) {
+      if (!grads[i].n) continue;
+      a.in[a.count] = grads[i].data;
+      a.out[a.count] = out ? out[i].data : grads[i].data;
+      a.n[a.count] = grads[i].n | (grads[i].dtype == LONGER_BF16 ? upd::kHalf : 0);
+      a.first[a.count++] = k;
+      k += upd::pieces(grads[i].n, shift);
+    }
+    if (k) upd::clip_kernel<<<k, 256, 0, st>>>(a);
+  }
+  return upd::launched("gradient clipping");
+}
+
+int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adamw* how, const float* norm, void* stream) {
+  if (!t || count <= 0) return api_error(LONGER_ERR_ARG, "an empty list of tensors");
+  if (!how) return api_error(LONGER_ERR_ARG, "how is NULL");
+  if (!(how->lr >= 0.) || !std::isfinite(how->lr)) return api_error(LONGER_ERR_ARG, "lr=%g: not negative, finite", how->lr);
+  if (!(how->beta1 >= 0. && how->beta1 < 1.) || !(how->beta2 >= 0. && how->beta2 < 1.)) return api_error(LONGER_ERR_ARG, "beta1=%g beta2=%g: 0 to below 1", how->beta1, how->beta2);
+  if (!(how->eps > 0.) || !std::isfinite(how->eps)) return api_error(LONGER_ERR_ARG, "eps=%g must be positive", how->eps);
+  if (how->step < 1) return api_error(LONGER_ERR_ARG, "step=%lld: counts from 1", (long long)how->step);
+  if ((uintptr_t)norm & 3) return api_error(LONGER_ERR_ARG, "norm is not aligned");
+  int64_t values = 0;
+  for (int i = 0; i < count; ++i) {
+    int rc = upd::check_tensor(t[i].p, t[i].n, LONGER_F32, i, "p");
+    if (!rc) rc = upd::check_tensor(t[i].m, t[i].n, LONGER_F32, i, "m");
+    if (!rc) rc = upd::check_tensor(t[i].v, t[i].n, LONGER_F32, i, "v");
+    if (!rc) rc = upd::check_tensor(t[i].g, t[i].n, t[i].g_dtype, i, "g");
+    if (!rc && t[i].w) rc = upd::check_tensor(t[i].w, t[i].n, t[i].w_dtype, i, "w");
+    if (rc) return rc;
+    if (!(t[i].decay >= 0.) || !std::isfinite(t[i].decay)) return api_error(LONGER_ERR_ARG, "tensor %d: decay=%g: not negative, finite", i, t[i].decay);
+    const void* at[5] = {t[i].p, t[i].m, t[i].v, t[i].g, t[i].w};
+    for (int j = 0; j < 5; ++j)
+      for (int k = 0; k < j; ++k)
+        if (t[i].n && at[j] && at[j] == at[k]) return api_error(LONGER_ERR_ARG, "tensor %d: two of p, m, v, g, w are the same memory", i);
+    values += t[i].n;
+    if (values > upd::kMostValues) return api_error(LONGER_ERR_ARG, "a list of more than 2^44 values");
+  }
+  const int shift = upd::piece_shift(values);
+  hipStream_t st = (hipStream_t)stream;
+  for (int i = 0; i < count;) {
+    upd::StepArgs a;
+    a.count = 0;
+    a.shift = shift;
+    a.norm = norm;
+    a.beta1 = (float)how->beta1;
+    a.one_beta1 = (float)(1. - how->beta1);
+    a.beta2 = (float)how->beta2;
+    a.one_beta2 = (float)(1. - how->beta2);
+    a.rate = (float)(how->lr / (1. - std::pow(how->beta1, (double)how->step)));
+    a.root = (float)(1. / std::sqrt(1. - std::pow(how->beta2, (double)how->step)));
+    a.eps = (float)how->eps;
+    uint32_t k = 0;
+    for (; i < count && a.count < upd::kStepList; ++i) {
+      if (!t[i].n) continue;
+      const int j = a.count++;
+      a.p[j] = t[i].p;
+      a.m[j] = t[i].m;
+      a.v[j] = t[i].v;
+      a.g[j] = t[i].g;
+      a.w[j] = t[i].w;
+      a.n[j] = t[i].n | (t[i].g_dtype == LONGER_BF16 ? upd::kHalf : 0) | (t[i].w && t[i].w_dtype == LONGER_BF16 ? upd::kHalfW : 0);
+      a.decay[j] = (float)(how->lr * t[i].decay);
+      a.first[j] = k;
+      k += upd::pieces(t[i].n, shift);
+    }
+    if (k) upd::step_kernel<<<k, 256, 0, st>>>(a);
+  }
+  return upd::launched("AdamW update");
+}
+
+}  // extern "C"

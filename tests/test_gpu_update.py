@@ -1,0 +1,237 @@
+"""longer_grad_norm, longer_clip_gradients and longer_adamw_step against the formulas in 64 bits: lists from one value to hundreds
+of tensors, mixed types, any alignment, empty tensors, gradients that are not finite, tensors beyond 2^31 values.
+
+Tolerances.  u = 2^-24.  The norm's squares and sums are exact to far below u, so it is off by one rounding to fp32; the factor by
+that, the division's and its own: 4 u.  A clipped value adds one rounding (bf16, with its 8 significant bits: 2^-8).  Moments and parameters are a handful of
+fp32 operations of known magnitudes: 24 u of the sum of the magnitudes covers them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_04421_amd as lg
+from gpu_util import guarded_empty
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+SIZES = {
+    "one": [1],
+    "few": [3, 0, 1, 128],
+    "edges": [4095, 4096, 4097, 1, 8191, 8193, 65, 63, 2, 0, 12289],
+    "block": [128, 128, 16384, 128, 16384, 128, 16384, 128, 16384, 128, 128, 128, 65536, 512, 65536, 128, 1024, 1],
+    "many": [(i * 37) % 301 for i in range(401)],
+    "large": [5_000_003, 17, 1 << 20, 999_999],
+}
+
+
+def lists(names, sizes, mixed, pad, seed=0, scale=1.0):
+    """Tensors of `sizes` one behind the other with `pad` NaN between them: float32, or (mixed) every second one bfloat16."""
+    r = torch.Generator().manual_seed(seed)
+    out = []
+    for name in names:
+        ts = []
+        for i, n in enumerate(sizes):
+            t = torch.bfloat16 if mixed and (i + len(name)) % 2 else torch.float32
+            buf = torch.full((n + 2 * pad,), float("nan"), dtype=t, device=DEV)
+            v = buf[pad:pad + n]
+            v.copy_(torch.randn(n, generator=r) * scale * torch.exp(torch.randn(n, generator=r)))
+            ts.append(v)
+        out.append(ts)
+    return out
+
+
+def np64(t):
+    return t.double().cpu().numpy().reshape(-1)
+
+
+def exact_norm(ts):
+    return math.sqrt(math.fsum(float(np.dot(np64(t), np64(t))) for t in ts))
+
+
+def norm_of(ts, max_norm):
+    tl = lg.TensorList(ts)
+    n = lg.longer_grad_norm_workspace_bytes(tl)
+    assert n > 0, lg.longer_last_error()
+    ws, g1 = guarded_empty(DEV, (n,), torch.uint8)
+    out, g2 = guarded_empty(DEV, (2,), torch.float32)
+    lg.longer_grad_norm(tl, max_norm, out, ws)
+    torch.cuda.synchronize()
+    g1.check("ws")
+    g2.check("norm")
+    return tl, out, ws
+
+
+@pytest.mark.parametrize("pad", [0, 1, 3])
+@pytest.mark.parametrize("mixed", [False, True])
+@pytest.mark.parametrize("which", sorted(SIZES))
+def test_norm_and_clip(which, mixed, pad):
+    print("  longer_grad_norm", which, mixed, pad, flush=True)
+    g, = lists(["g"], SIZES[which], mixed, pad, seed=len(which))
+    want = exact_norm(g)
+    for max_norm in (want / 3, want * 3, float("inf")):
+        tl, norm, ws = norm_of(g, max_norm)
+        c = max_norm / want if max_norm < want else 1.0
+        assert abs(float(norm[0]) - want) <= 2 * U * want
+        assert abs(float(norm[1]) - c) <= 4 * U * c
+        again = torch.empty_like(norm)
+        lg.longer_grad_norm(tl, max_norm, again, ws)
+        assert torch.equal(again, norm)
+        outs, guards = zip(*[guarded_empty(DEV, (t.numel(),), t.dtype) for t in g])
+        lg.longer_clip_gradients(tl, norm, lg.TensorList(outs))
+        for t, o, k in zip(g, outs, guards):
+            k.check("clipped")
+            w = np64(t) * c
+            tol = np.abs(w) * (2.0 ** -8 * 1.01 + 6 * U if t.dtype == torch.bfloat16 else 6 * U) + 2.0 ** -133
+            assert (np.abs(np64(o) - w) <= tol).all()
+            if c == 1.0:
+                assert torch.equal(o, t)
+    # in place: the same bits, and nothing beside the tensors
+    tl, norm, _ = norm_of(g, want / 3)
+    outs = [torch.empty_like(t) for t in g]
+    lg.longer_clip_gradients(tl, norm, lg.TensorList(outs))
+    lg.longer_clip_gradients(tl, norm)
+    for t, o in zip(g, outs):
+        assert torch.equal(t, o)
+        whole = t._base if t._base is not None else t
+        edge = np64(whole)[:pad], np64(whole)[pad + t.numel():]
+        assert np.isnan(edge[0]).all() and np.isnan(edge[1]).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_gradient_that_is_not_finite(bad):
+    g, = lists(["g"], SIZES["block"], True, 1)
+    g[7][g[7].numel() // 2] = bad
+    tl, norm, _ = norm_of(g, 1.0)
+    assert not math.isfinite(float(norm[0])) and float(norm[1]) == 0.0
+    p, m, v = lists(["p", "m", "v"], SIZES["block"], False, 1, seed=4)
+    for t in v:
+        t.abs_()
+    w = [t.to(torch.bfloat16) for t in p]
+    before = [t.clone() for t in p + m + v + w]
+    lg.longer_adamw_step(lg.AdamWList(p, m, v, g, w, [0.1] * len(p)), norm, 1e-2, 0.9, 0.99, 1e-8, 3)
+    for t, b in zip(p + m + v + w, before):
+        assert torch.equal(t, b)
+    lg.longer_clip_gradients(tl, norm)
+    assert all(bool((t == 0).all()) for t in g)
+
+
+def test_values_whose_squares_leave_fp32():
+    for scale in (1e25, 1e-30):
+        g, = lists(["g"], [70_001, 5], False, 1, seed=2, scale=scale)
+        want = exact_norm(g)
+        _, norm, _ = norm_of(g, want / 2)
+        assert abs(float(norm[0]) - want) <= 2 * U * want and abs(float(norm[1]) - 0.5) <= 4 * U
+    z, = lists(["g"], [100], False, 0)
+    z[0].zero_()
+    _, norm, _ = norm_of(z, 1.0)
+    assert norm.tolist() == [0.0, 1.0]
+    z[0].fill_(3e38)                                   # the norm itself is beyond fp32: as an infinity
+    _, norm, _ = norm_of(z, 1.0)
+    assert norm.tolist() == [float("inf"), 0.0]
+
+
+def test_tensors_beyond_2_to_the_31_values():
+    n = (1 << 31) + 77
+    g = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    marks = [0, 12345, (1 << 31) - 1, 1 << 31, (1 << 31) + 3, n - 1]
+    for k, i in enumerate(marks):
+        g[i] = float(k + 1)
+    want = math.sqrt(sum((k + 1) ** 2 for k in range(len(marks))))
+    tl, norm, _ = norm_of([g], want / 2)
+    assert abs(float(norm[0]) - want) <= 2 * U * want
+    lg.longer_clip_gradients(tl, norm)
+    for k, i in enumerate(marks):
+        assert abs(float(g[i]) - (k + 1) / 2) <= (k + 1) * 2.0 ** -8
+    assert int((g != 0).sum()) == len(marks)
+
+
+@pytest.mark.parametrize("pad", [0, 1])
+@pytest.mark.parametrize("which,weights,grads",
+                         [(s, w, g) for s in sorted(SIZES) for w in ("none", "bf16", "f32", "mixed") for g in ("f32", "mixed")
+                          if s != "large" or (w, g) in (("bf16", "f32"), ("mixed", "mixed"))])       # the largest list: two of the combinations
+def test_adamw(which, weights, grads, pad):
+    sizes = SIZES[which]
+    print("  longer_adamw_step", which, weights, grads, pad, flush=True)
+    g, = lists(["g"], sizes, grads == "mixed", pad, seed=1, scale=0.01)
+    p, m, v = lists(["p", "m", "v"], sizes, False, pad, seed=2, scale=0.05)
+    for t in v:
+        t.square_()
+    for t in m + v:
+        t[::5] = 0.0
+    w = None
+    if weights != "none":
+        w, = lists(["w"], sizes, weights == "mixed", pad, seed=3)
+        if weights == "bf16":
+            w = [t.to(torch.bfloat16) for t in w]
+        if weights == "mixed" and len(w) > 2:
+            w[2] = None
+    decay = [0.1 * (i % 3) for i in range(len(sizes))]
+    lr, b1, b2, eps = 1e-2, 0.9, 0.999, 1e-8
+    params = lg.AdamWList(p, m, v, g, w, decay)
+    norm_exact = exact_norm(g)
+    for step, max_norm in ((1, None), (2, norm_exact / 4), (1000, norm_exact * 4)):
+        old = [[np64(t) for t in ts] for ts in (p, m, v)]
+        c, norm = 1.0, None
+        if max_norm is not None:
+            c, norm = min(1.0, max_norm / norm_exact), norm_of(g, max_norm)[1]
+        keep = [t.clone() for t in g]
+        lg.longer_adamw_step(params, norm, lr, b1, b2, eps, step)
+        torch.cuda.synchronize()
+        for i in range(len(sizes)):
+            p0, m0, v0 = (o[i] for o in old)
+            gi = c * np64(g[i])
+            assert torch.equal(g[i], keep[i])
+            m1, v1 = b1 * m0 + (1 - b1) * gi, b2 * v0 + (1 - b2) * gi * gi
+            den = np.sqrt(v1 / (1 - b2 ** step)) + eps
+            rate = lr / (1 - b1 ** step)
+            p1 = p0 - rate * m1 / den - lr * decay[i] * p0
+            ma = b1 * np.abs(m0) + (1 - b1) * np.abs(gi)
+            for got, want, mag in ((m[i], m1, ma), (v[i], v1, v1), (p[i], p1, np.abs(p0) + rate * ma / den)):
+                off = np.abs(np64(got) - want)
+                assert (off <= 24 * U * mag + 2.0 ** -140).all(), (i, step)
+            if w is not None and w[i] is not None:
+                assert torch.equal(w[i], p[i].to(w[i].dtype))
+    for t in p + m + v:
+        whole = t._base if t._base is not None else t
+        assert int(torch.isnan(whole).sum()) == whole.numel() - t.numel()
+
+
+def test_step_on_another_stream_and_in_a_graph():
+    sizes = SIZES["block"] * 6
+    g, p, m, v = lists(["g", "p", "m", "v"], sizes, False, 0, seed=5, scale=0.1)
+    for t in v:
+        t.square_()
+    start = [t.clone() for t in p + m + v]
+    w = [torch.empty(t.numel(), dtype=torch.bfloat16, device=DEV) for t in p]
+    params, tl = lg.AdamWList(p, m, v, g, w, [0.0] * len(p)), lg.TensorList(g)
+    ws = torch.empty(lg.longer_grad_norm_workspace_bytes(tl), dtype=torch.uint8, device=DEV)
+    norm = torch.empty(2, device=DEV)
+
+    def step(stream=None):
+        lg.longer_grad_norm(tl, 0.5, norm, ws, stream=stream)
+        lg.longer_adamw_step(params, norm, 1e-3, 0.9, 0.99, 1e-8, 7, stream=stream)
+
+    def back():
+        for t, b in zip(p + m + v, start):
+            t.copy_(b)
+
+    step()
+    want = [t.clone() for t in p + m + v + w]
+    back()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    step(s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(p + m + v + w, want))
+    back()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        back()
+        norm.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(p + m + v + w, want))
