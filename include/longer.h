@@ -337,7 +337,7 @@ typedef struct { void* data; int64_t user_stride, row_stride; int32_t dtype; } l
 
 /* x -> y, of one dtype, ln_g / ln_b [d] of that dtype.  lens int32 [B] (device) or NULL: rows l >= lens[b] are
  * padding, never read and written as exact zeros.  y may be x itself (same data and strides), else the two may not
- * overlap.  1 <= d <= LONGER_MAX_NORM_WIDTH, B L < 2^31, eps > 0.  Takes no workspace. */
+ * overlap.  1 <= d <= LONGER_MAX_NORM_WIDTH, B L < 2^31 - 2^21, eps a positive normal number.  Takes no workspace. */
 #define LONGER_MAX_NORM_WIDTH 16384
 int longer_layer_norm(const longer_rows* x, const void* ln_g, const void* ln_b, const int32_t* lens,
                       int B, int L, int d, float eps, const longer_rows* y, void* stream);

@@ -1,0 +1,409 @@
+// Layer norm of token rows and its backward pass: one read of a row, everything else in registers.
+//
+// A row of d values is cut into pieces of V values, at most 16 bytes of the narrower type; LPR lanes hold it, NV pieces each (piece
+// lane + LPR i), so a wave holds 64 / LPR rows at once and a row wider than a wave's pieces has a workgroup's lanes.  The statistics
+// take two sums in lanes, the mean and then the centred squares: no cancellation, and the row is there already.
+//
+// Widths that no piece divides: the last piece is moved back to end with the row, so that every access is whole and inside it; its
+// first values (below `lo`) are also its neighbour's, take no part in sums, and are computed and stored twice, to the same bits.
+// Loads and stores are aligned to the element only, which the memory path takes at any address.
+#pragma once
+#include "../../include/longer.h"
+#include "device.h"
+
+namespace longer {
+
+int api_error(int code, const char* fmt, ...);   // longer_api.hip
+
+namespace ln {
+
+struct Rows { char* data; int64_t user, row; };      // strides in elements
+
+struct Params {
+  Rows x, dy, out;                  // out: y, or dx
+  const void *g, *b;
+  const int32_t* lens;
+  int rows, L, d;
+  int step_u, step_l;               // rows from one of a workgroup's turns to its next, as users and rows
+  float eps, inv_d;
+  float* part;                      // backward: [workgroups][2][d] column sums
+};
+
+enum { FULL, PIECES, VALUES };      // what is masked: nothing, whole pieces past the row, values of the last piece too
+
+template <typename T, int V> struct Piece_ { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
+template <typename T, int V> using Piece = typename Piece_<T, V>::type;
+
+template <int CTRL> __device__ __forceinline__ float with_dpp(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+
+// sum over groups of LPR adjacent lanes, in every lane (every lane of the wave takes part)
+template <int LPR>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if constexpr (LPR >= 2) v = with_dpp<0xB1>(v);       // the neighbour's
+  if constexpr (LPR >= 4) v = with_dpp<0x4E>(v);       // the other pair's
+  if constexpr (LPR >= 8) v = with_dpp<0x141>(v);      // mirrored in 8
+  if constexpr (LPR >= 16) v = with_dpp<0x140>(v);     // mirrored in 16
+  if constexpr (LPR >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    const unsigned lo = r[0], hi = r[1];           // (named: a bit cast of a vector's element takes the first one)
+    v = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+  }
+  if constexpr (LPR >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    const unsigned lo = r[0], hi = r[1];           // (named: a bit cast of a vector's element takes the first one)
+    v = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+  }
+  return v;
+}
+
+// Sum of N values over a row's lanes.  Rows of several waves meet in LDS, in one of two places in turn: a wave that writes a place
+// again has passed the barrier of the other one, which every wave reaches after its reads.
+template <int LPR, int THREADS, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float* lds, int turn) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = lanes_sum<(LPR < 64 ? LPR : 64)>(v[k]);
+  if constexpr (LPR > 64) {
+    constexpr int W = THREADS / 64, S = LPR / 64;
+    float* at = lds + turn * 3 * W;
+    const int wave = threadIdx.x / 64;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < N; ++k) at[k * W + wave] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[k] = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) v[k] += at[k * W + wave / S * S + s];
+    }
+  }
+}
+
+// A lane's columns
+template <int V, int LPR, int NV, int MODE>
+struct Columns {
+  int col[NV], lo[NV];              // first column; first value that is its own (V: the piece is past the row)
+  __device__ __forceinline__ Columns(int lane, int d) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + LPR * i) * V;
+      col[i] = MODE == FULL ? c : min(c, d - V);
+      lo[i] = MODE == FULL ? 0 : min(c - col[i], V);
+    }
+  }
+  __device__ __forceinline__ bool there(int i) const { return MODE == FULL || lo[i] < V; }
+  __device__ __forceinline__ bool own(int i, int j) const { return MODE == FULL || (MODE == PIECES ? lo[i] < V : j >= lo[i]); }
+};
+
+// A workgroup's walk over the rows: its next turns' places, and the lengths of their users asked for one turn ahead of the rows.
+struct Walk {
+  int r, u, l, n;
+  __device__ __forceinline__ Walk(const Params& p, int first) {
+    r = first;
+    u = (unsigned)first / (unsigned)p.L;
+    l = first - u * p.L;
+    ask(p);
+  }
+  __device__ __forceinline__ void ask(const Params& p) { n = p.lens && r < p.rows ? p.lens[u] : p.L; }
+  __device__ __forceinline__ bool valid(const Params& p) const { return r < p.rows && l < n; }
+  __device__ __forceinline__ Walk next(const Params& p, int step) const {
+    Walk w = *this;
+    w.r = r + step;                           // (at most two turns past the last row: the host keeps that below 2^31)
+    w.u += p.step_u;
+    w.l += p.step_l;
+    if (w.l >= p.L) { w.l -= p.L; ++w.u; }
+    w.ask(p);
+    return w;
+  }
+};
+
+template <typename T, int V, int LPR, int NV, int MODE>
+__device__ __forceinline__ void load_row(Piece<T, V> (&x)[NV], const Rows& r, const Walk& at, bool ok, const Columns<V, LPR, NV, MODE>& c) {
+  const T* row = (const T*)r.data + at.u * r.user + at.l * r.row;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    x[i] = (Piece<T, V>)(T)0.f;
+    if (ok && c.there(i)) x[i] = *(const Piece<T, V>*)(row + c.col[i]);
+  }
+}
+
+template <typename T, int V, int NV, int LPR, int MODE>
+__device__ __forceinline__ void load_vector(float (&v)[NV][V], const void* p, const Columns<V, LPR, NV, MODE>& c) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    Piece<T, V> w = (Piece<T, V>)(T)0.f;
+    if (c.there(i)) w = *(const Piece<T, V>*)((const T*)p + c.col[i]);
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[i][j] = (float)w[j];
+  }
+}
+
+// y = (x - mean) / sqrt(var + eps) g + b
+template <typename T, int V, int LPR, int NV, int MODE, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
+  constexpr int RPB = THREADS / LPR;
+  __shared__ float lds[LPR > 64 ? 6 * (THREADS / 64) : 1];
+  const Columns<V, LPR, NV, MODE> c(threadIdx.x % LPR, p.d);
+  float g[NV][V], b[NV][V];
+  load_vector<T>(g, p.g, c);
+  load_vector<T>(b, p.b, c);
+  const int step = gridDim.x * RPB;
+  Walk at(p, blockIdx.x * RPB + threadIdx.x / LPR);
+  bool ok = at.valid(p);
+  Piece<T, V> x[NV];
+  load_row<T>(x, p.x, at, ok, c);
+  Walk ahead = at.next(p, step);
+  for (int first = blockIdx.x * RPB; first < p.rows; first += step) {
+    // the next turn's rows are under way while this one's are worked on
+    const bool ok_ahead = ahead.valid(p);
+    Piece<T, V> x_ahead[NV];
+    load_row<T>(x_ahead, p.x, ahead, ok_ahead, c);
+    const Walk ahead2 = ahead.next(p, step);
+    float y[NV][V];
+    if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : ok) {       // (a row of several waves has its workgroup to itself)
+      float s[1] = {0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          y[i][j] = (float)x[i][j];
+          s[0] += MODE != VALUES || c.own(i, j) ? y[i][j] : 0.f;       // (a piece past the row holds zeros)
+        }
+      row_sum<LPR, THREADS>(s, lds, 0);
+      const float mean = s[0] * p.inv_d;
+      s[0] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          y[i][j] -= mean;
+          const float own = c.own(i, j) ? y[i][j] : 0.f;
+          s[0] = fmaf(own, own, s[0]);
+        }
+      row_sum<LPR, THREADS>(s, lds, 1);
+      const float r = __builtin_amdgcn_rsqf(fmaf(s[0], p.inv_d, p.eps));
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[i][j] = fmaf(y[i][j] * r, g[i][j], b[i][j]);
+    }
+    if (at.r < p.rows) {
+      T* row = (T*)p.out.data + at.u * p.out.user + at.l * p.out.row;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (!c.there(i)) continue;
+        Piece<T, V> w;
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[j] = (T)(ok ? y[i][j] : 0.f);
+        *(Piece<T, V>*)(row + c.col[i]) = w;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) x[i] = x_ahead[i];
+    at = ahead;
+    ok = ok_ahead;
+    ahead = ahead2;
+  }
+}
+
+// dx = r (q - mean(q) - xh mean(q xh)), q = dy g, and the workgroup's share of sum dy xh and sum dy.  The second sum over a row
+// takes the centred squares, q and q (x - mean) at once.
+template <typename T, typename U, int V, int LPR, int NV, int MODE>
+__global__ __launch_bounds__(1024) void grad_kernel(Params p) {
+  constexpr int THREADS = 1024, RPB = THREADS / LPR, GROUPS = LPR < 64 ? THREADS / 64 : RPB, WIDE = LPR * NV * V;
+  constexpr bool AHEAD = NV * V <= 8;                    // room for the next turn's rows (16 waves leave 128 registers each)
+  __shared__ float lds[LPR > 64 ? 6 * (THREADS / 64) : 1];
+  __shared__ float sums[GROUPS > 1 ? 2 * WIDE : 1];
+  const Columns<V, LPR, NV, MODE> c(threadIdx.x % LPR, p.d);
+  float g[NV][V], dg[NV][V], db[NV][V];
+  load_vector<T>(g, p.g, c);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f;
+  const int step = gridDim.x * RPB;
+  Walk at(p, blockIdx.x * RPB + threadIdx.x / LPR);
+  bool ok = at.valid(p);
+  Piece<T, V> x[NV];
+  Piece<U, V> dy[NV];
+  load_row<T>(x, p.x, at, ok, c);
+  load_row<U>(dy, p.dy, at, ok, c);
+  Walk ahead = at.next(p, step);
+  for (int first = blockIdx.x * RPB; first < p.rows; first += step) {
+    const bool ok_ahead = ahead.valid(p);
+    Piece<T, V> x_ahead[NV];
+    Piece<U, V> dy_ahead[NV];
+    if constexpr (AHEAD) {
+      load_row<T>(x_ahead, p.x, ahead, ok_ahead, c);
+      load_row<U>(dy_ahead, p.dy, ahead, ok_ahead, c);
+    }
+    const Walk ahead2 = ahead.next(p, step);
+    float xc[NV][V], k0 = 0.f, k1 = 0.f, k2 = 0.f;      // dx = k0 q + k1 (x - mean) + k2
+    if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : RPB > 1 || ok) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          xc[i][j] = (float)x[i][j];
+          s[0] += MODE != VALUES || c.own(i, j) ? xc[i][j] : 0.f;
+        }
+      row_sum<LPR, THREADS>(s, lds, 0);
+      const float mean = s[0] * p.inv_d;
+      float t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          xc[i][j] -= mean;
+          const float own = c.own(i, j) ? xc[i][j] : 0.f;
+          float q = (float)dy[i][j] * g[i][j];
+          if (MODE == VALUES && !c.own(i, j)) q = 0.f;
+          t[0] = fmaf(own, own, t[0]);
+          t[1] += q;
+          t[2] = fmaf(q, own, t[2]);
+        }
+      row_sum<LPR, THREADS>(t, lds, 1);
+      const float r = __builtin_amdgcn_rsqf(fmaf(t[0], p.inv_d, p.eps));
+      k0 = r;
+      k1 = -(t[2] * p.inv_d) * r * r * r;
+      k2 = -(t[1] * p.inv_d) * r;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float v = (float)dy[i][j];
+          db[i][j] += v;
+          dg[i][j] = fmaf(v, xc[i][j] * r, dg[i][j]);           // (a row that does not count: v = 0, xc = 0)
+          xc[i][j] = fmaf(k0 * v, g[i][j], fmaf(k1, xc[i][j], k2));
+        }
+    }
+    if (at.r < p.rows) {
+      U* row = (U*)p.out.data + at.u * p.out.user + at.l * p.out.row;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (!c.there(i)) continue;
+        Piece<U, V> w;
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[j] = (U)(ok ? xc[i][j] : 0.f);
+        *(Piece<U, V>*)(row + c.col[i]) = w;
+      }
+    }
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) { x[i] = x_ahead[i]; dy[i] = dy_ahead[i]; }
+    } else {
+      load_row<T>(x, p.x, ahead, ok_ahead, c);
+      load_row<U>(dy, p.dy, ahead, ok_ahead, c);
+    }
+    at = ahead;
+    ok = ok_ahead;
+    ahead = ahead2;
+  }
+  // columns: the rows of a wave, then the workgroup's groups of rows, one after the other
+  float* part = p.part + (size_t)blockIdx.x * 2 * p.d;
+  if constexpr (GROUPS == 1) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (c.own(i, j)) { part[c.col[i] + j] = dg[i][j]; part[p.d + c.col[i] + j] = db[i][j]; }
+  } else {
+    if constexpr (LPR < 64) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+          for (int o = LPR; o < 64; o <<= 1) { dg[i][j] += __shfl_xor(dg[i][j], o); db[i][j] += __shfl_xor(db[i][j], o); }
+    }
+    const int group = threadIdx.x / (LPR < 64 ? 64 : LPR);
+    const bool first_rows = LPR >= 64 || (threadIdx.x & 63) < LPR;
+    for (int k = 0; k < GROUPS; ++k) {
+      if (group == k && first_rows)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (c.own(i, j)) {
+              float* at = sums + c.col[i] + j;
+              at[0] = k ? at[0] + dg[i][j] : dg[i][j];
+              at[WIDE] = k ? at[WIDE] + db[i][j] : db[i][j];
+            }
+      __syncthreads();
+    }
+    for (int i = threadIdx.x; i < p.d; i += THREADS) { part[i] = sums[i]; part[p.d + i] = sums[WIDE + i]; }
+  }
+}
+
+// ------------------------------------------------------------------------------------ host
+struct Shape { int lpr, nv, mode, v; };
+
+// lanes and pieces of a row for pieces of `v` values, at most `most` of them a lane
+inline Shape shape(int d, int v, int most) {
+  if (d < v) return {8, 1, PIECES, 1};
+  const int pieces = (d + v - 1) / v;
+  Shape s = {1, 1, 0, v};
+  while (s.lpr < pieces && s.lpr < 64) s.lpr *= 2;
+  if (pieces > 64 * most) s.lpr = pieces > 256 * most ? 1024 : 256;
+  s.nv = (pieces + s.lpr - 1) / s.lpr;
+  s.mode = d % v ? VALUES : pieces == s.lpr * s.nv ? FULL : PIECES;
+  return s;
+}
+
+// The backward launch of one pair of types; the workgroups that it takes (at most `most`), each of which leaves its column sums.
+template <int LPR> inline unsigned grad_groups(const Params& p, unsigned most) {
+  const unsigned turns = ((unsigned)p.rows + 1024 / LPR - 1) / (1024 / LPR);
+  return turns < most ? turns : most;
+}
+
+template <typename T, typename U, int V, int LPR, int NV>
+inline unsigned launch_grad(Params& p, int mode, unsigned most, float* only, hipStream_t st) {
+  const unsigned grid = grad_groups<LPR>(p, most);
+  const int64_t step = (int64_t)grid * (1024 / LPR);
+  p.step_u = (int)(step / p.L);
+  p.step_l = (int)(step % p.L);
+  if (grid == 1) p.part = only;
+  if (mode == FULL) grad_kernel<T, U, V, LPR, NV, FULL><<<grid, 1024, 0, st>>>(p);
+  else if (mode == PIECES) grad_kernel<T, U, V, LPR, NV, PIECES><<<grid, 1024, 0, st>>>(p);
+  else if constexpr (V > 1) grad_kernel<T, U, V, LPR, NV, VALUES><<<grid, 1024, 0, st>>>(p);
+  return grid;
+}
+
+// (8 values a lane, beside their column sums and the next turn's; twice as many where even a workgroup's lanes are too few)
+template <typename T, typename U, int V>
+inline unsigned grad(Params& p, unsigned most, float* only, hipStream_t st) {
+  const Shape s = shape(p.d, V, 8 / V);
+  if (s.v == 1) return launch_grad<T, U, 1, 8, 1>(p, s.mode, most, only, st);
+  switch (s.lpr * 8 + s.nv) {
+    case 1 * 8 + 1: return launch_grad<T, U, V, 1, 1>(p, s.mode, most, only, st);
+    case 2 * 8 + 1: return launch_grad<T, U, V, 2, 1>(p, s.mode, most, only, st);
+    case 4 * 8 + 1: return launch_grad<T, U, V, 4, 1>(p, s.mode, most, only, st);
+    case 8 * 8 + 1: return launch_grad<T, U, V, 8, 1>(p, s.mode, most, only, st);
+    case 16 * 8 + 1: return launch_grad<T, U, V, 16, 1>(p, s.mode, most, only, st);
+    case 32 * 8 + 1: return launch_grad<T, U, V, 32, 1>(p, s.mode, most, only, st);
+    case 64 * 8 + 1: return launch_grad<T, U, V, 64, 1>(p, s.mode, most, only, st);
+    case 256 * 8 + 1: return launch_grad<T, U, V, 256, 1>(p, s.mode, most, only, st);
+    case 1024 * 8 + 1: return launch_grad<T, U, V, 1024, 1>(p, s.mode, most, only, st);
+    case 1024 * 8 + 2: return launch_grad<T, U, V, 1024, 2>(p, s.mode, most, only, st);
+  }
+  if constexpr (V == 4) {
+    switch (s.lpr * 8 + s.nv) {
+      case 64 * 8 + 2: return launch_grad<T, U, V, 64, 2>(p, s.mode, most, only, st);
+      case 256 * 8 + 2: return launch_grad<T, U, V, 256, 2>(p, s.mode, most, only, st);
+      case 1024 * 8 + 3: return launch_grad<T, U, V, 1024, 3>(p, s.mode, most, only, st);
+      case 1024 * 8 + 4: return launch_grad<T, U, V, 1024, 4>(p, s.mode, most, only, st);
+    }
+  }
+  return 0;                          // (no width comes here)
+}
+
+// inst_norm_grad_*.hip
+unsigned grad_f32(Params& p, unsigned most, float* only, hipStream_t st);
+unsigned grad_bf16_f32(Params& p, unsigned most, float* only, hipStream_t st);
+unsigned grad_bf16(Params& p, unsigned most, float* only, hipStream_t st);
+
+}  // namespace ln
+}  // namespace longer

@@ -1,144 +1,42 @@
-// Layer norm of token rows and its backward pass (longer_layer_norm, longer_layer_norm_backward).
-#include "../../include/longer.h"
-#include "device.h"
+// Layer norm of token rows and its backward pass (longer_layer_norm, longer_layer_norm_backward): argument checks and dispatch.
+#include "layer_norm.h"
+
+#include <algorithm>
+#include <cfloat>
 
 namespace longer {
-
-int api_error(int code, const char* fmt, ...);   // longer_api.hip
-
 namespace ln {
 
-struct Rows { char* data; int64_t user, row; };      // strides in elements
-
-struct Params {
-  Rows x, dy, out;                  // out: y, or dx
-  const void *g, *b;
-  const int32_t* lens;
-  int rows, L, d;
-  float eps;
-  float* stats;                     // [rows][2], mean and 1 / sqrt(var + eps)
-};
-
-template <typename T> __device__ __forceinline__ T* row_of(const Rows& r, int u, int l) { return (T*)r.data + u * r.user + l * r.row; }
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
-// a wave per row
-template <typename T>
-__global__ __launch_bounds__(256) void norm_kernel(Params p) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (r >= p.rows) return;
-  const int u = r / p.L, l = r - u * p.L;
-  T* y = row_of<T>(p.out, u, l);
-  if (p.lens && l >= p.lens[u]) {
-    for (int c = lane; c < p.d; c += 64) y[c] = (T)0.f;
-    return;
-  }
-  const T* x = row_of<T>(p.x, u, l);
+// out[c] = sum over the workgroups of part[.][c], 32 columns a workgroup, 32 shares of the sum in a fixed order
+__global__ __launch_bounds__(1024) void join_kernel(const float* part, int slices, int n, float* out) {
+  __shared__ float lds[32][33];
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
   float s = 0.f;
-  for (int c = lane; c < p.d; c += 64) s += (float)x[c];
-  const float mean = wave_sum(s) / p.d;
-  s = 0.f;
-  for (int c = lane; c < p.d; c += 64) { const float v = (float)x[c] - mean; s += v * v; }
-  const float rs = 1.f / sqrtf(wave_sum(s) / p.d + p.eps);
-  for (int c = lane; c < p.d; c += 64) y[c] = (T)(((float)x[c] - mean) * rs * (float)((const T*)p.g)[c] + (float)((const T*)p.b)[c]);
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void stats_kernel(Params p) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (r >= p.rows) return;
-  const int u = r / p.L, l = r - u * p.L;
-  if (p.lens && l >= p.lens[u]) return;
-  const T* x = row_of<T>(p.x, u, l);
-  float s = 0.f;
-  for (int c = lane; c < p.d; c += 64) s += (float)x[c];
-  const float mean = wave_sum(s) / p.d;
-  s = 0.f;
-  for (int c = lane; c < p.d; c += 64) { const float v = (float)x[c] - mean; s += v * v; }
-  const float rs = 1.f / sqrtf(wave_sum(s) / p.d + p.eps);
-  if (lane == 0) { p.stats[2 * (size_t)r] = mean; p.stats[2 * (size_t)r + 1] = rs; }
-}
-
-// (after the column sums: dx may be dy)
-template <typename T, typename U>
-__global__ __launch_bounds__(256) void grad_kernel(Params p) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (r >= p.rows) return;
-  const int u = r / p.L, l = r - u * p.L;
-  U* dx = row_of<U>(p.out, u, l);
-  if (p.lens && l >= p.lens[u]) {
-    for (int c = lane; c < p.d; c += 64) dx[c] = (U)0.f;
-    return;
+  if (c < n) {
+#pragma unroll 8
+    for (int i = share; i < slices; i += 32) s += part[(size_t)i * n + c];
   }
-  const T* x = row_of<T>(p.x, u, l);
-  const U* dy = row_of<U>(p.dy, u, l);
-  const float mean = p.stats[2 * (size_t)r], rs = p.stats[2 * (size_t)r + 1];
-  float q1 = 0.f, q2 = 0.f;
-  for (int c = lane; c < p.d; c += 64) {
-    const float q = (float)dy[c] * (float)((const T*)p.g)[c];
-    q1 += q;
-    q2 += q * (((float)x[c] - mean) * rs);
-  }
-  q1 = wave_sum(q1) / p.d;
-  q2 = wave_sum(q2) / p.d;
-  for (int c = lane; c < p.d; c += 64) {
-    const float q = (float)dy[c] * (float)((const T*)p.g)[c];
-    dx[c] = (U)(rs * (q - q1 - (((float)x[c] - mean) * rs) * q2));
-  }
-}
-
-// column sums over a slice of the rows: a lane per column, a wave per row
-template <typename T, typename U>
-__global__ __launch_bounds__(256) void param_kernel(Params p, float* part) {
-  __shared__ float sum[2][4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-  float dg = 0.f, db = 0.f;
-  for (int r = blockIdx.y * 4 + wave; r < p.rows; r += gridDim.y * 4) {
-    const int u = r / p.L, l = r - u * p.L;
-    if ((p.lens && l >= p.lens[u]) || c >= p.d) continue;
-    const float dy = (float)row_of<U>(p.dy, u, l)[c];
-    dg += dy * (((float)row_of<T>(p.x, u, l)[c] - p.stats[2 * (size_t)r]) * p.stats[2 * (size_t)r + 1]);
-    db += dy;
-  }
-  sum[0][wave][lane] = dg;
-  sum[1][wave][lane] = db;
+  lds[share][threadIdx.x & 31] = s;
   __syncthreads();
-  if (wave < 2 && c < p.d) {
-    float s = 0.f;
-    for (int w = 0; w < 4; ++w) s += sum[wave][w][lane];
-    part[((size_t)blockIdx.y * 2 + wave) * p.d + c] = s;
-  }
-}
-
-__global__ __launch_bounds__(256) void join_kernel(const float* part, int slices, int n, float* out) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= n) return;
-  float s = 0.f;
-  for (int i = 0; i < slices; ++i) s += part[(size_t)i * n + c];
+  if (share || c >= n) return;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) s += lds[i][threadIdx.x];
   out[c] = s;
 }
 
 // ------------------------------------------------------------------------------------ host
-constexpr int kSlices = 64;
-
-struct Workspace { size_t stats, part, total; };
-static Workspace workspace(int B, int L, int d) {
-  Workspace w;
-  w.stats = 0;
-  w.part = ((size_t)B * L * 8 + 255) & ~(size_t)255;
-  w.total = (w.part + (size_t)kSlices * 2 * d * 4 + 255) & ~(size_t)255;
-  return w;
-}
+constexpr int kGradGroups = 512;                    // workgroups of a backward launch: two for each compute unit
 
 static int check_sizes(int B, int L, int d) {
-  if (B <= 0 || L <= 0 || (int64_t)B * L >= ((int64_t)1 << 31)) return api_error(LONGER_ERR_ARG, "B=%d L=%d: at least 1 each, B * L below 2^31", B, L);
+  if (B <= 0 || L <= 0 || (int64_t)B * L >= ((int64_t)1 << 31) - (1 << 21)) return api_error(LONGER_ERR_ARG, "B=%d L=%d: at least 1 each, B * L below 2^31 - 2^21", B, L);
   if (d <= 0 || d > LONGER_MAX_NORM_WIDTH) return api_error(LONGER_ERR_ARG, "d=%d: 1 to %d", d, LONGER_MAX_NORM_WIDTH);
   return 0;
+}
+
+// column sums of every workgroup (of one alone: in their place at once)
+static size_t workspace_bytes(int B, int L, int d) {
+  return ((size_t)std::min<int64_t>((int64_t)B * L, kGradGroups) * 2 * d * 4 + 255) & ~(size_t)255;
 }
 
 static int size_of(int dtype) { return dtype == LONGER_F32 ? 4 : dtype == LONGER_BF16 ? 2 : 0; }
@@ -183,14 +81,42 @@ static int launched(const char* what) {
   return hipGetLastError() == hipSuccess ? 0 : api_error(LONGER_ERR_HIP, "%s launch failed", what);
 }
 
-template <typename T, typename U>
-static int backward(const Params& p, float* part, float* grads, hipStream_t st) {
-  const unsigned grid = (unsigned)(((int64_t)p.rows + 3) / 4);
-  stats_kernel<T><<<grid, 256, 0, st>>>(p);
-  param_kernel<T, U><<<dim3((p.d + 63) / 64, kSlices), 256, 0, st>>>(p, part);
-  join_kernel<<<(2 * p.d + 255) / 256, 256, 0, st>>>(part, kSlices, 2 * p.d, grads);
-  grad_kernel<T, U><<<grid, 256, 0, st>>>(p);
-  return launched("layer norm gradient");
+template <typename T, int V, int LPR, int NV>
+static void launch_norm(Params& p, int mode, hipStream_t st) {
+  constexpr int THREADS = LPR > 256 ? 1024 : 256, RPB = THREADS / LPR;
+  // eight turns a workgroup, so that loading the vectors and the first rows is a small part; fewer where that would leave
+  // compute units idle
+  const int64_t turns = ((int64_t)p.rows + RPB - 1) / RPB;
+  const unsigned grid = (unsigned)std::max((turns + 7) / 8, std::min<int64_t>(turns, 2048 * 256 / THREADS));
+  const int64_t step = (int64_t)grid * RPB;
+  p.step_u = (int)(step / p.L);
+  p.step_l = (int)(step % p.L);
+  if (mode == FULL) norm_kernel<T, V, LPR, NV, FULL, THREADS><<<grid, THREADS, 0, st>>>(p);
+  else if (mode == PIECES) norm_kernel<T, V, LPR, NV, PIECES, THREADS><<<grid, THREADS, 0, st>>>(p);
+  else if constexpr (V > 1) norm_kernel<T, V, LPR, NV, VALUES, THREADS><<<grid, THREADS, 0, st>>>(p);
+}
+
+template <typename T, int V>
+static void norm(Params& p, hipStream_t st) {
+  const Shape s = shape(p.d, V, 4);
+  if (s.v == 1) return launch_norm<T, 1, 8, 1>(p, s.mode, st);
+  switch (s.lpr * 8 + s.nv) {
+    case 1 * 8 + 1: return launch_norm<T, V, 1, 1>(p, s.mode, st);
+    case 2 * 8 + 1: return launch_norm<T, V, 2, 1>(p, s.mode, st);
+    case 4 * 8 + 1: return launch_norm<T, V, 4, 1>(p, s.mode, st);
+    case 8 * 8 + 1: return launch_norm<T, V, 8, 1>(p, s.mode, st);
+    case 16 * 8 + 1: return launch_norm<T, V, 16, 1>(p, s.mode, st);
+    case 32 * 8 + 1: return launch_norm<T, V, 32, 1>(p, s.mode, st);
+    case 64 * 8 + 1: return launch_norm<T, V, 64, 1>(p, s.mode, st);
+    case 64 * 8 + 2: return launch_norm<T, V, 64, 2>(p, s.mode, st);
+    case 64 * 8 + 3: return launch_norm<T, V, 64, 3>(p, s.mode, st);
+    case 64 * 8 + 4: return launch_norm<T, V, 64, 4>(p, s.mode, st);
+    case 256 * 8 + 2: return launch_norm<T, V, 256, 2>(p, s.mode, st);
+    case 256 * 8 + 3: return launch_norm<T, V, 256, 3>(p, s.mode, st);
+    case 256 * 8 + 4: return launch_norm<T, V, 256, 4>(p, s.mode, st);
+    case 1024 * 8 + 2: return launch_norm<T, V, 1024, 2>(p, s.mode, st);
+    default: if constexpr (V < 8) { return s.nv == 3 ? launch_norm<T, V, 1024, 3>(p, s.mode, st) : launch_norm<T, V, 1024, 4>(p, s.mode, st); }
+  }
 }
 
 }  // namespace ln
@@ -209,18 +135,17 @@ int longer_layer_norm(const longer_rows* x, const void* ln_g, const void* ln_b, 
   if (!rc) rc = ln::check_vector(ln_b, x->dtype, "ln_b");
   if (!rc && x->dtype != y->dtype) rc = api_error(LONGER_ERR_ARG, "x and y have one dtype");
   if (!rc) rc = ln::check_alias(x, y, "x and y", B, L);
-  if (!rc && !(eps > 0.f)) rc = api_error(LONGER_ERR_ARG, "eps must be positive");
+  if (!rc && !(eps >= FLT_MIN)) rc = api_error(LONGER_ERR_ARG, "eps must be positive (a normal number)");
   if (!rc && ((uintptr_t)lens & 3)) rc = api_error(LONGER_ERR_ARG, "lens is not aligned");
   if (rc) return rc;
-  const ln::Params p = {ln::rows_of(x, B, L), {}, ln::rows_of(y, B, L), ln_g, ln_b, lens, B * L, L, d, eps, nullptr};
-  const unsigned grid = (unsigned)(((int64_t)B * L + 3) / 4);
-  if (x->dtype == LONGER_F32) ln::norm_kernel<float><<<grid, 256, 0, (hipStream_t)stream>>>(p);
-  else ln::norm_kernel<__bf16><<<grid, 256, 0, (hipStream_t)stream>>>(p);
+  ln::Params p = {ln::rows_of(x, B, L), {}, ln::rows_of(y, B, L), ln_g, ln_b, lens, B * L, L, d, 0, 0, eps, 1.f / d, nullptr};
+  if (x->dtype == LONGER_F32) ln::norm<float, 4>(p, (hipStream_t)stream);
+  else ln::norm<__bf16, 8>(p, (hipStream_t)stream);
   return ln::launched("layer norm");
 }
 
 size_t longer_layer_norm_backward_workspace_bytes(int B, int L, int d) {
-  return ln::check_sizes(B, L, d) ? 0 : ln::workspace(B, L, d).total;
+  return ln::check_sizes(B, L, d) ? 0 : ln::workspace_bytes(B, L, d);
 }
 
 int longer_layer_norm_backward(const longer_rows* x, const void* ln_g, const longer_rows* dy, const int32_t* lens,
@@ -236,19 +161,20 @@ int longer_layer_norm_backward(const longer_rows* x, const void* ln_g, const lon
     rc = api_error(LONGER_ERR_ARG, "dy and dx are both fp32 or both of x's dtype");
   if (!rc) rc = ln::check_alias(dy, dx, "dy and dx", B, L);
   if (!rc && x->data == dx->data) rc = api_error(LONGER_ERR_ARG, "dx may not be x");
-  if (!rc && !(eps > 0.f)) rc = api_error(LONGER_ERR_ARG, "eps must be positive");
+  if (!rc && !(eps >= FLT_MIN)) rc = api_error(LONGER_ERR_ARG, "eps must be positive (a normal number)");
   if (!rc && ((uintptr_t)lens & 3)) rc = api_error(LONGER_ERR_ARG, "lens is not aligned");
   if (!rc && (!ws || ((uintptr_t)ws & 255))) rc = api_error(LONGER_ERR_ARG, "ws must be 256-byte aligned and not NULL");
   if (rc) return rc;
-  const ln::Workspace w = ln::workspace(B, L, d);
-  if (ws_bytes < w.total) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, w.total);
-  const ln::Params p = {ln::rows_of(x, B, L), ln::rows_of(dy, B, L), ln::rows_of(dx, B, L), ln_g, nullptr, lens, B * L, L, d, eps,
-                        (float*)((char*)ws + w.stats)};
-  float* part = (float*)((char*)ws + w.part);
+  const size_t need = ln::workspace_bytes(B, L, d);
+  if (ws_bytes < need) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, need);
+  ln::Params p = {ln::rows_of(x, B, L), ln::rows_of(dy, B, L), ln::rows_of(dx, B, L), ln_g, nullptr, lens, B * L, L, d, 0, 0, eps, 1.f / d,
+                  (float*)ws};
   hipStream_t st = (hipStream_t)stream;
-  if (x->dtype == LONGER_F32) return ln::backward<float, float>(p, part, grads_out, st);
-  if (dy->dtype == LONGER_F32) return ln::backward<__bf16, float>(p, part, grads_out, st);
-  return ln::backward<__bf16, __bf16>(p, part, grads_out, st);
+  const unsigned groups = x->dtype == LONGER_F32 ? ln::grad_f32(p, ln::kGradGroups, grads_out, st)
+                          : dy->dtype == LONGER_F32 ? ln::grad_bf16_f32(p, ln::kGradGroups, grads_out, st)
+                                                    : ln::grad_bf16(p, ln::kGradGroups, grads_out, st);
+  if (groups > 1) ln::join_kernel<<<(2 * d + 31) / 32, 1024, 0, st>>>((const float*)ws, (int)groups, 2 * d, grads_out);
+  return ln::launched("layer norm gradient");
 }
 
 }  // extern "C"
