@@ -187,17 +187,24 @@ def _ptr(t) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     import torch
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream or None
+    if stream is None:           # (the handle itself: a Stream object costs as much time as a launch)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
 
 
+_GPU_SEEN = False
+
+
 def _require_gpu():
+    global _GPU_SEEN
+    if _GPU_SEEN:
+        return
     import torch
     if not torch.cuda.is_available():
         raise LongerError("no GPU visible: the LONGER hot path has no CPU fallback")
+    _GPU_SEEN = True
 
 
 class DeviceModel:
@@ -501,20 +508,25 @@ def longer_input_generation_backward(ccfg, weights, E, tdiff, lens, B, L, d_e, d
 
 
 # ----------------------------------------------------------------------------- the training step around the gradients
+_TENSOR_DTYPES = {}
+
+
 def _tensor_dtype(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return 0
-    if t.dtype == torch.bfloat16:
-        return 1
-    raise LongerError("tensors are float32 or bfloat16, not %s" % t.dtype)
+    code = _TENSOR_DTYPES.get(t.dtype)
+    if code is None:
+        import torch
+        _TENSOR_DTYPES.update({torch.float32: _DTYPE["f32"], torch.bfloat16: _DTYPE["bf16"]})
+        code = _TENSOR_DTYPES.get(t.dtype)
+        if code is None:
+            raise LongerError("tensors are float32 or bfloat16, not %s" % t.dtype)
+    return code
 
 
-def _rows(t, B, L, d, name) -> CRows:
-    if not t.is_cuda or t.shape != (B, L, d):
-        raise LongerError("%s must be a device tensor [%d, %d, %d]" % (name, B, L, d))
+def _rows(t, shape, name) -> CRows:
+    if t.shape != shape or not t.is_cuda:
+        raise LongerError("%s must be a device tensor [%d, %d, %d]" % ((name,) + tuple(shape)))
     su, sr, sc = t.stride()
-    if d > 1 and sc != 1:
+    if sc != 1 and shape[2] > 1:
         raise LongerError("%s: the values of a row must be adjacent" % name)
     return CRows(t.data_ptr(), su, sr, _tensor_dtype(t))
 
@@ -526,8 +538,10 @@ def _vector(t, n, dtype, name):
 
 
 def _lens(lens, B):
+    if lens is None:
+        return None
     import torch
-    return None if lens is None else _vector(lens, B, torch.int32, "lens")
+    return _vector(lens, B, torch.int32, "lens")
 
 
 def longer_layer_norm(X, ln_g, ln_b, lens, eps, Y_out, stream=None):
@@ -536,8 +550,8 @@ def longer_layer_norm(X, ln_g, ln_b, lens, eps, Y_out, stream=None):
     _require_gpu()
     if X.dim() != 3:
         raise LongerError("X must be a device tensor [B, L, d]")
-    B, L, d = X.shape
-    x, y = _rows(X, B, L, d, "X"), _rows(Y_out, B, L, d, "Y_out")
+    B, L, d = shape = X.shape
+    x, y = _rows(X, shape, "X"), _rows(Y_out, shape, "Y_out")
     _check(load_library().longer_layer_norm(ctypes.byref(x), _vector(ln_g, d, X.dtype, "ln_g"), _vector(ln_b, d, X.dtype, "ln_b"),
                                             _lens(lens, B), B, L, d, eps, ctypes.byref(y), _stream(stream)), "longer_layer_norm")
 
@@ -552,8 +566,8 @@ def longer_layer_norm_backward(X, ln_g, dY, lens, eps, dX_out, grads_out, ws, st
     _require_gpu()
     if X.dim() != 3:
         raise LongerError("X must be a device tensor [B, L, d]")
-    B, L, d = X.shape
-    x, dy, dx = _rows(X, B, L, d, "X"), _rows(dY, B, L, d, "dY"), _rows(dX_out, B, L, d, "dX_out")
+    B, L, d = shape = X.shape
+    x, dy, dx = _rows(X, shape, "X"), _rows(dY, shape, "dY"), _rows(dX_out, shape, "dX_out")
     _check(load_library().longer_layer_norm_backward(ctypes.byref(x), _vector(ln_g, d, X.dtype, "ln_g"), ctypes.byref(dy),
                                                      _lens(lens, B), B, L, d, eps, ctypes.byref(dx),
                                                      _vector(grads_out, 2 * d, torch.float32, "grads_out"), _ptr(ws),

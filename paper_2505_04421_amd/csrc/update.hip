@@ -13,11 +13,11 @@ namespace upd {
 
 // A launch takes its tensors in its arguments (under 4 KB of them), so a call needs no table in device memory and
 // keeps none.  (Arrays of 4 and 8 byte elements only: beside a byte array the compiler takes the others by scalar loads from a base
-// that is off a multiple of 4, and scalar loads drop the two low bits of each part of their address.)  Each tensor is cut into pieces of 2^shift values, numbered over the launch's list; a workgroup takes one.
+// that is off a multiple of 4, and scalar loads drop the two low bits of each part of their address.)  Each tensor is cut into
+// pieces of 2^shift values, numbered over the launch's list; a workgroup takes one.
 struct Piece { int t; int64_t begin; };
 
-// first[i] = number of tensor i's first piece, ascending: the last i with first[i] <= b (an empty tensor has its
-// successor's number and is never the last one)
+// first[i] = number of tensor i's first piece, ascending: the last i with first[i] <= b (an empty tensor is not in the list)
 template <int N>
 __device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int count, uint32_t b, int shift) {
   const int lane = threadIdx.x & 63;
@@ -29,6 +29,12 @@ __device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int coun
   }
   return {n - 1, (int64_t)(b - first[n - 1]) << shift};
 }
+
+// 16 bytes of a tensor, aligned to its element only
+template <typename T> struct Line_ { typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
+template <typename T> using Line = typename Line_<T>::type;
+template <typename T> struct Four_ { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
+template <typename T> using Four = typename Four_<T>::type;
 
 constexpr int kNormList = 192, kClipList = 128, kStepList = 64;
 constexpr int64_t kHalf = (int64_t)1 << 62;         // in a tensor's size: its values (an update's gradients) are bf16
@@ -71,18 +77,40 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   return v;
 }
 
+// sum of squares in 64 bits: exact squares, nothing to scale, and no time beside the loads
+template <typename T>
+__device__ __forceinline__ double squares(const T* g, uint32_t n) {
+  constexpr int V = 16 / sizeof(T), U = 4;
+  const uint32_t lines = n / V;
+  double s[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) s[j] = 0.;
+  uint32_t i = threadIdx.x;
+  for (; i + 256 * (U - 1) < lines; i += 256 * U) {
+    Line<T> x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k] = *(const Line<T>*)(g + (size_t)(i + 256 * k) * V);
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) { const double v = (float)x[k][j]; s[j] = fma(v, v, s[j]); }
+  }
+  for (; i < lines; i += 256) {
+    const Line<T> x = *(const Line<T>*)(g + (size_t)i * V);
+#pragma unroll
+    for (int j = 0; j < V; ++j) { const double v = (float)x[j]; s[j] = fma(v, v, s[j]); }
+  }
+  if (lines * V + threadIdx.x < n) { const double v = (float)g[lines * V + threadIdx.x]; s[0] = fma(v, v, s[0]); }
+#pragma unroll
+  for (int j = 1; j < V; ++j) s[0] += s[j];
+  return s[0];
+}
+
 __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
   __shared__ double lds[4];
   const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
-  const int64_t n = a.n[w.t] & kCount, end = min(n, w.begin + ((int64_t)1 << a.shift));
-  double s = 0.;
-  if (a.n[w.t] & kHalf) {
-    const __bf16* g = (const __bf16*)a.data[w.t];
-    for (int64_t i = w.begin + threadIdx.x; i < end; i += 256) { const double v = (float)g[i]; s = fma(v, v, s); }
-  } else {
-    const float* g = (const float*)a.data[w.t];
-    for (int64_t i = w.begin + threadIdx.x; i < end; i += 256) { const double v = g[i]; s = fma(v, v, s); }
-  }
+  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)1 << a.shift);
+  double s = a.n[w.t] & kHalf ? squares((const __bf16*)a.data[w.t] + w.begin, n) : squares((const float*)a.data[w.t] + w.begin, n);
   s = block_sum(s, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
@@ -99,8 +127,25 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double* part, uin
 }
 
 template <typename T>
-__device__ __forceinline__ void clip_piece(const T* in, T* out, int64_t begin, int64_t end, float c, bool finite) {
-  for (int64_t i = begin + threadIdx.x; i < end; i += 256) out[i] = finite ? (T)((float)in[i] * c) : (T)0.f;
+__device__ __forceinline__ void clip_piece(const T* in, T* out, uint32_t n, float c, bool finite) {
+  constexpr int V = 16 / sizeof(T), U = 4;
+  const uint32_t lines = n / V;
+  auto put = [&](uint32_t i, Line<T> x) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = (T)(finite ? (float)x[j] * c : 0.f);
+    *(Line<T>*)(out + (size_t)i * V) = x;
+  };
+  uint32_t i = threadIdx.x;
+  for (; i + 256 * (U - 1) < lines; i += 256 * U) {
+    Line<T> x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k] = *(const Line<T>*)(in + (size_t)(i + 256 * k) * V);
+#pragma unroll
+    for (int k = 0; k < U; ++k) put(i + 256 * k, x[k]);
+  }
+  for (; i < lines; i += 256) put(i, *(const Line<T>*)(in + (size_t)i * V));
+  i = lines * V + threadIdx.x;
+  if (i < n) out[i] = (T)(finite ? (float)in[i] * c : 0.f);
 }
 
 __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
@@ -108,9 +153,68 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
   const float c = a.norm[1];
   const bool finite = isfinite(a.norm[0]);
   if (c == 1.f && a.in[w.t] == a.out[w.t]) return;
-  const int64_t n = a.n[w.t] & kCount, end = min(n, w.begin + ((int64_t)1 << a.shift));
-  if (a.n[w.t] & kHalf) clip_piece((const __bf16*)a.in[w.t], (__bf16*)a.out[w.t], w.begin, end, c, finite);
-  else clip_piece((const float*)a.in[w.t], (float*)a.out[w.t], w.begin, end, c, finite);
+  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)1 << a.shift);
+  if (a.n[w.t] & kHalf) clip_piece((const __bf16*)a.in[w.t] + w.begin, (__bf16*)a.out[w.t] + w.begin, n, c, finite);
+  else clip_piece((const float*)a.in[w.t] + w.begin, (float*)a.out[w.t] + w.begin, n, c, finite);
+}
+
+struct Place { float *p, *m, *v; const void* g; void* w; };
+
+// one value (one copy of the formula for whole vectors and tails: the same bits whatever the piece)
+__device__ __forceinline__ void step_value(const StepArgs& a, float decay, float g, float& p, float& m, float& v) {
+  m = fmaf(a.beta1, m, a.one_beta1 * g);
+  v = fmaf(a.beta2, v, a.one_beta2 * (g * g));
+  p -= fmaf(decay, p, a.rate * (m / fmaf(sqrtf(v), a.root, a.eps)));
+}
+
+template <typename G, typename W, bool COPY>
+__device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, uint32_t n, float c, float decay) {
+  const G* gs = (const G*)t.g;
+  W* ws = (W*)t.w;
+  const uint32_t fours = n / 4;
+  for (uint32_t i = threadIdx.x; i < fours; i += 256) {
+    const size_t at = (size_t)i * 4;
+    const Four<G> g = *(const Four<G>*)(gs + at);
+    Four<float> m = *(const Four<float>*)(t.m + at), v = *(const Four<float>*)(t.v + at), p = *(const Four<float>*)(t.p + at);
+    Four<W> w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float pj = p[j], mj = m[j], vj = v[j];
+      step_value(a, decay, c * (float)g[j], pj, mj, vj);
+      p[j] = pj;
+      m[j] = mj;
+      v[j] = vj;
+      w[j] = (W)pj;
+    }
+    *(Four<float>*)(t.m + at) = m;
+    *(Four<float>*)(t.v + at) = v;
+    *(Four<float>*)(t.p + at) = p;
+    if (COPY) *(Four<W>*)(ws + at) = w;
+  }
+  const uint32_t i = fours * 4 + threadIdx.x;
+  if (i < n) {
+    float p = t.p[i], m = t.m[i], v = t.v[i];
+    step_value(a, decay, c * (float)gs[i], p, m, v);
+    t.p[i] = p;
+    t.m[i] = m;
+    t.v[i] = v;
+    if (COPY) ws[i] = (W)p;
+  }
+}
+
+template <typename G>
+__device__ __forceinline__ void step_piece(const StepArgs& a, Place t, int64_t begin, bool half_w, uint32_t n, float c, float decay) {
+  t.p += begin;
+  t.m += begin;
+  t.v += begin;
+  t.g = (const G*)t.g + begin;
+  if (!t.w) return step_piece<G, float, false>(a, t, n, c, decay);
+  if (half_w) {
+    t.w = (__bf16*)t.w + begin;
+    return step_piece<G, __bf16, true>(a, t, n, c, decay);
+  }
+  t.w = (float*)t.w + begin;
+  step_piece<G, float, true>(a, t, n, c, decay);
 }
 
 __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
@@ -120,22 +224,11 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
     c = a.norm[1];
   }
   const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
-  const int64_t n = a.n[w.t] & kCount, end = min(n, w.begin + ((int64_t)1 << a.shift));
-  const bool half_g = a.n[w.t] & kHalf, half_w = a.n[w.t] & kHalfW;
-  for (int64_t i = w.begin + threadIdx.x; i < end; i += 256) {
-    const float g = c * (half_g ? (float)((const __bf16*)a.g[w.t])[i] : ((const float*)a.g[w.t])[i]);
-    const float m = a.beta1 * a.m[w.t][i] + a.one_beta1 * g;
-    const float v = a.beta2 * a.v[w.t][i] + a.one_beta2 * (g * g);
-    float p = a.p[w.t][i];
-    p -= a.rate * (m / (sqrtf(v) * a.root + a.eps)) + a.decay[w.t] * p;
-    a.m[w.t][i] = m;
-    a.v[w.t][i] = v;
-    a.p[w.t][i] = p;
-    if (a.w[w.t]) {
-      if (half_w) ((__bf16*)a.w[w.t])[i] = (__bf16)p;
-      else ((float*)a.w[w.t])[i] = p;
-    }
-  }
+  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)1 << a.shift);
+  const bool half_w = a.n[w.t] & kHalfW;
+  const Place t = {a.p[w.t], a.m[w.t], a.v[w.t], a.g[w.t], a.w[w.t]};
+  if (a.n[w.t] & kHalf) step_piece<__bf16>(a, t, w.begin, half_w, n, c, a.decay[w.t]);
+  else step_piece<float>(a, t, w.begin, half_w, n, c, a.decay[w.t]);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -167,10 +260,11 @@ static int check_list(const longer_tensor* t, int count, int64_t* values) {
   return 0;
 }
 
-// piece size: at most 4096 pieces beside one more for each tensor
+// Values of a piece, as a power of two: about 4096 pieces in all (16 workgroups for each compute unit), at least 2048 values, so
+// that a short list has as many workgroups as it can feed, at most 2^20.
 static int piece_shift(int64_t values) {
-  int s = 12;
-  while ((values >> s) > 4096) ++s;
+  int s = 11;
+  while (s < 20 && (values >> s) > 4096) ++s;
   return s;
 }
 static uint32_t pieces(int64_t n, int shift) { return (uint32_t)((n + ((int64_t)1 << shift) - 1) >> shift); }
