@@ -162,7 +162,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
     load_row<T>(x_ahead, p.x, ahead, ok_ahead, c);
     const Walk ahead2 = ahead.next(p, step);
     float y[NV][V];
-    if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : ok) {       // (a row of several waves has its workgroup to itself)
+    // (no row of the wave counts: nothing to do; rows of several waves meet at barriers, which their whole workgroup has to reach)
+    if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : RPB > 1 || ok) {
       float s[1] = {0.f};
 #pragma unroll
       for (int i = 0; i < NV; ++i)
@@ -341,41 +342,103 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
 // ------------------------------------------------------------------------------------ host
 struct Shape { int lpr, nv, mode, v; };
 
-// lanes and pieces of a row for pieces of `v` values, at most `most` of them a lane
-inline Shape shape(int d, int v, int most) {
+// lanes and pieces of a row for pieces of `v` values: as few lanes as hold it with `wave` pieces each where a wave can, with `more`
+// each beyond
+inline Shape shape(int d, int v, int wave, int more) {
   if (d < v) return {8, 1, PIECES, 1};
   const int pieces = (d + v - 1) / v;
   Shape s = {1, 1, 0, v};
   while (s.lpr < pieces && s.lpr < 64) s.lpr *= 2;
-  if (pieces > 64 * most) s.lpr = pieces > 256 * most ? 1024 : 256;
+  while (pieces > s.lpr * (s.lpr > 64 ? more : wave) && s.lpr < 1024) s.lpr *= 2;
   s.nv = (pieces + s.lpr - 1) / s.lpr;
   s.mode = d % v ? VALUES : pieces == s.lpr * s.nv ? FULL : PIECES;
   return s;
 }
 
-// The backward launch of one pair of types; the workgroups that it takes (at most `most`), each of which leaves its column sums.
-template <int LPR> inline unsigned grad_groups(const Params& p, unsigned most) {
-  const unsigned turns = ((unsigned)p.rows + 1024 / LPR - 1) / (1024 / LPR);
-  return turns < most ? turns : most;
+// Workgroups of a launch: as many as the card holds at once, each with its share of the turns (a few more than it holds would take
+// a second round for themselves), or a turn each.
+template <typename K>
+inline unsigned resident(K kernel, int threads) {
+  int n = 0;
+  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != hipSuccess || n < 1) n = 1;
+  return 256u * n;
 }
 
-template <typename T, typename U, int V, int LPR, int NV>
-inline unsigned launch_grad(Params& p, int mode, unsigned most, float* only, hipStream_t st) {
-  const unsigned grid = grad_groups<LPR>(p, most);
-  const int64_t step = (int64_t)grid * (1024 / LPR);
+inline void set_step(Params& p, unsigned grid, int rows_per_turn) {
+  const int64_t step = (int64_t)grid * rows_per_turn;
   p.step_u = (int)(step / p.L);
   p.step_l = (int)(step % p.L);
-  if (grid == 1) p.part = only;
-  if (mode == FULL) grad_kernel<T, U, V, LPR, NV, FULL><<<grid, 1024, 0, st>>>(p);
-  else if (mode == PIECES) grad_kernel<T, U, V, LPR, NV, PIECES><<<grid, 1024, 0, st>>>(p);
-  else if constexpr (V > 1) grad_kernel<T, U, V, LPR, NV, VALUES><<<grid, 1024, 0, st>>>(p);
-  return grid;
 }
 
-// (8 values a lane, beside their column sums and the next turn's; twice as many where even a workgroup's lanes are too few)
+template <typename T, int V, int LPR, int NV, int MODE>
+inline void launch_norm(Params& p, hipStream_t st) {
+  constexpr int THREADS = LPR > 256 ? LPR : 256, RPB = THREADS / LPR;
+  static const unsigned most = resident(norm_kernel<T, V, LPR, NV, MODE, THREADS>, THREADS);
+  const unsigned turns = ((unsigned)p.rows + RPB - 1) / RPB, grid = turns < most ? turns : most;
+  set_step(p, grid, RPB);
+  norm_kernel<T, V, LPR, NV, MODE, THREADS><<<grid, THREADS, 0, st>>>(p);
+}
+template <typename T, int V, int LPR, int NV>
+inline void launch_norm(Params& p, int mode, hipStream_t st) {
+  if (mode == FULL) launch_norm<T, V, LPR, NV, FULL>(p, st);
+  else if (mode == PIECES) launch_norm<T, V, LPR, NV, PIECES>(p, st);
+  else if constexpr (V > 1) launch_norm<T, V, LPR, NV, VALUES>(p, st);
+}
+
+// (four pieces a lane in one wave before a row takes several, which meet in LDS)
+template <typename T, int V>
+inline void norm(Params& p, hipStream_t st) {
+  const Shape s = shape(p.d, V, 4, 4);
+  if (s.v == 1) return launch_norm<T, 1, 8, 1>(p, s.mode, st);
+  switch (s.lpr * 8 + s.nv) {
+    case 1 * 8 + 1: return launch_norm<T, V, 1, 1>(p, s.mode, st);
+    case 2 * 8 + 1: return launch_norm<T, V, 2, 1>(p, s.mode, st);
+    case 4 * 8 + 1: return launch_norm<T, V, 4, 1>(p, s.mode, st);
+    case 8 * 8 + 1: return launch_norm<T, V, 8, 1>(p, s.mode, st);
+    case 16 * 8 + 1: return launch_norm<T, V, 16, 1>(p, s.mode, st);
+    case 32 * 8 + 1: return launch_norm<T, V, 32, 1>(p, s.mode, st);
+    case 64 * 8 + 1: return launch_norm<T, V, 64, 1>(p, s.mode, st);
+    case 64 * 8 + 2: return launch_norm<T, V, 64, 2>(p, s.mode, st);
+    case 64 * 8 + 3: return launch_norm<T, V, 64, 3>(p, s.mode, st);
+    case 64 * 8 + 4: return launch_norm<T, V, 64, 4>(p, s.mode, st);
+    case 128 * 8 + 3: return launch_norm<T, V, 128, 3>(p, s.mode, st);
+    case 128 * 8 + 4: return launch_norm<T, V, 128, 4>(p, s.mode, st);
+    case 256 * 8 + 3: return launch_norm<T, V, 256, 3>(p, s.mode, st);
+    case 256 * 8 + 4: return launch_norm<T, V, 256, 4>(p, s.mode, st);
+    case 512 * 8 + 3: return launch_norm<T, V, 512, 3>(p, s.mode, st);
+    case 512 * 8 + 4: return launch_norm<T, V, 512, 4>(p, s.mode, st);
+  }
+  if constexpr (V == 4) {
+    if (s.nv == 3) launch_norm<T, V, 1024, 3>(p, s.mode, st);
+    else launch_norm<T, V, 1024, 4>(p, s.mode, st);
+  }
+}
+
+// The backward launch; the workgroups that it takes (at most `most`), each of which leaves its column sums.
+template <typename T, typename U, int V, int LPR, int NV, int MODE>
+inline unsigned launch_grad(Params& p, unsigned most, float* only, hipStream_t st) {
+  static const unsigned held = resident(grad_kernel<T, U, V, LPR, NV, MODE>, 1024);
+  const unsigned turns = ((unsigned)p.rows + 1024 / LPR - 1) / (1024 / LPR);
+  unsigned grid = turns < held ? turns : held;
+  if (grid > most) grid = most;
+  set_step(p, grid, 1024 / LPR);
+  if (grid == 1) p.part = only;
+  grad_kernel<T, U, V, LPR, NV, MODE><<<grid, 1024, 0, st>>>(p);
+  return grid;
+}
+template <typename T, typename U, int V, int LPR, int NV>
+inline unsigned launch_grad(Params& p, int mode, unsigned most, float* only, hipStream_t st) {
+  if (mode == FULL) return launch_grad<T, U, V, LPR, NV, FULL>(p, most, only, st);
+  if (mode == PIECES) return launch_grad<T, U, V, LPR, NV, PIECES>(p, most, only, st);
+  if constexpr (V > 1) return launch_grad<T, U, V, LPR, NV, VALUES>(p, most, only, st);
+  return 0;
+}
+
+// (8 values a lane, beside their column sums and the next turn's; more only where even a workgroup's lanes are too few)
 template <typename T, typename U, int V>
 inline unsigned grad(Params& p, unsigned most, float* only, hipStream_t st) {
-  const Shape s = shape(p.d, V, 8 / V);
+  constexpr int N = 8 / V;
+  const Shape s = shape(p.d, V, N, N);
   if (s.v == 1) return launch_grad<T, U, 1, 8, 1>(p, s.mode, most, only, st);
   switch (s.lpr * 8 + s.nv) {
     case 1 * 8 + 1: return launch_grad<T, U, V, 1, 1>(p, s.mode, most, only, st);
@@ -385,22 +448,22 @@ inline unsigned grad(Params& p, unsigned most, float* only, hipStream_t st) {
     case 16 * 8 + 1: return launch_grad<T, U, V, 16, 1>(p, s.mode, most, only, st);
     case 32 * 8 + 1: return launch_grad<T, U, V, 32, 1>(p, s.mode, most, only, st);
     case 64 * 8 + 1: return launch_grad<T, U, V, 64, 1>(p, s.mode, most, only, st);
-    case 256 * 8 + 1: return launch_grad<T, U, V, 256, 1>(p, s.mode, most, only, st);
-    case 1024 * 8 + 1: return launch_grad<T, U, V, 1024, 1>(p, s.mode, most, only, st);
-    case 1024 * 8 + 2: return launch_grad<T, U, V, 1024, 2>(p, s.mode, most, only, st);
+    case 128 * 8 + N: return launch_grad<T, U, V, 128, N>(p, s.mode, most, only, st);
+    case 256 * 8 + N: return launch_grad<T, U, V, 256, N>(p, s.mode, most, only, st);
+    case 512 * 8 + N: return launch_grad<T, U, V, 512, N>(p, s.mode, most, only, st);
+    case 1024 * 8 + N: return launch_grad<T, U, V, 1024, N>(p, s.mode, most, only, st);
   }
   if constexpr (V == 4) {
-    switch (s.lpr * 8 + s.nv) {
-      case 64 * 8 + 2: return launch_grad<T, U, V, 64, 2>(p, s.mode, most, only, st);
-      case 256 * 8 + 2: return launch_grad<T, U, V, 256, 2>(p, s.mode, most, only, st);
-      case 1024 * 8 + 3: return launch_grad<T, U, V, 1024, 3>(p, s.mode, most, only, st);
-      case 1024 * 8 + 4: return launch_grad<T, U, V, 1024, 4>(p, s.mode, most, only, st);
-    }
+    if (s.lpr == 64) return launch_grad<T, U, V, 64, 2>(p, s.mode, most, only, st);
+    return s.nv == 3 ? launch_grad<T, U, V, 1024, 3>(p, s.mode, most, only, st) : launch_grad<T, U, V, 1024, 4>(p, s.mode, most, only, st);
+  } else {
+    return launch_grad<T, U, V, 1024, 2>(p, s.mode, most, only, st);
   }
-  return 0;                          // (no width comes here)
 }
 
-// inst_norm_grad_*.hip
+// inst_norm_*.hip
+void norm_f32(Params& p, hipStream_t st);
+void norm_bf16(Params& p, hipStream_t st);
 unsigned grad_f32(Params& p, unsigned most, float* only, hipStream_t st);
 unsigned grad_bf16_f32(Params& p, unsigned most, float* only, hipStream_t st);
 unsigned grad_bf16(Params& p, unsigned most, float* only, hipStream_t st);

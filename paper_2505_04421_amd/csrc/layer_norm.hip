@@ -26,7 +26,7 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, int slice
 }
 
 // ------------------------------------------------------------------------------------ host
-constexpr int kGradGroups = 512;                    // workgroups of a backward launch: two for each compute unit
+constexpr int kGradGroups = 512;                    // most workgroups of a backward launch: two for each compute unit
 
 static int check_sizes(int B, int L, int d) {
   if (B <= 0 || L <= 0 || (int64_t)B * L >= ((int64_t)1 << 31) - (1 << 21)) return api_error(LONGER_ERR_ARG, "B=%d L=%d: at least 1 each, B * L below 2^31 - 2^21", B, L);
@@ -81,44 +81,6 @@ static int launched(const char* what) {
   return hipGetLastError() == hipSuccess ? 0 : api_error(LONGER_ERR_HIP, "%s launch failed", what);
 }
 
-template <typename T, int V, int LPR, int NV>
-static void launch_norm(Params& p, int mode, hipStream_t st) {
-  constexpr int THREADS = LPR > 256 ? 1024 : 256, RPB = THREADS / LPR;
-  // eight turns a workgroup, so that loading the vectors and the first rows is a small part; fewer where that would leave
-  // compute units idle
-  const int64_t turns = ((int64_t)p.rows + RPB - 1) / RPB;
-  const unsigned grid = (unsigned)std::max((turns + 7) / 8, std::min<int64_t>(turns, 2048 * 256 / THREADS));
-  const int64_t step = (int64_t)grid * RPB;
-  p.step_u = (int)(step / p.L);
-  p.step_l = (int)(step % p.L);
-  if (mode == FULL) norm_kernel<T, V, LPR, NV, FULL, THREADS><<<grid, THREADS, 0, st>>>(p);
-  else if (mode == PIECES) norm_kernel<T, V, LPR, NV, PIECES, THREADS><<<grid, THREADS, 0, st>>>(p);
-  else if constexpr (V > 1) norm_kernel<T, V, LPR, NV, VALUES, THREADS><<<grid, THREADS, 0, st>>>(p);
-}
-
-template <typename T, int V>
-static void norm(Params& p, hipStream_t st) {
-  const Shape s = shape(p.d, V, 4);
-  if (s.v == 1) return launch_norm<T, 1, 8, 1>(p, s.mode, st);
-  switch (s.lpr * 8 + s.nv) {
-    case 1 * 8 + 1: return launch_norm<T, V, 1, 1>(p, s.mode, st);
-    case 2 * 8 + 1: return launch_norm<T, V, 2, 1>(p, s.mode, st);
-    case 4 * 8 + 1: return launch_norm<T, V, 4, 1>(p, s.mode, st);
-    case 8 * 8 + 1: return launch_norm<T, V, 8, 1>(p, s.mode, st);
-    case 16 * 8 + 1: return launch_norm<T, V, 16, 1>(p, s.mode, st);
-    case 32 * 8 + 1: return launch_norm<T, V, 32, 1>(p, s.mode, st);
-    case 64 * 8 + 1: return launch_norm<T, V, 64, 1>(p, s.mode, st);
-    case 64 * 8 + 2: return launch_norm<T, V, 64, 2>(p, s.mode, st);
-    case 64 * 8 + 3: return launch_norm<T, V, 64, 3>(p, s.mode, st);
-    case 64 * 8 + 4: return launch_norm<T, V, 64, 4>(p, s.mode, st);
-    case 256 * 8 + 2: return launch_norm<T, V, 256, 2>(p, s.mode, st);
-    case 256 * 8 + 3: return launch_norm<T, V, 256, 3>(p, s.mode, st);
-    case 256 * 8 + 4: return launch_norm<T, V, 256, 4>(p, s.mode, st);
-    case 1024 * 8 + 2: return launch_norm<T, V, 1024, 2>(p, s.mode, st);
-    default: if constexpr (V < 8) { return s.nv == 3 ? launch_norm<T, V, 1024, 3>(p, s.mode, st) : launch_norm<T, V, 1024, 4>(p, s.mode, st); }
-  }
-}
-
 }  // namespace ln
 }  // namespace longer
 
@@ -139,8 +101,8 @@ int longer_layer_norm(const longer_rows* x, const void* ln_g, const void* ln_b, 
   if (!rc && ((uintptr_t)lens & 3)) rc = api_error(LONGER_ERR_ARG, "lens is not aligned");
   if (rc) return rc;
   ln::Params p = {ln::rows_of(x, B, L), {}, ln::rows_of(y, B, L), ln_g, ln_b, lens, B * L, L, d, 0, 0, eps, 1.f / d, nullptr};
-  if (x->dtype == LONGER_F32) ln::norm<float, 4>(p, (hipStream_t)stream);
-  else ln::norm<__bf16, 8>(p, (hipStream_t)stream);
+  if (x->dtype == LONGER_F32) ln::norm_f32(p, (hipStream_t)stream);
+  else ln::norm_bf16(p, (hipStream_t)stream);
   return ln::launched("layer norm");
 }
 

@@ -14,12 +14,12 @@ namespace upd {
 // A launch takes its tensors in its arguments (under 4 KB of them), so a call needs no table in device memory and
 // keeps none.  (Arrays of 4 and 8 byte elements only: beside a byte array the compiler takes the others by scalar loads from a base
 // that is off a multiple of 4, and scalar loads drop the two low bits of each part of their address.)  Each tensor is cut into
-// pieces of 2^shift values, numbered over the launch's list; a workgroup takes one.
+// pieces, numbered over the launch's list; a workgroup takes one.
 struct Piece { int t; int64_t begin; };
 
 // first[i] = number of tensor i's first piece, ascending: the last i with first[i] <= b (an empty tensor is not in the list)
 template <int N>
-__device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int count, uint32_t b, int shift) {
+__device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int count, uint32_t b, int64_t values) {
   const int lane = threadIdx.x & 63;
   int n = 0;
 #pragma unroll
@@ -27,7 +27,7 @@ __device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int coun
     const int i = k + lane;
     n += __popcll(__ballot(i < count && first[i < N ? i : 0] <= b));
   }
-  return {n - 1, (int64_t)(b - first[n - 1]) << shift};
+  return {n - 1, (b - first[n - 1]) * values};
 }
 
 // 16 bytes of a tensor, aligned to its element only
@@ -37,6 +37,13 @@ template <typename T> struct Four_ { typedef T type __attribute__((ext_vector_ty
 template <typename T> using Four = typename Four_<T>::type;
 
 constexpr int kNormList = 192, kClipList = 128, kStepList = 64;
+// Values of a piece.  An update has five streams to keep going and a clip two: with small pieces, in the list's order, what is under
+// way at one time is one stretch of each, in few memory pages (128 million parameters, an update in pieces of 1024 / 2048 / 4096 /
+// 8192 / 32768 values by 256 threads: 725 / 765 / 808 / 830 / 890 us; four values a thread in workgroups of 256 / 512 / 1024: 725 /
+// 720 / 711; 257 million values clipped in pieces of 1024 / 2048 / 4096 / 8192 / 65536: 364 / 362 / 390 / 420 / 420).  The norm's
+// pieces, each of which leaves a sum to be joined, are as large as keeps every compute unit busy (at 2048 in all instead of 4096:
+// 180 us for 171).
+constexpr int kStepPiece = 4096, kClipPiece = 2048;
 constexpr int64_t kHalf = (int64_t)1 << 62;         // in a tensor's size: its values (an update's gradients) are bf16
 constexpr int64_t kHalfW = (int64_t)1 << 61;        // and the update's copy w is
 constexpr int64_t kCount = kHalfW - 1;
@@ -45,15 +52,16 @@ struct NormArgs {
   const void* data[kNormList];
   int64_t n[kNormList];
   uint32_t first[kNormList];
-  int count, shift;
+  int count;
+  int64_t piece;
 };
 struct ClipArgs {
   const void* in[kClipList];
   void* out[kClipList];
   int64_t n[kClipList];
   uint32_t first[kClipList];
-  int count, shift;
   const float* norm;
+  int count;
 };
 struct StepArgs {
   float *p[kStepList], *m[kStepList], *v[kStepList];
@@ -62,18 +70,20 @@ struct StepArgs {
   int64_t n[kStepList];
   uint32_t first[kStepList];
   float decay[kStepList];                            // lr * decay
-  int count, shift;
   const float* norm;
+  int count;
   float beta1, one_beta1, beta2, one_beta2, rate, root, eps;   // rate = lr / (1 - beta1^t), root = 1 / sqrt(1 - beta2^t)
 };
 
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v, double* lds) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
   v = 0.;
-  for (unsigned w = 0; w < blockDim.x / 64; ++w) v += lds[w];
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) v += lds[w];
   return v;
 }
 
@@ -106,20 +116,22 @@ __device__ __forceinline__ double squares(const T* g, uint32_t n) {
   return s[0];
 }
 
+// (from the list's end to its start: what is read last is what a pass behind this one reads first, and may still be near)
 __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
   __shared__ double lds[4];
-  const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
-  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)1 << a.shift);
+  const uint32_t b = gridDim.x - 1 - blockIdx.x;
+  const Piece w = find_piece(a.first, a.count, b, a.piece);
+  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, a.piece);
   double s = a.n[w.t] & kHalf ? squares((const __bf16*)a.data[w.t] + w.begin, n) : squares((const float*)a.data[w.t] + w.begin, n);
-  s = block_sum(s, lds);
-  if (threadIdx.x == 0) part[blockIdx.x] = s;
+  s = block_sum<256>(s, lds);
+  if (threadIdx.x == 0) part[b] = s;
 }
 
 __global__ __launch_bounds__(1024) void norm_join_kernel(const double* part, uint32_t n, float max_norm, float* norm) {
   __shared__ double lds[16];
   double s = 0.;
   for (uint32_t i = threadIdx.x; i < n; i += 1024) s += part[i];
-  s = block_sum(s, lds);
+  s = block_sum<1024>(s, lds);
   if (threadIdx.x) return;
   const float v = (float)sqrt(s);
   norm[0] = v;
@@ -128,32 +140,28 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double* part, uin
 
 template <typename T>
 __device__ __forceinline__ void clip_piece(const T* in, T* out, uint32_t n, float c, bool finite) {
-  constexpr int V = 16 / sizeof(T), U = 4;
-  const uint32_t lines = n / V;
-  auto put = [&](uint32_t i, Line<T> x) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = (T)(finite ? (float)x[j] * c : 0.f);
-    *(Line<T>*)(out + (size_t)i * V) = x;
-  };
-  uint32_t i = threadIdx.x;
-  for (; i + 256 * (U - 1) < lines; i += 256 * U) {
+  constexpr uint32_t V = 16 / sizeof(T), U = kClipPiece / 256 / V;
+  if (n == kClipPiece) {
     Line<T> x[U];
 #pragma unroll
-    for (int k = 0; k < U; ++k) x[k] = *(const Line<T>*)(in + (size_t)(i + 256 * k) * V);
+    for (uint32_t k = 0; k < U; ++k) x[k] = *(const Line<T>*)(in + (threadIdx.x + 256 * k) * V);
 #pragma unroll
-    for (int k = 0; k < U; ++k) put(i + 256 * k, x[k]);
+    for (uint32_t k = 0; k < U; ++k) {
+#pragma unroll
+      for (uint32_t j = 0; j < V; ++j) x[k][j] = (T)(finite ? (float)x[k][j] * c : 0.f);
+      __builtin_nontemporal_store(x[k], (Line<T>*)(out + (threadIdx.x + 256 * k) * V));
+    }
+  } else {
+    for (uint32_t i = threadIdx.x; i < n; i += 256) out[i] = (T)(finite ? (float)in[i] * c : 0.f);
   }
-  for (; i < lines; i += 256) put(i, *(const Line<T>*)(in + (size_t)i * V));
-  i = lines * V + threadIdx.x;
-  if (i < n) out[i] = (T)(finite ? (float)in[i] * c : 0.f);
 }
 
 __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
-  const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
+  const Piece w = find_piece(a.first, a.count, blockIdx.x, kClipPiece);
   const float c = a.norm[1];
   const bool finite = isfinite(a.norm[0]);
   if (c == 1.f && a.in[w.t] == a.out[w.t]) return;
-  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)1 << a.shift);
+  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)kClipPiece);
   if (a.n[w.t] & kHalf) clip_piece((const __bf16*)a.in[w.t] + w.begin, (__bf16*)a.out[w.t] + w.begin, n, c, finite);
   else clip_piece((const float*)a.in[w.t] + w.begin, (float*)a.out[w.t] + w.begin, n, c, finite);
 }
@@ -167,15 +175,18 @@ __device__ __forceinline__ void step_value(const StepArgs& a, float decay, float
   p -= fmaf(decay, p, a.rate * (m / fmaf(sqrtf(v), a.root, a.eps)));
 }
 
+// Four values a lane.  Moments, parameters and their copy pass by once: nontemporal, they leave the last cache to the gradients that
+// the norm has just read, and to the next norm's (128 million parameters: norm 87 us for 150, both together 830 us for 915).
 template <typename G, typename W, bool COPY>
 __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, uint32_t n, float c, float decay) {
   const G* gs = (const G*)t.g;
   W* ws = (W*)t.w;
-  const uint32_t fours = n / 4;
-  for (uint32_t i = threadIdx.x; i < fours; i += 256) {
-    const size_t at = (size_t)i * 4;
-    const Four<G> g = *(const Four<G>*)(gs + at);
-    Four<float> m = *(const Four<float>*)(t.m + at), v = *(const Four<float>*)(t.v + at), p = *(const Four<float>*)(t.p + at);
+  const uint32_t i = threadIdx.x * 4;
+  if (i + 4 <= n) {
+    const Four<G> g = *(const Four<G>*)(gs + i);
+    Four<float> m = __builtin_nontemporal_load((const Four<float>*)(t.m + i));
+    Four<float> v = __builtin_nontemporal_load((const Four<float>*)(t.v + i));
+    Four<float> p = __builtin_nontemporal_load((const Four<float>*)(t.p + i));
     Four<W> w;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -186,19 +197,19 @@ __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, ui
       v[j] = vj;
       w[j] = (W)pj;
     }
-    *(Four<float>*)(t.m + at) = m;
-    *(Four<float>*)(t.v + at) = v;
-    *(Four<float>*)(t.p + at) = p;
-    if (COPY) *(Four<W>*)(ws + at) = w;
-  }
-  const uint32_t i = fours * 4 + threadIdx.x;
-  if (i < n) {
-    float p = t.p[i], m = t.m[i], v = t.v[i];
-    step_value(a, decay, c * (float)gs[i], p, m, v);
-    t.p[i] = p;
-    t.m[i] = m;
-    t.v[i] = v;
-    if (COPY) ws[i] = (W)p;
+    __builtin_nontemporal_store(m, (Four<float>*)(t.m + i));
+    __builtin_nontemporal_store(v, (Four<float>*)(t.v + i));
+    __builtin_nontemporal_store(p, (Four<float>*)(t.p + i));
+    if (COPY) __builtin_nontemporal_store(w, (Four<W>*)(ws + i));
+  } else {
+    for (uint32_t k = i; k < n; ++k) {
+      float p = t.p[k], m = t.m[k], v = t.v[k];
+      step_value(a, decay, c * (float)gs[k], p, m, v);
+      t.p[k] = p;
+      t.m[k] = m;
+      t.v[k] = v;
+      if (COPY) ws[k] = (W)p;
+    }
   }
 }
 
@@ -217,14 +228,14 @@ __device__ __forceinline__ void step_piece(const StepArgs& a, Place t, int64_t b
   step_piece<G, float, true>(a, t, n, c, decay);
 }
 
-__global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
+__global__ __launch_bounds__(kStepPiece / 4) void step_kernel(StepArgs a) {
   float c = 1.f;
   if (a.norm) {
     if (!isfinite(a.norm[0])) return;
     c = a.norm[1];
   }
-  const Piece w = find_piece(a.first, a.count, blockIdx.x, a.shift);
-  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)1 << a.shift);
+  const Piece w = find_piece(a.first, a.count, blockIdx.x, kStepPiece);
+  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)kStepPiece);
   const bool half_w = a.n[w.t] & kHalfW;
   const Place t = {a.p[w.t], a.m[w.t], a.v[w.t], a.g[w.t], a.w[w.t]};
   if (a.n[w.t] & kHalf) step_piece<__bf16>(a, t, w.begin, half_w, n, c, a.decay[w.t]);
@@ -238,7 +249,7 @@ static int launched(const char* what) {
   return hipGetLastError() == hipSuccess ? 0 : api_error(LONGER_ERR_HIP, "%s launch failed", what);
 }
 
-constexpr int64_t kMostValues = (int64_t)1 << 44;    // of a list: offsets in bytes, and the piece numbers, stay far inside their types
+constexpr int64_t kMostValues = (int64_t)1 << 40;    // of a list: more than a GPU's memory holds
 
 static int check_tensor(const void* p, int64_t n, int dtype, int i, const char* name) {
   if (n < 0 || n > kMostValues) return api_error(LONGER_ERR_ARG, "tensor %d: n=%lld out of range", i, (long long)n);
@@ -254,27 +265,51 @@ static int check_list(const longer_tensor* t, int count, int64_t* values) {
   for (int i = 0; i < count; ++i) {
     if (int rc = check_tensor(t[i].data, t[i].n, t[i].dtype, i, "data")) return rc;
     sum += t[i].n;
-    if (sum > kMostValues) return api_error(LONGER_ERR_ARG, "a list of more than 2^44 values");
+    if (sum > kMostValues) return api_error(LONGER_ERR_ARG, "a list of more than 2^40 values");
   }
   *values = sum;
   return 0;
 }
 
-// Values of a piece, as a power of two: about 4096 pieces in all (16 workgroups for each compute unit), at least 2048 values, so
-// that a short list has as many workgroups as it can feed, at most 2^20.
-static int piece_shift(int64_t values) {
-  int s = 11;
-  while (s < 20 && (values >> s) > 4096) ++s;
-  return s;
+// The norm's pieces: about 4096 in all (sixteen workgroups for each compute unit), of at least 2048 values, so that a short list has as
+// many workgroups as it can feed.
+static int64_t norm_piece(int64_t values) {
+  int64_t piece = 2048;
+  while (piece * 4096 < values) piece *= 2;
+  return piece;
 }
-static uint32_t pieces(int64_t n, int shift) { return (uint32_t)((n + ((int64_t)1 << shift) - 1) >> shift); }
+static uint32_t pieces(int64_t n, int64_t piece) { return (uint32_t)((n + piece - 1) / piece); }
 
-static uint32_t list_pieces(const longer_tensor* t, int count, int shift) {
+static uint32_t list_pieces(const longer_tensor* t, int count, int64_t piece) {
   uint32_t k = 0;
-  for (int i = 0; i < count; ++i) k += pieces(t[i].n, shift);
+  for (int i = 0; i < count; ++i) k += pieces(t[i].n, piece);
   return k;
 }
 static size_t norm_bytes(uint32_t n) { return ((size_t)(n ? n : 1) * 8 + 255) & ~(size_t)255; }
+
+// Cuts a list into launches: `add(j, i, begin, n, first)` puts values [begin, begin + n) of tensor i in place j of a launch, their
+// pieces numbered from `first`; `go(entries, pieces)` launches.  A launch ends with its list full or at 2^23 workgroups (the grid
+// counts threads in 32 bits); a tensor may go on in the next.
+template <typename Size, typename Add, typename Go>
+static void launches(int count, int most, int64_t piece, Size size, Add add, Go go) {
+  constexpr uint32_t kMostPieces = 1u << 23;
+  int64_t begin = 0;
+  for (int i = 0; i < count;) {
+    int entries = 0;
+    uint32_t k = 0;
+    while (i < count && entries < most && k < kMostPieces) {
+      const int64_t left = size(i) - begin;
+      const int64_t n = left < (kMostPieces - k) * piece ? left : (kMostPieces - k) * piece;
+      if (n) {
+        add(entries++, i, begin, n, k);
+        k += pieces(n, piece);
+      }
+      begin += n;
+      if (n == left) { ++i; begin = 0; }
+    }
+    if (k) go(entries, k);
+  }
+}
 
 }  // namespace upd
 }  // namespace longer
@@ -286,7 +321,7 @@ extern "C" {
 size_t longer_grad_norm_workspace_bytes(const longer_tensor* grads, int count) {
   int64_t values;
   if (upd::check_list(grads, count, &values)) return 0;
-  return upd::norm_bytes(upd::list_pieces(grads, count, upd::piece_shift(values)));
+  return upd::norm_bytes(upd::list_pieces(grads, count, upd::norm_piece(values)));
 }
 
 int longer_grad_norm(const longer_tensor* grads, int count, float max_norm, float* norm_out,
@@ -297,27 +332,25 @@ int longer_grad_norm(const longer_tensor* grads, int count, float max_norm, floa
   if ((uintptr_t)norm_out & 3) return api_error(LONGER_ERR_ARG, "norm_out is not aligned");
   if ((uintptr_t)ws & 255) return api_error(LONGER_ERR_ARG, "ws must be 256-byte aligned");
   if (!(max_norm > 0.f)) return api_error(LONGER_ERR_ARG, "max_norm must be positive");
-  const int shift = upd::piece_shift(values);
-  const uint32_t all = upd::list_pieces(grads, count, shift);
+  const int64_t piece = upd::norm_piece(values);
+  const uint32_t all = upd::list_pieces(grads, count, piece);
   if (ws_bytes < upd::norm_bytes(all)) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, upd::norm_bytes(all));
   hipStream_t st = (hipStream_t)stream;
   uint32_t done = 0;
-  for (int i = 0; i < count;) {
-    upd::NormArgs a;
-    a.count = 0;
-    a.shift = shift;
-    uint32_t k = 0;
-    for (; i < count && a.count < upd::kNormList; ++i) {
-      if (!grads[i].n) continue;
-      a.data[a.count] = grads[i].data;
-      a.n[a.count] = grads[i].n | (grads[i].dtype == LONGER_BF16 ? upd::kHalf : 0);
-      a.first[a.count++] = k;
-      k += upd::pieces(grads[i].n, shift);
-    }
-    if (!k) break;
-    upd::norm_kernel<<<k, 256, 0, st>>>(a, (double*)ws + done);
-    done += k;
-  }
+  upd::NormArgs a;
+  a.piece = piece;
+  upd::launches(count, upd::kNormList, piece, [&](int i) { return grads[i].n; },
+                [&](int j, int i, int64_t begin, int64_t n, uint32_t first) {
+                  const bool half = grads[i].dtype == LONGER_BF16;
+                  a.data[j] = (const char*)grads[i].data + begin * (half ? 2 : 4);
+                  a.n[j] = n | (half ? upd::kHalf : 0);
+                  a.first[j] = first;
+                },
+                [&](int entries, uint32_t k) {
+                  a.count = entries;
+                  upd::norm_kernel<<<k, 256, 0, st>>>(a, (double*)ws + done);
+                  done += k;
+                });
   upd::norm_join_kernel<<<1, 1024, 0, st>>>((const double*)ws, done, max_norm, norm_out);
   return upd::launched("gradient norm");
 }
@@ -331,24 +364,21 @@ int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, 
       if (out[i].n != grads[i].n || out[i].dtype != grads[i].dtype) return api_error(LONGER_ERR_ARG, "tensor %d: out has another size or dtype", i);
   }
   if (!norm || ((uintptr_t)norm & 3)) return api_error(LONGER_ERR_ARG, "norm is NULL or not aligned");
-  const int shift = upd::piece_shift(values);
   hipStream_t st = (hipStream_t)stream;
-  for (int i = 0; i < count;) {
-    upd::ClipArgs a;
-    a.count = 0;
-    a.shift = shift;
-    a.norm = norm;
-    uint32_t k = 0;
-    for (; i < count && a.count < upd::kClipList; ++i) {
-      if (!grads[i].n) continue;
-      a.in[a.count] = grads[i].data;
-      a.out[a.count] = out ? out[i].data : grads[i].data;
-      a.n[a.count] = grads[i].n | (grads[i].dtype == LONGER_BF16 ? upd::kHalf : 0);
-      a.first[a.count++] = k;
-      k += upd::pieces(grads[i].n, shift);
-    }
-    if (k) upd::clip_kernel<<<k, 256, 0, st>>>(a);
-  }
+  upd::ClipArgs a;
+  a.norm = norm;
+  upd::launches(count, upd::kClipList, upd::kClipPiece, [&](int i) { return grads[i].n; },
+                [&](int j, int i, int64_t begin, int64_t n, uint32_t first) {
+                  const bool half = grads[i].dtype == LONGER_BF16;
+                  a.in[j] = (const char*)grads[i].data + begin * (half ? 2 : 4);
+                  a.out[j] = (char*)(out ? out[i].data : grads[i].data) + begin * (half ? 2 : 4);
+                  a.n[j] = n | (half ? upd::kHalf : 0);
+                  a.first[j] = first;
+                },
+                [&](int entries, uint32_t k) {
+                  a.count = entries;
+                  upd::clip_kernel<<<k, 256, 0, st>>>(a);
+                });
   return upd::launched("gradient clipping");
 }
 
@@ -374,38 +404,34 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
       for (int k = 0; k < j; ++k)
         if (t[i].n && at[j] && at[j] == at[k]) return api_error(LONGER_ERR_ARG, "tensor %d: two of p, m, v, g, w are the same memory", i);
     values += t[i].n;
-    if (values > upd::kMostValues) return api_error(LONGER_ERR_ARG, "a list of more than 2^44 values");
+    if (values > upd::kMostValues) return api_error(LONGER_ERR_ARG, "a list of more than 2^40 values");
   }
-  const int shift = upd::piece_shift(values);
   hipStream_t st = (hipStream_t)stream;
-  for (int i = 0; i < count;) {
-    upd::StepArgs a;
-    a.count = 0;
-    a.shift = shift;
-    a.norm = norm;
-    a.beta1 = (float)how->beta1;
-    a.one_beta1 = (float)(1. - how->beta1);
-    a.beta2 = (float)how->beta2;
-    a.one_beta2 = (float)(1. - how->beta2);
-    a.rate = (float)(how->lr / (1. - std::pow(how->beta1, (double)how->step)));
-    a.root = (float)(1. / std::sqrt(1. - std::pow(how->beta2, (double)how->step)));
-    a.eps = (float)how->eps;
-    uint32_t k = 0;
-    for (; i < count && a.count < upd::kStepList; ++i) {
-      if (!t[i].n) continue;
-      const int j = a.count++;
-      a.p[j] = t[i].p;
-      a.m[j] = t[i].m;
-      a.v[j] = t[i].v;
-      a.g[j] = t[i].g;
-      a.w[j] = t[i].w;
-      a.n[j] = t[i].n | (t[i].g_dtype == LONGER_BF16 ? upd::kHalf : 0) | (t[i].w && t[i].w_dtype == LONGER_BF16 ? upd::kHalfW : 0);
-      a.decay[j] = (float)(how->lr * t[i].decay);
-      a.first[j] = k;
-      k += upd::pieces(t[i].n, shift);
-    }
-    if (k) upd::step_kernel<<<k, 256, 0, st>>>(a);
-  }
+  upd::StepArgs a;
+  a.norm = norm;
+  a.beta1 = (float)how->beta1;
+  a.one_beta1 = (float)(1. - how->beta1);
+  a.beta2 = (float)how->beta2;
+  a.one_beta2 = (float)(1. - how->beta2);
+  a.rate = (float)(how->lr / (1. - std::pow(how->beta1, (double)how->step)));
+  a.root = (float)(1. / std::sqrt(1. - std::pow(how->beta2, (double)how->step)));
+  a.eps = (float)how->eps;
+  upd::launches(count, upd::kStepList, upd::kStepPiece, [&](int i) { return t[i].n; },
+                [&](int j, int i, int64_t begin, int64_t n, uint32_t first) {
+                  const bool half_g = t[i].g_dtype == LONGER_BF16, half_w = t[i].w && t[i].w_dtype == LONGER_BF16;
+                  a.p[j] = t[i].p + begin;
+                  a.m[j] = t[i].m + begin;
+                  a.v[j] = t[i].v + begin;
+                  a.g[j] = (const char*)t[i].g + begin * (half_g ? 2 : 4);
+                  a.w[j] = t[i].w ? (char*)t[i].w + begin * (half_w ? 2 : 4) : nullptr;
+                  a.n[j] = n | (half_g ? upd::kHalf : 0) | (half_w ? upd::kHalfW : 0);
+                  a.first[j] = first;
+                  a.decay[j] = (float)(how->lr * t[i].decay);
+                },
+                [&](int entries, uint32_t k) {
+                  a.count = entries;
+                  upd::step_kernel<<<k, upd::kStepPiece / 4, 0, st>>>(a);
+                });
   return upd::launched("AdamW update");
 }
 
