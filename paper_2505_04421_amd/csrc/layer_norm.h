@@ -24,6 +24,7 @@ struct Params {
   const void *g, *b;
   const int32_t* lens;
   int rows, L, d;
+  int spread;                       // workgroups' groups in turn, not each workgroup's side by side
   int step_u, step_l;               // rows from one of a workgroup's turns to its next, as users and rows
   float eps, inv_d;
   float* part;                      // backward: [workgroups][2][d] column sums
@@ -97,6 +98,25 @@ struct Columns {
   __device__ __forceinline__ bool own(int i, int j) const { return MODE == FULL || (MODE == PIECES ? lo[i] < V : j >= lo[i]); }
 };
 
+// A row's lanes, or a wave's rows side by side, are a group.  A workgroup's groups of a turn are neighbours (rows that share a cache
+// line are then one die's); where rows may be padding, which comes in long stretches, the workgroups' first groups are neighbours,
+// then their second ones, so that every compute unit has its share (gradients of 512 users of up to 5000 rows of 128: 479 us for 499;
+// but of 128000 dense rows of 255: 99 for 91).
+template <int LPR> constexpr int kGroupRows = LPR < 64 ? 64 / LPR : 1;
+template <int LPR, int THREADS>
+__device__ __forceinline__ int first_turn(const Params& p) {
+  constexpr int RPW = kGroupRows<LPR>, GROUPS = THREADS / LPR / RPW;
+  if (LPR > 64 && GROUPS == 1) return blockIdx.x;
+  const int group = threadIdx.x / (LPR * RPW);
+  return (p.spread ? group * gridDim.x + blockIdx.x : blockIdx.x * GROUPS + group) * RPW;
+}
+
+// (of its first group, which has the most turns: what waves go by that meet at barriers)
+template <int LPR, int THREADS>
+__device__ __forceinline__ int first_of_workgroup(const Params& p) {
+  return p.spread ? blockIdx.x : blockIdx.x * (THREADS / LPR);
+}
+
 // A workgroup's walk over the rows: its next turns' places, and the lengths of their users asked for one turn ahead of the rows.
 struct Walk {
   int r, u, l, n;
@@ -150,12 +170,13 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
   load_vector<T>(g, p.g, c);
   load_vector<T>(b, p.b, c);
   const int step = gridDim.x * RPB;
-  Walk at(p, blockIdx.x * RPB + threadIdx.x / LPR);
+  const int first_row = first_turn<LPR, THREADS>(p);
+  Walk at(p, first_row + (LPR < 64 ? threadIdx.x % 64 / LPR : 0));
   bool ok = at.valid(p);
   Piece<T, V> x[NV];
   load_row<T>(x, p.x, at, ok, c);
   Walk ahead = at.next(p, step);
-  for (int first = blockIdx.x * RPB; first < p.rows; first += step) {
+  for (int first = LPR > 64 ? first_of_workgroup<LPR, THREADS>(p) : first_row; first < p.rows; first += step) {
     // the next turn's rows are under way while this one's are worked on
     const bool ok_ahead = ahead.valid(p);
     Piece<T, V> x_ahead[NV];
@@ -214,9 +235,9 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
 template <typename T, typename U, int V, int LPR, int NV, int MODE>
 __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
   constexpr int THREADS = 1024, RPB = THREADS / LPR, GROUPS = LPR < 64 ? THREADS / 64 : RPB, WIDE = LPR * NV * V;
-  constexpr bool AHEAD = NV * V <= 8;                    // room for the next turn's rows (16 waves leave 128 registers each)
+  constexpr bool AHEAD = NV * V <= 12;                   // room for the next turn's rows (16 waves leave 128 registers each)
   __shared__ float lds[LPR > 64 ? 6 * (THREADS / 64) : 1];
-  __shared__ float sums[GROUPS > 1 ? 2 * WIDE : 1];
+  __shared__ float sums[GROUPS > 1 ? GROUPS * WIDE : 1];
   const Columns<V, LPR, NV, MODE> c(threadIdx.x % LPR, p.d);
   float g[NV][V], dg[NV][V], db[NV][V];
   load_vector<T>(g, p.g, c);
@@ -225,14 +246,15 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
 #pragma unroll
     for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f;
   const int step = gridDim.x * RPB;
-  Walk at(p, blockIdx.x * RPB + threadIdx.x / LPR);
+  const int first_row = first_turn<LPR, THREADS>(p);
+  Walk at(p, first_row + (LPR < 64 ? threadIdx.x % 64 / LPR : 0));
   bool ok = at.valid(p);
   Piece<T, V> x[NV];
   Piece<U, V> dy[NV];
   load_row<T>(x, p.x, at, ok, c);
   load_row<U>(dy, p.dy, at, ok, c);
   Walk ahead = at.next(p, step);
-  for (int first = blockIdx.x * RPB; first < p.rows; first += step) {
+  for (int first = LPR > 64 ? first_of_workgroup<LPR, THREADS>(p) : first_row; first < p.rows; first += step) {
     const bool ok_ahead = ahead.valid(p);
     Piece<T, V> x_ahead[NV];
     Piece<U, V> dy_ahead[NV];
@@ -303,54 +325,63 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
     ok = ok_ahead;
     ahead = ahead2;
   }
-  // columns: the rows of a wave, then the workgroup's groups of rows, one after the other
+  // columns: the rows of a wave, then the workgroup's groups of rows
   float* part = p.part + (size_t)blockIdx.x * 2 * p.d;
-  if constexpr (GROUPS == 1) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (c.own(i, j)) { part[c.col[i] + j] = dg[i][j]; part[p.d + c.col[i] + j] = db[i][j]; }
-  } else {
-    if constexpr (LPR < 64) {
+  auto leave = [&](float (&v)[NV][V], float* out) {
+    if constexpr (GROUPS == 1) {
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j)
-#pragma unroll
-          for (int o = LPR; o < 64; o <<= 1) { dg[i][j] += __shfl_xor(dg[i][j], o); db[i][j] += __shfl_xor(db[i][j], o); }
-    }
-    const int group = threadIdx.x / (LPR < 64 ? 64 : LPR);
-    const bool first_rows = LPR >= 64 || (threadIdx.x & 63) < LPR;
-    for (int k = 0; k < GROUPS; ++k) {
-      if (group == k && first_rows)
+          if (c.own(i, j)) out[c.col[i] + j] = v[i][j];
+    } else {
+      if constexpr (LPR < 64) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
           for (int j = 0; j < V; ++j)
-            if (c.own(i, j)) {
-              float* at = sums + c.col[i] + j;
-              at[0] = k ? at[0] + dg[i][j] : dg[i][j];
-              at[WIDE] = k ? at[WIDE] + db[i][j] : db[i][j];
-            }
+#pragma unroll
+            for (int o = LPR; o < 64; o <<= 1) v[i][j] += __shfl_xor(v[i][j], o);
+      }
+      float* mine = sums + threadIdx.x / (LPR < 64 ? 64 : LPR) * WIDE;
+      if (LPR >= 64 || (threadIdx.x & 63) < LPR)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (c.own(i, j)) mine[c.col[i] + j] = v[i][j];
       __syncthreads();
+      for (int i = threadIdx.x; i < p.d; i += THREADS) {
+        float t = 0.f;
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) t += sums[k * WIDE + i];
+        out[i] = t;
+      }
     }
-    for (int i = threadIdx.x; i < p.d; i += THREADS) { part[i] = sums[i]; part[p.d + i] = sums[WIDE + i]; }
-  }
+  };
+  leave(dg, part);
+  __syncthreads();
+  leave(db, part + p.d);
 }
 
 // ------------------------------------------------------------------------------------ host
 struct Shape { int lpr, nv, mode, v; };
 
-// lanes and pieces of a row for pieces of `v` values: as few lanes as hold it with `wave` pieces each where a wave can, with `more`
-// each beyond
-inline Shape shape(int d, int v, int wave, int more) {
+// Lanes and pieces of a row, for pieces of `v` values: up to `most` pieces a lane, as few places for pieces as hold the row; at equal
+// count as few lanes.  A row wider than 1024 lanes hold that way has as many a lane as it needs.
+inline Shape shape(int d, int v, int most) {
   if (d < v) return {8, 1, PIECES, 1};
   const int pieces = (d + v - 1) / v;
   Shape s = {1, 1, 0, v};
   while (s.lpr < pieces && s.lpr < 64) s.lpr *= 2;
-  while (pieces > s.lpr * (s.lpr > 64 ? more : wave) && s.lpr < 1024) s.lpr *= 2;
-  s.nv = (pieces + s.lpr - 1) / s.lpr;
+  if (pieces > 64) {
+    s.lpr = 1024;
+    s.nv = (pieces + 1023) / 1024;
+    for (int lpr = 512; lpr >= 64; lpr /= 2) {
+      const int nv = (pieces + lpr - 1) / lpr;
+      if (nv <= most && lpr * nv <= s.lpr * s.nv) { s.lpr = lpr; s.nv = nv; }
+    }
+  }
   s.mode = d % v ? VALUES : pieces == s.lpr * s.nv ? FULL : PIECES;
   return s;
 }
@@ -364,7 +395,8 @@ inline unsigned resident(K kernel, int threads) {
   return 256u * n;
 }
 
-inline void set_step(Params& p, unsigned grid, int rows_per_turn) {
+inline void set_step(Params& p, unsigned grid, int rows_per_turn, bool spread) {
+  p.spread = spread;
   const int64_t step = (int64_t)grid * rows_per_turn;
   p.step_u = (int)(step / p.L);
   p.step_l = (int)(step % p.L);
@@ -374,8 +406,12 @@ template <typename T, int V, int LPR, int NV, int MODE>
 inline void launch_norm(Params& p, hipStream_t st) {
   constexpr int THREADS = LPR > 256 ? LPR : 256, RPB = THREADS / LPR;
   static const unsigned most = resident(norm_kernel<T, V, LPR, NV, MODE, THREADS>, THREADS);
-  const unsigned turns = ((unsigned)p.rows + RPB - 1) / RPB, grid = turns < most ? turns : most;
-  set_step(p, grid, RPB);
+  const unsigned turns = ((unsigned)p.rows + RPB - 1) / RPB;
+  unsigned grid = turns < most ? turns : most;
+  // ragged users: shares of eight turns, dealt as workgroups end (512 users of up to 5000 rows of 128: 177 us for 197)
+  const bool dealt = p.lens && turns >= 32 * most;
+  if (dealt) grid = turns / 8;
+  set_step(p, grid, RPB, p.lens && !dealt);
   norm_kernel<T, V, LPR, NV, MODE, THREADS><<<grid, THREADS, 0, st>>>(p);
 }
 template <typename T, int V, int LPR, int NV>
@@ -388,7 +424,7 @@ inline void launch_norm(Params& p, int mode, hipStream_t st) {
 // (four pieces a lane in one wave before a row takes several, which meet in LDS)
 template <typename T, int V>
 inline void norm(Params& p, hipStream_t st) {
-  const Shape s = shape(p.d, V, 4, 4);
+  const Shape s = shape(p.d, V, 4);
   if (s.v == 1) return launch_norm<T, 1, 8, 1>(p, s.mode, st);
   switch (s.lpr * 8 + s.nv) {
     case 1 * 8 + 1: return launch_norm<T, V, 1, 1>(p, s.mode, st);
@@ -421,7 +457,7 @@ inline unsigned launch_grad(Params& p, unsigned most, float* only, hipStream_t s
   const unsigned turns = ((unsigned)p.rows + 1024 / LPR - 1) / (1024 / LPR);
   unsigned grid = turns < held ? turns : held;
   if (grid > most) grid = most;
-  set_step(p, grid, 1024 / LPR);
+  set_step(p, grid, 1024 / LPR, p.lens != nullptr);
   if (grid == 1) p.part = only;
   grad_kernel<T, U, V, LPR, NV, MODE><<<grid, 1024, 0, st>>>(p);
   return grid;
@@ -434,11 +470,10 @@ inline unsigned launch_grad(Params& p, int mode, unsigned most, float* only, hip
   return 0;
 }
 
-// (8 values a lane, beside their column sums and the next turn's; more only where even a workgroup's lanes are too few)
+// (up to 8 or 12 values a lane, beside their column sums and the next turn's; 16 only where a workgroup's lanes are too few)
 template <typename T, typename U, int V>
 inline unsigned grad(Params& p, unsigned most, float* only, hipStream_t st) {
-  constexpr int N = 8 / V;
-  const Shape s = shape(p.d, V, N, N);
+  const Shape s = shape(p.d, V, V == 4 ? 3 : 1);
   if (s.v == 1) return launch_grad<T, U, 1, 8, 1>(p, s.mode, most, only, st);
   switch (s.lpr * 8 + s.nv) {
     case 1 * 8 + 1: return launch_grad<T, U, V, 1, 1>(p, s.mode, most, only, st);
@@ -448,16 +483,29 @@ inline unsigned grad(Params& p, unsigned most, float* only, hipStream_t st) {
     case 16 * 8 + 1: return launch_grad<T, U, V, 16, 1>(p, s.mode, most, only, st);
     case 32 * 8 + 1: return launch_grad<T, U, V, 32, 1>(p, s.mode, most, only, st);
     case 64 * 8 + 1: return launch_grad<T, U, V, 64, 1>(p, s.mode, most, only, st);
-    case 128 * 8 + N: return launch_grad<T, U, V, 128, N>(p, s.mode, most, only, st);
-    case 256 * 8 + N: return launch_grad<T, U, V, 256, N>(p, s.mode, most, only, st);
-    case 512 * 8 + N: return launch_grad<T, U, V, 512, N>(p, s.mode, most, only, st);
-    case 1024 * 8 + N: return launch_grad<T, U, V, 1024, N>(p, s.mode, most, only, st);
   }
   if constexpr (V == 4) {
-    if (s.lpr == 64) return launch_grad<T, U, V, 64, 2>(p, s.mode, most, only, st);
-    return s.nv == 3 ? launch_grad<T, U, V, 1024, 3>(p, s.mode, most, only, st) : launch_grad<T, U, V, 1024, 4>(p, s.mode, most, only, st);
+    switch (s.lpr * 8 + s.nv) {
+      case 64 * 8 + 2: return launch_grad<T, U, V, 64, 2>(p, s.mode, most, only, st);
+      case 64 * 8 + 3: return launch_grad<T, U, V, 64, 3>(p, s.mode, most, only, st);
+      case 128 * 8 + 2: return launch_grad<T, U, V, 128, 2>(p, s.mode, most, only, st);
+      case 128 * 8 + 3: return launch_grad<T, U, V, 128, 3>(p, s.mode, most, only, st);
+      case 256 * 8 + 2: return launch_grad<T, U, V, 256, 2>(p, s.mode, most, only, st);
+      case 256 * 8 + 3: return launch_grad<T, U, V, 256, 3>(p, s.mode, most, only, st);
+      case 512 * 8 + 2: return launch_grad<T, U, V, 512, 2>(p, s.mode, most, only, st);
+      case 512 * 8 + 3: return launch_grad<T, U, V, 512, 3>(p, s.mode, most, only, st);
+      case 1024 * 8 + 2: return launch_grad<T, U, V, 1024, 2>(p, s.mode, most, only, st);
+      case 1024 * 8 + 3: return launch_grad<T, U, V, 1024, 3>(p, s.mode, most, only, st);
+      default: return launch_grad<T, U, V, 1024, 4>(p, s.mode, most, only, st);
+    }
   } else {
-    return launch_grad<T, U, V, 1024, 2>(p, s.mode, most, only, st);
+    switch (s.lpr * 8 + s.nv) {
+      case 128 * 8 + 1: return launch_grad<T, U, V, 128, 1>(p, s.mode, most, only, st);
+      case 256 * 8 + 1: return launch_grad<T, U, V, 256, 1>(p, s.mode, most, only, st);
+      case 512 * 8 + 1: return launch_grad<T, U, V, 512, 1>(p, s.mode, most, only, st);
+      case 1024 * 8 + 1: return launch_grad<T, U, V, 1024, 1>(p, s.mode, most, only, st);
+      default: return launch_grad<T, U, V, 1024, 2>(p, s.mode, most, only, st);
+    }
   }
 }
 

@@ -100,7 +100,7 @@ int longer_layer_norm(const longer_rows* x, const void* ln_g, const void* ln_b, 
   if (!rc && !(eps >= FLT_MIN)) rc = api_error(LONGER_ERR_ARG, "eps must be positive (a normal number)");
   if (!rc && ((uintptr_t)lens & 3)) rc = api_error(LONGER_ERR_ARG, "lens is not aligned");
   if (rc) return rc;
-  ln::Params p = {ln::rows_of(x, B, L), {}, ln::rows_of(y, B, L), ln_g, ln_b, lens, B * L, L, d, 0, 0, eps, 1.f / d, nullptr};
+  ln::Params p = {ln::rows_of(x, B, L), {}, ln::rows_of(y, B, L), ln_g, ln_b, lens, B * L, L, d, 0, 0, 0, eps, 1.f / d, nullptr};
   if (x->dtype == LONGER_F32) ln::norm_f32(p, (hipStream_t)stream);
   else ln::norm_bf16(p, (hipStream_t)stream);
   return ln::launched("layer norm");
@@ -129,7 +129,7 @@ int longer_layer_norm_backward(const longer_rows* x, const void* ln_g, const lon
   if (rc) return rc;
   const size_t need = ln::workspace_bytes(B, L, d);
   if (ws_bytes < need) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, need);
-  ln::Params p = {ln::rows_of(x, B, L), ln::rows_of(dy, B, L), ln::rows_of(dx, B, L), ln_g, nullptr, lens, B * L, L, d, 0, 0, eps, 1.f / d,
+  ln::Params p = {ln::rows_of(x, B, L), ln::rows_of(dy, B, L), ln::rows_of(dx, B, L), ln_g, nullptr, lens, B * L, L, d, 0, 0, 0, eps, 1.f / d,
                   (float*)ws};
   hipStream_t st = (hipStream_t)stream;
   const unsigned groups = x->dtype == LONGER_F32 ? ln::grad_f32(p, ln::kGradGroups, grads_out, st)
