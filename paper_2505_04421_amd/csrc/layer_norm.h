@@ -59,28 +59,38 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-// Sum of N values over a row's lanes.  Rows of several waves meet in LDS, in one of two places in turn: a wave that writes a place
-// again has passed the barrier of the other one, which every wave reaches after its reads.
-template <int LPR, int THREADS, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float* lds, int turn) {
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = lanes_sum<(LPR < 64 ? LPR : 64)>(v[k]);
-  if constexpr (LPR > 64) {
-    constexpr int W = THREADS / 64, S = LPR / 64;
-    float* at = lds + turn * 3 * W;
-    const int wave = threadIdx.x / 64;
-    if ((threadIdx.x & 63) == 0)
-#pragma unroll
-      for (int k = 0; k < N; ++k) at[k * W + wave] = v[k];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      v[k] = 0.f;
-#pragma unroll
-      for (int s = 0; s < S; ++s) v[k] += at[k * W + wave / S * S + s];
-    }
+// Rows of several waves.  Each wave centres its values on its own mean; then one barrier a row brings the waves' sums together:
+// with n_w values, mean m_w and e_w = m_w - mean, the row's centred squares are sum of (wave's + n_w e_w^2), its sum of q (x - mean)
+// is sum of (wave's q (x - m_w) + e_w wave's q), none of which cancels.  Two places in LDS in turn: a wave that writes one again has
+// passed the other's barrier, which every wave reaches after its reads.
+struct Shares { float s, squares, q, qx; };
+template <int LPR, int THREADS>
+struct Meeting {
+  static constexpr int W = THREADS / 64, S = LPR / 64;
+  struct Memory { Shares at[2][W]; float n[W], inv_n[W]; };
+  Memory& m;
+  float inv_n;
+  int turn = 0;
+  __device__ __forceinline__ Meeting(Memory& memory, int own) : m(memory) {      // own: values of the row that the lane has
+    const float n = lanes_sum<64>((float)own);
+    inv_n = n > 0.f ? 1.f / n : 0.f;
+    if ((threadIdx.x & 63) == 0) { m.n[threadIdx.x / 64] = n; m.inv_n[threadIdx.x / 64] = inv_n; }
   }
-}
+  // the wave's shares (s: its sum) to the row's; gives the row's mean, the same bits in every wave (two may hold the same value)
+  __device__ __forceinline__ float join(Shares& v, float inv_d) {
+    const int wave = threadIdx.x / 64;
+    if ((threadIdx.x & 63) == 0) m.at[turn][wave] = v;
+    __syncthreads();
+    const int other = wave / S * S + threadIdx.x % S;
+    Shares o = m.at[turn][other];
+    turn ^= 1;
+    const float mean = lanes_sum<S>(o.s) * inv_d, e = o.s * m.inv_n[other] - mean;
+    v.squares = lanes_sum<S>(fmaf(m.n[other] * e, e, o.squares));
+    v.q = lanes_sum<S>(o.q);
+    v.qx = lanes_sum<S>(fmaf(e, o.q, o.qx));
+    return mean;
+  }
+};
 
 // A lane's columns
 template <int V, int LPR, int NV, int MODE>
@@ -95,6 +105,20 @@ struct Columns {
     }
   }
   __device__ __forceinline__ bool there(int i) const { return MODE == FULL || lo[i] < V; }
+  // whether some lane of the wave has values that are not its own: only there sums leave values out
+  __device__ __forceinline__ bool masked() const {
+    if (MODE == FULL) return false;
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) some |= lo[i] > 0;
+    return __builtin_amdgcn_ballot_w64(some) != 0;
+  }
+  __device__ __forceinline__ int owned() const {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) n += MODE == FULL ? V : V - lo[i];
+    return n;
+  }
   __device__ __forceinline__ bool own(int i, int j) const { return MODE == FULL || (MODE == PIECES ? lo[i] < V : j >= lo[i]); }
 };
 
@@ -164,8 +188,11 @@ __device__ __forceinline__ void load_vector(float (&v)[NV][V], const void* p, co
 template <typename T, int V, int LPR, int NV, int MODE, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
   constexpr int RPB = THREADS / LPR;
-  __shared__ float lds[LPR > 64 ? 6 * (THREADS / 64) : 1];
+  typedef Meeting<(LPR > 64 ? LPR : 64), THREADS> Waves;
+  __shared__ typename Waves::Memory lds;
   const Columns<V, LPR, NV, MODE> c(threadIdx.x % LPR, p.d);
+  Waves waves(lds, c.owned());
+  const bool masked = c.masked();
   float g[NV][V], b[NV][V];
   load_vector<T>(g, p.g, c);
   load_vector<T>(b, p.b, c);
@@ -185,27 +212,45 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
     float y[NV][V];
     // (no row of the wave counts: nothing to do; rows of several waves meet at barriers, which their whole workgroup has to reach)
     if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : RPB > 1 || ok) {
-      float s[1] = {0.f};
+      Shares s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          y[i][j] = (float)x[i][j];
-          s[0] += MODE != VALUES || c.own(i, j) ? y[i][j] : 0.f;       // (a piece past the row holds zeros)
-        }
-      row_sum<LPR, THREADS>(s, lds, 0);
-      const float mean = s[0] * p.inv_d;
-      s[0] = 0.f;
+        for (int j = 0; j < V; ++j) y[i][j] = (float)x[i][j];
+      auto sum = [&](auto all) {
+        s.s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) s.s += decltype(all)::value || c.own(i, j) ? y[i][j] : 0.f;
+      };
+      // (a piece past the row holds zeros)
+      if (MODE == VALUES && masked) sum(std::false_type()); else sum(std::true_type());
+      s.s = lanes_sum<(LPR < 64 ? LPR : 64)>(s.s);
+      const float mean = s.s * (LPR > 64 ? waves.inv_n : p.inv_d);
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          y[i][j] -= mean;
-          const float own = c.own(i, j) ? y[i][j] : 0.f;
-          s[0] = fmaf(own, own, s[0]);
-        }
-      row_sum<LPR, THREADS>(s, lds, 1);
-      const float r = __builtin_amdgcn_rsqf(fmaf(s[0], p.inv_d, p.eps));
+        for (int j = 0; j < V; ++j) y[i][j] -= mean;
+      auto squares = [&](auto all) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float own = decltype(all)::value || c.own(i, j) ? y[i][j] : 0.f;
+            s.squares = fmaf(own, own, s.squares);
+          }
+      };
+      if (masked) squares(std::false_type()); else squares(std::true_type());
+      s.squares = lanes_sum<(LPR < 64 ? LPR : 64)>(s.squares);
+      if constexpr (LPR > 64) {
+        const float row_mean = waves.join(s, p.inv_d);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) y[i][j] = (float)x[i][j] - row_mean;
+      }
+      const float r = __builtin_amdgcn_rsqf(fmaf(s.squares, p.inv_d, p.eps));
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -230,15 +275,18 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
   }
 }
 
-// dx = r (q - mean(q) - xh mean(q xh)), q = dy g, and the workgroup's share of sum dy xh and sum dy.  The second sum over a row
-// takes the centred squares, q and q (x - mean) at once.
+// dx = r (q - mean(q) - xh mean(q xh)), q = dy g, and the workgroup's share of sum dy xh and sum dy.  Beside the centred squares a
+// row's sums of q and q (x - mean) are taken.
 template <typename T, typename U, int V, int LPR, int NV, int MODE>
 __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
   constexpr int THREADS = 1024, RPB = THREADS / LPR, GROUPS = LPR < 64 ? THREADS / 64 : RPB, WIDE = LPR * NV * V;
-  constexpr bool AHEAD = NV * V <= 12;                   // room for the next turn's rows (16 waves leave 128 registers each)
-  __shared__ float lds[LPR > 64 ? 6 * (THREADS / 64) : 1];
+  constexpr bool AHEAD = NV * V <= 8;                    // room for the next turn's rows beside this one's (16 waves leave 128 registers each)
+  typedef Meeting<(LPR > 64 ? LPR : 64), THREADS> Waves;
+  __shared__ typename Waves::Memory lds;
   __shared__ float sums[GROUPS > 1 ? GROUPS * WIDE : 1];
   const Columns<V, LPR, NV, MODE> c(threadIdx.x % LPR, p.d);
+  Waves waves(lds, c.owned());
+  const bool masked = c.masked();
   float g[NV][V], dg[NV][V], db[NV][V];
   load_vector<T>(g, p.g, c);
 #pragma unroll
@@ -263,44 +311,61 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
       load_row<U>(dy_ahead, p.dy, ahead, ok_ahead, c);
     }
     const Walk ahead2 = ahead.next(p, step);
-    float xc[NV][V], k0 = 0.f, k1 = 0.f, k2 = 0.f;      // dx = k0 q + k1 (x - mean) + k2
+    float xc[NV][V];
     if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : RPB > 1 || ok) {
-      float s[1] = {0.f};
+      constexpr int WAVE = LPR < 64 ? LPR : 64;
+      Shares s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) xc[i][j] = (float)x[i][j];
+      auto sum = [&](auto all) {
+        s.s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) s.s += decltype(all)::value || c.own(i, j) ? xc[i][j] : 0.f;
+      };
+      if (MODE == VALUES && masked) sum(std::false_type()); else sum(std::true_type());
+      s.s = lanes_sum<WAVE>(s.s);
+      const float mean = s.s * (LPR > 64 ? waves.inv_n : p.inv_d);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) xc[i][j] -= mean;
+      auto sums = [&](auto all) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const bool mine = decltype(all)::value || c.own(i, j);
+            const float own = mine ? xc[i][j] : 0.f, q = mine ? (float)dy[i][j] * g[i][j] : 0.f;
+            s.squares = fmaf(own, own, s.squares);
+            s.q += q;
+            s.qx = fmaf(q, own, s.qx);
+          }
+      };
+      if (masked) sums(std::false_type()); else sums(std::true_type());
+      s.squares = lanes_sum<WAVE>(s.squares);
+      s.q = lanes_sum<WAVE>(s.q);
+      s.qx = lanes_sum<WAVE>(s.qx);
+      if constexpr (LPR > 64) {
+        const float row_mean = waves.join(s, p.inv_d);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) xc[i][j] = (float)x[i][j] - row_mean;
+      }
+      const float r = __builtin_amdgcn_rsqf(fmaf(s.squares, p.inv_d, p.eps));
+      const float k1 = -(s.qx * p.inv_d) * r * r * r, k2 = -(s.q * p.inv_d) * r;       // dx = r q + k1 (x - mean) + k2
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          xc[i][j] = (float)x[i][j];
-          s[0] += MODE != VALUES || c.own(i, j) ? xc[i][j] : 0.f;
-        }
-      row_sum<LPR, THREADS>(s, lds, 0);
-      const float mean = s[0] * p.inv_d;
-      float t[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          xc[i][j] -= mean;
-          const float own = c.own(i, j) ? xc[i][j] : 0.f;
-          float q = (float)dy[i][j] * g[i][j];
-          if (MODE == VALUES && !c.own(i, j)) q = 0.f;
-          t[0] = fmaf(own, own, t[0]);
-          t[1] += q;
-          t[2] = fmaf(q, own, t[2]);
-        }
-      row_sum<LPR, THREADS>(t, lds, 1);
-      const float r = __builtin_amdgcn_rsqf(fmaf(t[0], p.inv_d, p.eps));
-      k0 = r;
-      k1 = -(t[2] * p.inv_d) * r * r * r;
-      k2 = -(t[1] * p.inv_d) * r;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float v = (float)dy[i][j];
+          const float v = (float)dy[i][j], rv = r * v;                  // (a row that does not count: v = 0, x - mean = 0)
           db[i][j] += v;
-          dg[i][j] = fmaf(v, xc[i][j] * r, dg[i][j]);           // (a row that does not count: v = 0, xc = 0)
-          xc[i][j] = fmaf(k0 * v, g[i][j], fmaf(k1, xc[i][j], k2));
+          dg[i][j] = fmaf(rv, xc[i][j], dg[i][j]);
+          xc[i][j] = fmaf(rv, g[i][j], fmaf(k1, xc[i][j], k2));
         }
     }
     if (at.r < p.rows) {
