@@ -3,7 +3,9 @@
 #include "../../include/longer.h"
 #include "device.h"
 
+#include <algorithm>
 #include <cmath>
+#include <cstring>
 
 namespace longer {
 
@@ -17,17 +19,23 @@ namespace upd {
 // pieces, numbered over the launch's list; a workgroup takes one.
 struct Piece { int t; int64_t begin; };
 
-// first[i] = number of tensor i's first piece, ascending: the last i with first[i] <= b (an empty tensor is not in the list)
-template <int N>
-__device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int count, uint32_t b, int64_t values) {
+// the last of `count` ascending numbers at first[0], first[STRIDE], ... that is not above b: the tensor of piece b, by the number of its
+// first piece (an empty tensor is not in the list)
+template <int N, int STRIDE>
+__device__ __forceinline__ int find_piece(const uint32_t* first, int count, uint32_t b) {
   const int lane = threadIdx.x & 63;
   int n = 0;
 #pragma unroll
   for (int k = 0; k < N; k += 64) {
     const int i = k + lane;
-    n += __popcll(__ballot(i < count && first[i < N ? i : 0] <= b));
+    n += __popcll(__ballot(i < count && first[(i < N ? i : 0) * STRIDE] <= b));
   }
-  return {n - 1, (b - first[n - 1]) * values};
+  return n - 1;
+}
+template <int N>
+__device__ __forceinline__ Piece find_piece(const uint32_t (&first)[N], int count, uint32_t b, int64_t values) {
+  const int t = find_piece<N, 1>(first, count, b);
+  return {t, (b - first[t]) * values};
 }
 
 // 16 bytes of a tensor, aligned to its element only
@@ -36,7 +44,7 @@ template <typename T> using Line = typename Line_<T>::type;
 template <typename T> struct Four_ { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
 template <typename T> using Four = typename Four_<T>::type;
 
-constexpr int kNormList = 192, kClipList = 128, kStepList = 64;
+constexpr int kNormList = 192, kClipList = 128;
 // Values of a piece.  An update has five streams to keep going and a clip two: with small pieces, in the list's order, what is under
 // way at one time is one stretch of each, in few memory pages (128 million parameters, an update in pieces of 1024 / 2048 / 4096 /
 // 8192 / 32768 values by 256 threads: 725 / 765 / 808 / 830 / 890 us; four values a thread in workgroups of 256 / 512 / 1024: 725 /
@@ -44,9 +52,8 @@ constexpr int kNormList = 192, kClipList = 128, kStepList = 64;
 // pieces, each of which leaves a sum to be joined, are as large as keeps every compute unit busy (at 2048 in all instead of 4096:
 // 180 us for 171).
 constexpr int kStepPiece = 4096, kClipPiece = 2048;
-constexpr int64_t kHalf = (int64_t)1 << 62;         // in a tensor's size: its values (an update's gradients) are bf16
-constexpr int64_t kHalfW = (int64_t)1 << 61;        // and the update's copy w is
-constexpr int64_t kCount = kHalfW - 1;
+constexpr int64_t kHalf = (int64_t)1 << 62;         // in a tensor's size: its values are bf16
+constexpr int64_t kCount = kHalf - 1;
 
 struct NormArgs {
   const void* data[kNormList];
@@ -63,15 +70,16 @@ struct ClipArgs {
   const float* norm;
   int count;
 };
+// An update's list.  Tensors whose p, m, v, g and w each lie in one buffer, at the same place, as a training program keeps them, share
+// the buffers' addresses: a tensor is an entry of kEntry words from the front of the list (its place in values, 64 bits; its values; its first
+// piece; lr * decay; its buffers and types), the buffers are kBuffers words from the end: 155 tensors of common buffers to a launch,
+// or 58 with buffers of their own.
+constexpr int kStepWords = 940, kEntry = 6, kBuffers = 10, kStepList = 192;
+constexpr uint32_t kHalfG = 1u << 16, kHalfW = 1u << 17, kCopy = 1u << 18, kGroup = 0xffff;
 struct StepArgs {
-  float *p[kStepList], *m[kStepList], *v[kStepList];
-  const void* g[kStepList];
-  void* w[kStepList];
-  int64_t n[kStepList];
-  uint32_t first[kStepList];
-  float decay[kStepList];                            // lr * decay
-  const float* norm;
+  uint32_t list[kStepWords];
   int count;
+  const float* norm;
   float beta1, one_beta1, beta2, one_beta2, rate, root, eps;   // rate = lr / (1 - beta1^t), root = 1 / sqrt(1 - beta2^t)
 };
 
@@ -213,18 +221,18 @@ __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, ui
   }
 }
 
+__device__ __forceinline__ uint64_t two_words(const uint32_t* w) { return w[0] | (uint64_t)w[1] << 32; }
+
 template <typename G>
-__device__ __forceinline__ void step_piece(const StepArgs& a, Place t, int64_t begin, bool half_w, uint32_t n, float c, float decay) {
-  t.p += begin;
-  t.m += begin;
-  t.v += begin;
-  t.g = (const G*)t.g + begin;
-  if (!t.w) return step_piece<G, float, false>(a, t, n, c, decay);
-  if (half_w) {
-    t.w = (__bf16*)t.w + begin;
+__device__ __forceinline__ void step_piece(const StepArgs& a, const uint32_t* buffers, int64_t at, uint32_t kind, uint32_t n, float c, float decay) {
+  Place t = {(float*)two_words(buffers) + at, (float*)two_words(buffers + 2) + at, (float*)two_words(buffers + 4) + at,
+             (const G*)two_words(buffers + 6) + at, nullptr};
+  if (!(kind & kCopy)) return step_piece<G, float, false>(a, t, n, c, decay);
+  if (kind & kHalfW) {
+    t.w = (__bf16*)two_words(buffers + 8) + at;
     return step_piece<G, __bf16, true>(a, t, n, c, decay);
   }
-  t.w = (float*)t.w + begin;
+  t.w = (float*)two_words(buffers + 8) + at;
   step_piece<G, float, true>(a, t, n, c, decay);
 }
 
@@ -234,12 +242,13 @@ __global__ __launch_bounds__(kStepPiece / 4) void step_kernel(StepArgs a) {
     if (!isfinite(a.norm[0])) return;
     c = a.norm[1];
   }
-  const Piece w = find_piece(a.first, a.count, blockIdx.x, kStepPiece);
-  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)kStepPiece);
-  const bool half_w = a.n[w.t] & kHalfW;
-  const Place t = {a.p[w.t], a.m[w.t], a.v[w.t], a.g[w.t], a.w[w.t]};
-  if (a.n[w.t] & kHalf) step_piece<__bf16>(a, t, w.begin, half_w, n, c, a.decay[w.t]);
-  else step_piece<float>(a, t, w.begin, half_w, n, c, a.decay[w.t]);
+  const uint32_t* e = a.list + kEntry * find_piece<kStepList, kEntry>(a.list + 3, a.count, blockIdx.x);
+  const uint32_t begin = (blockIdx.x - e[3]) * kStepPiece, n = min(e[2] - begin, (uint32_t)kStepPiece), kind = e[5];
+  const int64_t at = (int64_t)two_words(e) + begin;
+  const uint32_t* buffers = a.list + kStepWords - kBuffers * ((kind & kGroup) + 1);
+  const float decay = __uint_as_float(e[4]);
+  if (kind & kHalfG) step_piece<__bf16>(a, buffers, at, kind, n, c, decay);
+  else step_piece<float>(a, buffers, at, kind, n, c, decay);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -249,6 +258,7 @@ static int launched(const char* what) {
   return hipGetLastError() == hipSuccess ? 0 : api_error(LONGER_ERR_HIP, "%s launch failed", what);
 }
 
+constexpr int64_t kMostEntry = (int64_t)1 << 30;     // values of one place in a launch's list
 constexpr int64_t kMostValues = (int64_t)1 << 40;    // of a list: more than a GPU's memory holds
 
 static int check_tensor(const void* p, int64_t n, int dtype, int i, const char* name) {
@@ -288,20 +298,21 @@ static uint32_t list_pieces(const longer_tensor* t, int count, int64_t piece) {
 static size_t norm_bytes(uint32_t n) { return ((size_t)(n ? n : 1) * 8 + 255) & ~(size_t)255; }
 
 // Cuts a list into launches: `add(j, i, begin, n, first)` puts values [begin, begin + n) of tensor i in place j of a launch, their
-// pieces numbered from `first`; `go(entries, pieces)` launches.  A launch ends with its list full or at 2^23 workgroups (the grid
-// counts threads in 32 bits); a tensor may go on in the next.
+// pieces numbered from `first`, or says that the launch has no room for them; `go(entries, pieces)` launches.  A launch ends full or at
+// `most_pieces` workgroups (the grid counts threads in 32 bits); a tensor may go on in the next place.
 template <typename Size, typename Add, typename Go>
-static void launches(int count, int most, int64_t piece, Size size, Add add, Go go) {
-  constexpr uint32_t kMostPieces = 1u << 23;
+static void launches(int count, int64_t piece, uint32_t most_pieces, Size size, Add add, Go go) {
   int64_t begin = 0;
   for (int i = 0; i < count;) {
     int entries = 0;
     uint32_t k = 0;
-    while (i < count && entries < most && k < kMostPieces) {
+    while (i < count && k < most_pieces) {
       const int64_t left = size(i) - begin;
-      const int64_t n = left < (kMostPieces - k) * piece ? left : (kMostPieces - k) * piece;
+      const int64_t room = std::min((most_pieces - k) * piece, std::max(piece, kMostEntry));
+      const int64_t n = std::min(left, room);
       if (n) {
-        add(entries++, i, begin, n, k);
+        if (!add(entries, i, begin, n, k)) break;
+        ++entries;
         k += pieces(n, piece);
       }
       begin += n;
@@ -339,12 +350,14 @@ int longer_grad_norm(const longer_tensor* grads, int count, float max_norm, floa
   uint32_t done = 0;
   upd::NormArgs a;
   a.piece = piece;
-  upd::launches(count, upd::kNormList, piece, [&](int i) { return grads[i].n; },
+  upd::launches(count, piece, 1u << 23, [&](int i) { return grads[i].n; },
                 [&](int j, int i, int64_t begin, int64_t n, uint32_t first) {
+                  if (j == upd::kNormList) return false;
                   const bool half = grads[i].dtype == LONGER_BF16;
                   a.data[j] = (const char*)grads[i].data + begin * (half ? 2 : 4);
                   a.n[j] = n | (half ? upd::kHalf : 0);
                   a.first[j] = first;
+                  return true;
                 },
                 [&](int entries, uint32_t k) {
                   a.count = entries;
@@ -367,13 +380,15 @@ int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, 
   hipStream_t st = (hipStream_t)stream;
   upd::ClipArgs a;
   a.norm = norm;
-  upd::launches(count, upd::kClipList, upd::kClipPiece, [&](int i) { return grads[i].n; },
+  upd::launches(count, upd::kClipPiece, 1u << 23, [&](int i) { return grads[i].n; },
                 [&](int j, int i, int64_t begin, int64_t n, uint32_t first) {
+                  if (j == upd::kClipList) return false;
                   const bool half = grads[i].dtype == LONGER_BF16;
                   a.in[j] = (const char*)grads[i].data + begin * (half ? 2 : 4);
                   a.out[j] = (char*)(out ? out[i].data : grads[i].data) + begin * (half ? 2 : 4);
                   a.n[j] = n | (half ? upd::kHalf : 0);
                   a.first[j] = first;
+                  return true;
                 },
                 [&](int entries, uint32_t k) {
                   a.count = entries;
@@ -416,17 +431,40 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
   a.rate = (float)(how->lr / (1. - std::pow(how->beta1, (double)how->step)));
   a.root = (float)(1. / std::sqrt(1. - std::pow(how->beta2, (double)how->step)));
   a.eps = (float)how->eps;
-  upd::launches(count, upd::kStepList, upd::kStepPiece, [&](int i) { return t[i].n; },
+  int groups = 0;                                     // of the launch at hand, and the last one's buffers, where place 0 would be
+  uint64_t last[5];
+  uint32_t last_kind = 0;
+  upd::launches(count, upd::kStepPiece, 1u << 21, [&](int i) { return t[i].n; },
                 [&](int j, int i, int64_t begin, int64_t n, uint32_t first) {
+                  if (j == 0) groups = 0;
                   const bool half_g = t[i].g_dtype == LONGER_BF16, half_w = t[i].w && t[i].w_dtype == LONGER_BF16;
-                  a.p[j] = t[i].p + begin;
-                  a.m[j] = t[i].m + begin;
-                  a.v[j] = t[i].v + begin;
-                  a.g[j] = (const char*)t[i].g + begin * (half_g ? 2 : 4);
-                  a.w[j] = t[i].w ? (char*)t[i].w + begin * (half_w ? 2 : 4) : nullptr;
-                  a.n[j] = n | (half_g ? upd::kHalf : 0) | (half_w ? upd::kHalfW : 0);
-                  a.first[j] = first;
-                  a.decay[j] = (float)(how->lr * t[i].decay);
+                  const uint32_t kind = (half_g ? upd::kHalfG : 0) | (half_w ? upd::kHalfW : 0) | (t[i].w ? upd::kCopy : 0);
+                  const uint64_t at[5] = {(uint64_t)t[i].p, (uint64_t)t[i].m, (uint64_t)t[i].v, (uint64_t)t[i].g, (uint64_t)t[i].w};
+                  const int64_t size[5] = {4, 4, 4, half_g ? 2 : 4, half_w ? 2 : 4};
+                  int64_t place = groups ? ((int64_t)(at[0] - last[0])) / 4 : 0;
+                  bool joins = groups && kind == last_kind;
+                  for (int k = 0; joins && k < (t[i].w ? 5 : 4); ++k) joins = (int64_t)(at[k] - last[k]) == place * size[k];
+                  if (upd::kEntry * (j + 1) + upd::kBuffers * (groups + !joins) > upd::kStepWords || j == upd::kStepList) return false;
+                  if (!joins) {
+                    uint32_t* b = a.list + upd::kStepWords - upd::kBuffers * ++groups;
+                    for (int k = 0; k < 5; ++k) {
+                      last[k] = at[k];
+                      b[2 * k] = (uint32_t)at[k];
+                      b[2 * k + 1] = (uint32_t)(at[k] >> 32);
+                    }
+                    last_kind = kind;
+                    place = 0;
+                  }
+                  place += begin;
+                  const float decay = (float)(how->lr * t[i].decay);
+                  uint32_t* e = a.list + upd::kEntry * j;
+                  e[0] = (uint32_t)place;
+                  e[1] = (uint32_t)((uint64_t)place >> 32);
+                  e[2] = (uint32_t)n;
+                  e[3] = first;
+                  std::memcpy(e + 4, &decay, 4);
+                  e[5] = kind | (uint32_t)(groups - 1);
+                  return true;
                 },
                 [&](int entries, uint32_t k) {
                   a.count = entries;

@@ -198,6 +198,67 @@ def test_adamw(which, weights, grads, pad):
         assert int(torch.isnan(whole).sum()) == whole.numel() - t.numel()
 
 
+def test_tensors_of_common_buffers():
+    """Tensors at the same places of common buffers (in any order, types and gaps) share their addresses in a launch: the same bits as
+    with buffers of their own."""
+    r = np.random.default_rng(7)
+    sizes = [int(n) for n in np.concatenate([r.integers(1, 300, 420), r.integers(4000, 9000, 20)])]
+    r.shuffle(sizes)
+    gaps = r.integers(0, 5, len(sizes))
+    starts = np.cumsum(np.array(sizes) + gaps) - sizes
+    total = int(starts[-1] + sizes[-1] + 9)
+    flat = {k: torch.randn(total, device=DEV) * 0.1 for k in "pmv"}
+    flat["v"].square_()
+    g32, g16 = torch.randn(total, device=DEV), torch.randn(total, device=DEV).to(torch.bfloat16)
+    w16, w32 = torch.zeros(total, device=DEV, dtype=torch.bfloat16), torch.zeros(total, device=DEV)
+    cut = lambda f: [f[int(a):int(a) + n] for a, n in zip(starts, sizes)]
+    order = list(r.permutation(len(sizes)))
+    kind = r.integers(0, 40, len(sizes))                  # mostly float32 gradients and bfloat16 copies, now and then others
+    own = {k: [t.clone() for t in cut(flat[k])] for k in "pmv"}
+    lists = {k: cut(flat[k]) for k in "pmv"}
+    g = [cut(g16)[i] if kind[i] == 0 else cut(g32)[i] for i in range(len(sizes))]
+    w = [None if kind[i] == 1 else cut(w32)[i] if kind[i] == 2 else cut(w16)[i] for i in range(len(sizes))]
+    own_g, own_w = [t.clone() for t in g], [None if t is None else t.clone() for t in w]
+    decay = [0.01 * (i % 4) for i in range(len(sizes))]
+    pick = lambda ts: [ts[i] for i in order]
+    before = {k: flat[k].clone() for k in "pmv"}
+    for ls, gs, ws in ((lists, g, w), (own, own_g, own_w)):
+        params = lg.AdamWList(pick(ls["p"]), pick(ls["m"]), pick(ls["v"]), pick(gs), pick(ws), pick(decay))
+        lg.longer_adamw_step(params, None, 1e-2, 0.9, 0.99, 1e-8, 5)
+    torch.cuda.synchronize()
+    inside = torch.zeros(total, dtype=torch.bool, device=DEV)
+    for t in cut(inside):
+        t.fill_(True)
+    for k in "pmv":
+        assert torch.equal(flat[k][~inside], before[k][~inside]) and not torch.equal(flat[k], before[k])
+        assert all(torch.equal(a, b) for a, b in zip(lists[k], own[k]))
+    for a, b, m in zip(w, own_w, lists["p"]):
+        assert a is None or (torch.equal(a, b) and torch.equal(a, m.to(a.dtype)))
+
+
+def test_lists_check_their_tensors():
+    t = torch.zeros(6, device=DEV)
+    with pytest.raises(lg.LongerError):
+        lg.TensorList([t.to(torch.float16)])
+    with pytest.raises(lg.LongerError):
+        lg.TensorList([t[::2]])
+    with pytest.raises(lg.LongerError):
+        lg.TensorList([t, t.cpu()])
+    with pytest.raises(lg.LongerError):
+        lg.AdamWList([t], [t.clone()], [t.clone()], [t.clone()], [t[:5]], [0.0])
+    with pytest.raises(lg.LongerError):
+        lg.AdamWList([t], [t.clone()], [t.to(torch.bfloat16)], [t.clone()], None, [0.0])
+    with pytest.raises(lg.LongerError):
+        lg.AdamWList([t], [None], [t.clone()], [t.clone()], None, [0.0])
+    one = lg.TensorList([t])
+    with pytest.raises(lg.LongerError):
+        lg.longer_grad_norm(one, 1.0, torch.empty(1, device=DEV), torch.empty(256, dtype=torch.uint8, device=DEV))
+    with pytest.raises(lg.LongerError):
+        lg.longer_clip_gradients(one, torch.empty(2, device=DEV), lg.TensorList([t, t]))
+    with pytest.raises(lg.LongerError):
+        lg.longer_grad_norm(lg.TensorList([]), 1.0, torch.empty(2, device=DEV), torch.empty(256, dtype=torch.uint8, device=DEV))
+
+
 def test_step_on_another_stream_and_in_a_graph():
     sizes = SIZES["block"] * 6
     g, p, m, v = lists(["g", "p", "m", "v"], sizes, False, 0, seed=5, scale=0.1)
