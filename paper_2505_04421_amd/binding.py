@@ -219,25 +219,32 @@ class DeviceModel:
         self.device = torch.device(device)
         self.tdtype = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
         self._keep = []
-        self.inner = (CBlock * max(1, len(weights["inner"])))(*[self._block(b) for b in weights["inner"]])
-        self.cross = (CBlock * 1)(self._block(weights["cross"]))
-        self.self_ = (CBlock * max(1, len(weights["self"])))(*[self._block(b) for b in weights["self"]])
+        # the device tensors, in the order of longer_forward_backward's gradients and with the keys of model_grad_views
+        self.parameters = {"inner": [], "cross": None, "self": []}
+        self.inner = (CBlock * max(1, len(weights["inner"])))(*[self._block(b, self.parameters["inner"]) for b in weights["inner"]])
+        cross = []
+        self.cross = (CBlock * 1)(self._block(weights["cross"], cross))
+        self.parameters["cross"] = cross[0]
+        self.self_ = (CBlock * max(1, len(weights["self"])))(*[self._block(b, self.parameters["self"]) for b in weights["self"]])
         hw, hb = self.upload(weights["head_w"]), self.upload(weights["head_b"])
         self._keep += [hw, hb]
+        self.parameters.update(head_w=hw, head_b=hb)
         self.weights = CWeights(inner=self.inner, cross=self.cross, self=self.self_,
                                 head_w=hw.data_ptr(), head_b=hb.data_ptr())
         if getattr(cfg, "q_learnable", False):
             self.q_learn = self.upload(weights["q_learn"])
             self.ccfg.q_learn = self.q_learn.data_ptr()
+            self.parameters["q_learn"] = self.q_learn
 
     def upload(self, a):
         import torch
         import numpy as np
         return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(self.device).to(self.tdtype).contiguous()
 
-    def _block(self, blk) -> CBlock:
+    def _block(self, blk, into) -> CBlock:
         ts = {f: self.upload(blk[f]) for f in BLOCK_FIELDS}
         self._keep.append(ts)
+        into.append(ts)
         return CBlock(**{f: ts[f].data_ptr() for f in BLOCK_FIELDS})
 
     def empty(self, *shape, dtype=None):
