@@ -148,9 +148,14 @@ struct Walk {
     r = first;
     u = (unsigned)first / (unsigned)p.L;
     l = first - u * p.L;
+    n = p.L;
     ask(p);
   }
-  __device__ __forceinline__ void ask(const Params& p) { n = p.lens && r < p.rows ? p.lens[u] : p.L; }
+  // no kernel writes lengths: where a workgroup's lanes share the row it is a scalar load
+  __device__ __forceinline__ void ask(const Params& p) {
+    typedef const __attribute__((address_space(4))) int32_t* fixed;
+    if (p.lens) n = r < p.rows ? ((fixed)p.lens)[u] : 0;
+  }
   __device__ __forceinline__ bool valid(const Params& p) const { return r < p.rows && l < n; }
   __device__ __forceinline__ Walk next(const Params& p, int step) const {
     Walk w = *this;
@@ -170,6 +175,21 @@ __device__ __forceinline__ void load_row(Piece<T, V> (&x)[NV], const Rows& r, co
   for (int i = 0; i < NV; ++i) {
     x[i] = (Piece<T, V>)(T)0.f;
     if (ok && c.there(i)) x[i] = *(const Piece<T, V>*)(row + c.col[i]);
+  }
+}
+
+// Waits for a row that is under way.  In front of a turn's stores, which are under conditions: behind them the wait would be for the
+// stores as well, each turn.
+template <typename T, int V, int NV>
+__device__ __forceinline__ void landed(Piece<T, V> (&x)[NV]) {
+  if constexpr (sizeof(T) * V >= 16) {
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * V / 4)));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      words w = __builtin_bit_cast(words, x[i]);
+      asm volatile("" : "+v"(w) : : "memory");
+      x[i] = __builtin_bit_cast(Piece<T, V>, w);
+    }
   }
 }
 
@@ -204,11 +224,11 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
   load_row<T>(x, p.x, at, ok, c);
   Walk ahead = at.next(p, step);
   for (int first = LPR > 64 ? first_of_workgroup<LPR, THREADS>(p) : first_row; first < p.rows; first += step) {
-    // the next turn's rows are under way while this one's are worked on
+    // the next turn's rows, and the length for the one after it, are under way while this one's are worked on
+    const Walk ahead2 = ahead.next(p, step);
     const bool ok_ahead = ahead.valid(p);
     Piece<T, V> x_ahead[NV];
     load_row<T>(x_ahead, p.x, ahead, ok_ahead, c);
-    const Walk ahead2 = ahead.next(p, step);
     float y[NV][V];
     // (no row of the wave counts: nothing to do; rows of several waves meet at barriers, which their whole workgroup has to reach)
     if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : RPB > 1 || ok) {
@@ -303,6 +323,7 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
   load_row<U>(dy, p.dy, at, ok, c);
   Walk ahead = at.next(p, step);
   for (int first = LPR > 64 ? first_of_workgroup<LPR, THREADS>(p) : first_row; first < p.rows; first += step) {
+    const Walk ahead2 = ahead.next(p, step);
     const bool ok_ahead = ahead.valid(p);
     Piece<T, V> x_ahead[NV];
     Piece<U, V> dy_ahead[NV];
@@ -310,7 +331,6 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
       load_row<T>(x_ahead, p.x, ahead, ok_ahead, c);
       load_row<U>(dy_ahead, p.dy, ahead, ok_ahead, c);
     }
-    const Walk ahead2 = ahead.next(p, step);
     float xc[NV][V];
     if (LPR <= 64 ? __builtin_amdgcn_ballot_w64(ok) != 0 : RPB > 1 || ok) {
       constexpr int WAVE = LPR < 64 ? LPR : 64;
@@ -368,6 +388,10 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
           xc[i][j] = fmaf(rv, g[i][j], fmaf(k1, xc[i][j], k2));
         }
     }
+    if constexpr (AHEAD) {
+      landed<T, V>(x_ahead);
+      landed<U, V>(dy_ahead);
+    }
     if (at.r < p.rows) {
       U* row = (U*)p.out.data + at.u * p.out.user + at.l * p.out.row;
 #pragma unroll
@@ -386,6 +410,10 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
       load_row<T>(x, p.x, ahead, ok_ahead, c);
       load_row<U>(dy, p.dy, ahead, ok_ahead, c);
     }
+    // Rows of one wave, gradients in 32 bits: until the stores are done no wave asks for more, which the memory rewards (512000 rows
+    // of 128: 127 us for 131, of 77: 81 for 89; rows of several waves, which barriers hold together: 106 for 88, gradients in 16
+    // bits: 81 for 79).
+    if constexpr (LPR <= 64 && sizeof(U) == 4) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
     at = ahead;
     ok = ok_ahead;
     ahead = ahead2;
