@@ -326,9 +326,9 @@ int longer_input_generation_backward(const longer_config* cfg, const longer_inpu
  * inputs, no clipping and no optimizer: these calls are the usual ones, and take part in no call above).
  *
  * Layer norm of token rows: Y = (X - mean) / sqrt(var + eps) * ln_g + ln_b over the d values of each row, biased
- * variance, statistics in fp32 from the centred values.  In front of longer_forward_backward it normalises the
- * rows of the embeddings (H, G); on the first m rows of each user's Y_out it is the final norm that the pre-norm
- * stack does not have.
+ * variance, statistics in fp32 from the centred values (whose squares have to be fp32 numbers: below 1e19).  In
+ * front of longer_forward_backward it normalises the rows of the embeddings (H, G); on the first m rows of each
+ * user's Y_out it is the final norm that the pre-norm stack does not have.
  *
  * Rows of a [B, L, d] tensor that need not be dense: value c of row l of user b lies at
  * data + b user_stride + l row_stride + c, strides in elements, not negative, aligned to the element only.  An

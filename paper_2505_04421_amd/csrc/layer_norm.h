@@ -64,8 +64,13 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // is sum of (wave's q (x - m_w) + e_w wave's q), none of which cancels.  Two places in LDS in turn: a wave that writes one again has
 // passed the other's barrier, which every wave reaches after its reads.
 struct Shares { float s, squares, q, qx; };
+template <int LPR, int THREADS, bool SEVERAL = (LPR > 64)>
+struct Meeting {                    // (rows of one wave: nothing)
+  struct Memory {};
+  __device__ __forceinline__ Meeting(Memory&, int) {}
+};
 template <int LPR, int THREADS>
-struct Meeting {
+struct Meeting<LPR, THREADS, true> {
   static constexpr int W = THREADS / 64, S = LPR / 64;
   struct Memory { Shares at[2][W]; float n[W], inv_n[W]; };
   Memory& m;
@@ -204,11 +209,12 @@ __device__ __forceinline__ void load_vector(float (&v)[NV][V], const void* p, co
   }
 }
 
-// y = (x - mean) / sqrt(var + eps) g + b
+// y = (x - mean) / sqrt(var + eps) g + b.  Bound by memory: x once, y once, at the rate of a copy (512000 rows of 128 bf16: 49.6 us, 5.3
+// TB/s; 8000 of 8192: 50.5, 5.2; of 8191, whose every other row is off the words' alignment: 62, 4.2; 4503 of 4099 fp32: 31, 4.8).
 template <typename T, int V, int LPR, int NV, int MODE, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
   constexpr int RPB = THREADS / LPR;
-  typedef Meeting<(LPR > 64 ? LPR : 64), THREADS> Waves;
+  typedef Meeting<LPR, THREADS> Waves;
   __shared__ typename Waves::Memory lds;
   const Columns<V, LPR, NV, MODE> c(threadIdx.x % LPR, p.d);
   Waves waves(lds, c.owned());
@@ -247,7 +253,9 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
       // (a piece past the row holds zeros)
       if (MODE == VALUES && masked) sum(std::false_type()); else sum(std::true_type());
       s.s = lanes_sum<(LPR < 64 ? LPR : 64)>(s.s);
-      const float mean = s.s * (LPR > 64 ? waves.inv_n : p.inv_d);
+      float share = p.inv_d;
+      if constexpr (LPR > 64) share = waves.inv_n;
+      const float mean = s.s * share;              // the row's, or of several waves the wave's
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -295,13 +303,16 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
   }
 }
 
-// dx = r (q - mean(q) - xh mean(q xh)), q = dy g, and the workgroup's share of sum dy xh and sum dy.  Beside the centred squares a
+// dx = r (q - mean(q) - xh mean(q xh)), q = dy g, and the workgroup's share of sum dy xh and sum dy: x and dy are read once for both.
+// Bound by memory (512000 rows of 128, x bf16, gradients fp32: 125 us, 5.2 TB/s; 7161 of 8192: 112, 5.2; gradients bf16: 81, 4.3, where a
+// row's arithmetic no longer hides).  Workgroups stay for the whole launch, so the column sums leave the chip once for each: 16 waves
+// in one keep those few (256 pairs of rows at width 8192: 17 MB written and read).  Beside the centred squares a
 // row's sums of q and q (x - mean) are taken.
 template <typename T, typename U, int V, int LPR, int NV, int MODE>
 __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
   constexpr int THREADS = 1024, RPB = THREADS / LPR, GROUPS = LPR < 64 ? THREADS / 64 : RPB, WIDE = LPR * NV * V;
   constexpr bool AHEAD = NV * V <= 8;                    // room for the next turn's rows beside this one's (16 waves leave 128 registers each)
-  typedef Meeting<(LPR > 64 ? LPR : 64), THREADS> Waves;
+  typedef Meeting<LPR, THREADS> Waves;
   __shared__ typename Waves::Memory lds;
   __shared__ float sums[GROUPS > 1 ? GROUPS * WIDE : 1];
   const Columns<V, LPR, NV, MODE> c(threadIdx.x % LPR, p.d);
@@ -348,7 +359,9 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
       };
       if (MODE == VALUES && masked) sum(std::false_type()); else sum(std::true_type());
       s.s = lanes_sum<WAVE>(s.s);
-      const float mean = s.s * (LPR > 64 ? waves.inv_n : p.inv_d);
+      float share = p.inv_d;
+      if constexpr (LPR > 64) share = waves.inv_n;
+      const float mean = s.s * share;              // the row's, or of several waves the wave's
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -502,7 +515,7 @@ inline void launch_norm(Params& p, hipStream_t st) {
   const unsigned turns = ((unsigned)p.rows + RPB - 1) / RPB;
   unsigned grid = turns < most ? turns : most;
   // ragged users: shares of eight turns, dealt as workgroups end (512 users of up to 5000 rows of 128: 177 us for 197)
-  const bool dealt = p.lens && turns >= 32 * most;
+  const bool dealt = p.lens && turns >= 32 * most && p.rows < (1 << 30);      // (two steps past the last row stay below 2^31)
   if (dealt) grid = turns / 8;
   set_step(p, grid, RPB, p.lens && !dealt);
   norm_kernel<T, V, LPR, NV, MODE, THREADS><<<grid, THREADS, 0, st>>>(p);
@@ -550,6 +563,9 @@ inline unsigned launch_grad(Params& p, unsigned most, float* only, hipStream_t s
   const unsigned turns = ((unsigned)p.rows + 1024 / LPR - 1) / (1024 / LPR);
   unsigned grid = turns < held ? turns : held;
   if (grid > most) grid = most;
+  // (up to two turns one workgroup takes alone, and leaves the sums themselves: 256 rows of 64, 7.7 us a call for 10.9, 6.3 for 7.0 in
+  // a graph; of four turns 8.7 for 11.0, but 8.8 for 7.1)
+  if (turns <= 2) grid = 1;
   set_step(p, grid, 1024 / LPR, p.lens != nullptr);
   if (grid == 1) p.part = only;
   grad_kernel<T, U, V, LPR, NV, MODE><<<grid, 1024, 0, st>>>(p);

