@@ -48,7 +48,7 @@ constexpr int kNormList = 192, kClipList = 128;
 // Values of a piece.  An update has five streams to keep going and a clip two: with small pieces, in the list's order, what is under
 // way at one time is one stretch of each, in few memory pages (128 million parameters, an update in pieces of 1024 / 2048 / 4096 /
 // 8192 / 32768 values by 256 threads: 725 / 765 / 808 / 830 / 890 us; four values a thread in workgroups of 256 / 512 / 1024: 725 /
-// 720 / 711; 257 million values clipped in pieces of 1024 / 2048 / 4096 / 8192 / 65536: 364 / 362 / 390 / 420 / 420).  The norm's
+// 720 / 711; 260 million values clipped in pieces of 1024 / 2048 / 4096 / 8192 / 65536: 364 / 362 / 390 / 420 / 420).  The norm's
 // pieces, each of which leaves a sum to be joined, are as large as keeps every compute unit busy (at 2048 in all instead of 4096:
 // 180 us for 171).
 constexpr int kStepPiece = 4096, kClipPiece = 2048;
@@ -124,9 +124,10 @@ __device__ __forceinline__ double squares(const T* g, uint32_t n) {
   return s[0];
 }
 
-// Bound by memory: 257 million fp32 values in 171 us, 6.0 TB/s; 1.2 million in 98 tensors: 4.5 us, and 3 for the sums' join, launch and
+// Bound by memory: 260 million fp32 values in 171 to 177 us, 5.9 TB/s or more; 1.2 million in 98 tensors: 4.5 us, and 3 for the sums' join, launch and
 // latency.
-// (from the list's end to its start: what is read last is what a pass behind this one reads first, and may still be near)
+// (from the list's end to its start: what is read last is what a pass behind this one reads first, and may still be near: 128 million
+// parameters, norm and update 858 us for 929)
 __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
   __shared__ double lds[4];
   const uint32_t b = gridDim.x - 1 - blockIdx.x;
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double* part, uin
   norm[1] = !isfinite(v) ? 0.f : v <= max_norm ? 1.f : max_norm / v;
 }
 
-// Bound by memory: 257 million fp32 values in 358 us, 5.7 TB/s, two lines of 16 bytes a lane.
+// Bound by memory: 260 million fp32 values in 358 to 364 us, 5.7 TB/s, two lines of 16 bytes a lane.
 template <typename T>
 __device__ __forceinline__ void clip_piece(const T* in, T* out, uint32_t n, float c, bool finite) {
   constexpr uint32_t V = 16 / sizeof(T), U = kClipPiece / 256 / V;
@@ -186,9 +187,10 @@ __device__ __forceinline__ void step_value(const StepArgs& a, float decay, float
   p -= fmaf(decay, p, a.rate * (m / fmaf(sqrtf(v), a.root, a.eps)));
 }
 
-// Bound by memory: 128 million values in 698 us, 5.5 TB/s; the square root and the quotient are the exact ones, which hide behind the
-// loads.  Four values a lane.  Moments, parameters and their copy pass by once: nontemporal, they leave the last cache to the gradients that
-// the norm has just read, and to the next norm's (128 million parameters: norm 87 us for 150, both together 830 us for 915).
+// Bound by memory: 128 million values in 704 us, 5.4 TB/s; the square root and the quotient are the exact ones, which hide behind the
+// loads.  Four values a lane.  Moments, parameters and their copy pass by once: nontemporal, they leave the last cache to the
+// gradients that the norm has just read, and to the next norm's (128 million parameters in pieces of 2048: norm 87 us for 150, both
+// together 858 us for 916).
 template <typename G, typename W, bool COPY>
 __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, uint32_t n, float c, float decay) {
   const G* gs = (const G*)t.g;
