@@ -44,7 +44,7 @@ template <typename T> using Line = typename Line_<T>::type;
 template <typename T> struct Four_ { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
 template <typename T> using Four = typename Four_<T>::type;
 
-constexpr int kNormList = 192, kClipList = 128;
+constexpr int kNormList = 248, kClipList = 166;
 // Values of a piece.  An update has five streams to keep going and a clip two: with small pieces, in the list's order, what is under
 // way at one time is one stretch of each, in few memory pages (128 million parameters, an update in pieces of 1024 / 2048 / 4096 /
 // 8192 / 32768 values by 256 threads: 725 / 765 / 808 / 830 / 890 us; four values a thread in workgroups of 256 / 512 / 1024: 725 /
@@ -52,20 +52,20 @@ constexpr int kNormList = 192, kClipList = 128;
 // pieces, each of which leaves a sum to be joined, are as large as keeps every compute unit busy (at 2048 in all instead of 4096:
 // 180 us for 171).
 constexpr int kStepPiece = 4096, kClipPiece = 2048;
-constexpr int64_t kHalf = (int64_t)1 << 62;         // in a tensor's size: its values are bf16
-constexpr int64_t kCount = kHalf - 1;
+constexpr uint32_t kHalf = 1u << 31;                // in an entry's size: its values are bf16
 
 struct NormArgs {
   const void* data[kNormList];
-  int64_t n[kNormList];
+  uint32_t n[kNormList];
   uint32_t first[kNormList];
   int count;
+  uint32_t pieces;
   int64_t piece;
 };
 struct ClipArgs {
   const void* in[kClipList];
   void* out[kClipList];
-  int64_t n[kClipList];
+  uint32_t n[kClipList];
   uint32_t first[kClipList];
   const float* norm;
   int count;
@@ -130,9 +130,9 @@ __device__ __forceinline__ double squares(const T* g, uint32_t n) {
 // parameters, norm and update 858 us for 929)
 __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
   __shared__ double lds[4];
-  const uint32_t b = gridDim.x - 1 - blockIdx.x;
+  const uint32_t b = a.pieces - 1 - blockIdx.x;
   const Piece w = find_piece(a.first, a.count, b, a.piece);
-  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, a.piece);
+  const uint32_t n = (uint32_t)min((a.n[w.t] & ~kHalf) - w.begin, a.piece);
   double s = a.n[w.t] & kHalf ? squares((const __bf16*)a.data[w.t] + w.begin, n) : squares((const float*)a.data[w.t] + w.begin, n);
   s = block_sum<256>(s, lds);
   if (threadIdx.x == 0) part[b] = s;
@@ -141,7 +141,12 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
 __global__ __launch_bounds__(1024) void norm_join_kernel(const double* part, uint32_t n, float max_norm, float* norm) {
   __shared__ double lds[16];
   double s = 0.;
-  for (uint32_t i = threadIdx.x; i < n; i += 1024) s += part[i];
+  for (uint32_t i = threadIdx.x; i < n; i += 4096) {          // (four at a time: a list's 4096 sums in one trip to memory)
+    double v[4];
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) v[k] = i + 1024 * k < n ? part[i + 1024 * k] : 0.;
+    s += (v[0] + v[1]) + (v[2] + v[3]);
+  }
   s = block_sum<1024>(s, lds);
   if (threadIdx.x) return;
   const float v = (float)sqrt(s);
@@ -173,7 +178,7 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
   const float c = a.norm[1];
   const bool finite = isfinite(a.norm[0]);
   if (c == 1.f && a.in[w.t] == a.out[w.t]) return;
-  const uint32_t n = (uint32_t)min((a.n[w.t] & kCount) - w.begin, (int64_t)kClipPiece);
+  const uint32_t n = (uint32_t)min((a.n[w.t] & ~kHalf) - w.begin, (int64_t)kClipPiece);
   if (a.n[w.t] & kHalf) clip_piece((const __bf16*)a.in[w.t] + w.begin, (__bf16*)a.out[w.t] + w.begin, n, c, finite);
   else clip_piece((const float*)a.in[w.t] + w.begin, (float*)a.out[w.t] + w.begin, n, c, finite);
 }
@@ -314,7 +319,7 @@ static void launches(int count, int64_t piece, uint32_t most_pieces, Size size, 
     uint32_t k = 0;
     while (i < count && k < most_pieces) {
       const int64_t left = size(i) - begin;
-      const int64_t room = std::min((most_pieces - k) * piece, std::max(piece, kMostEntry));
+      const int64_t room = std::min((most_pieces - k) * piece, kMostEntry);
       const int64_t n = std::min(left, room);
       if (n) {
         if (!add(entries, i, begin, n, k)) break;
@@ -361,12 +366,13 @@ int longer_grad_norm(const longer_tensor* grads, int count, float max_norm, floa
                   if (j == upd::kNormList) return false;
                   const bool half = grads[i].dtype == LONGER_BF16;
                   a.data[j] = (const char*)grads[i].data + begin * (half ? 2 : 4);
-                  a.n[j] = n | (half ? upd::kHalf : 0);
+                  a.n[j] = (uint32_t)n | (half ? upd::kHalf : 0);
                   a.first[j] = first;
                   return true;
                 },
                 [&](int entries, uint32_t k) {
                   a.count = entries;
+                  a.pieces = k;
                   upd::norm_kernel<<<k, 256, 0, st>>>(a, (double*)ws + done);
                   done += k;
                 });
@@ -392,7 +398,7 @@ int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, 
                   const bool half = grads[i].dtype == LONGER_BF16;
                   a.in[j] = (const char*)grads[i].data + begin * (half ? 2 : 4);
                   a.out[j] = (char*)(out ? out[i].data : grads[i].data) + begin * (half ? 2 : 4);
-                  a.n[j] = n | (half ? upd::kHalf : 0);
+                  a.n[j] = (uint32_t)n | (half ? upd::kHalf : 0);
                   a.first[j] = first;
                   return true;
                 },

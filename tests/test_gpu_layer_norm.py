@@ -249,6 +249,27 @@ def test_offsets_beyond_32_bits():
     ref.near(grads[0], ref.dg, ref.dg_tol, "ln_g's gradient")
 
 
+def test_more_than_2_to_the_30_rows():
+    """Rows of one value: y = ln_b and dx = 0 whatever x is; ln_b's gradient counts the rows that are there (dy = 1: shares below 2^24
+    are exact, and they meet in fewer than 128 additions, u of the total each)."""
+    B, L = 600, 2_000_000
+    r = torch.Generator(device=DEV).manual_seed(3)
+    lens = torch.randint(0, L + 1, (B,), generator=r, device=DEV, dtype=torch.int32)
+    there = (torch.arange(L, device=DEV) < lens[:, None])
+    x = torch.randn(B, L, 1, generator=r, device=DEV, dtype=torch.bfloat16)
+    g, b = torch.full((1,), 0.5, device=DEV, dtype=torch.bfloat16), torch.full((1,), 3.0, device=DEV, dtype=torch.bfloat16)
+    y = torch.full_like(x, 7.0)
+    for n in (None, lens):
+        print("  longer_layer_norm", B, L, 1, n is not None, flush=True)
+        lg.longer_layer_norm(x, g, b, n, EPS, y)
+        assert bool((y[..., 0] == (3.0 if n is None else torch.where(there, 3.0, 0.0))).all())
+    dy, grads = torch.ones(B, L, 1, device=DEV), torch.empty(2, 1, device=DEV)
+    lg.longer_layer_norm_backward(x, g, dy, lens, EPS, dy, grads, workspace(B, L, 1)[0])
+    assert not bool(dy.any()) and float(grads[0]) == 0.0
+    rows = int(lens.sum(dtype=torch.int64))
+    assert abs(float(grads[1]) - rows) <= 128 * U * rows
+
+
 def test_on_another_stream_and_in_a_graph():
     x, g, b, dy, lens = draw(40, 50, 128, "bf16", 10, True)
     want, dx, grads, ws = torch.empty_like(x), torch.empty_like(dy), torch.empty(2, 128, device=DEV), workspace(40, 50, 128)[0]
