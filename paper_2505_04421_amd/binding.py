@@ -518,14 +518,17 @@ def longer_input_generation_backward(ccfg, weights, E, tdiff, lens, B, L, d_e, d
 _TENSOR_DTYPES = {}
 
 
-def _tensor_dtype(t) -> int:
-    code = _TENSOR_DTYPES.get(t.dtype)
-    if code is None:
+def _tensor_dtypes():
+    if not _TENSOR_DTYPES:
         import torch
         _TENSOR_DTYPES.update({torch.float32: _DTYPE["f32"], torch.bfloat16: _DTYPE["bf16"]})
-        code = _TENSOR_DTYPES.get(t.dtype)
-        if code is None:
-            raise LongerError("tensors are float32 or bfloat16, not %s" % t.dtype)
+    return _TENSOR_DTYPES
+
+
+def _tensor_dtype(t) -> int:
+    code = _tensor_dtypes().get(t.dtype)
+    if code is None:
+        raise LongerError("tensors are float32 or bfloat16, not %s" % t.dtype)
     return code
 
 
@@ -584,10 +587,12 @@ def longer_layer_norm_backward(X, ln_g, dY, lens, eps, dX_out, grads_out, ws, st
 def _addresses(tensors, name):
     """Addresses, sizes and types of a list of tensors, a few passes over the list for long ones' sake."""
     import torch
-    if not all(t.is_cuda for t in tensors) or not all(map(torch.Tensor.is_contiguous, tensors)):
+    if not all([t.is_cuda for t in tensors]) or not all(map(torch.Tensor.is_contiguous, tensors)):
         raise LongerError("%s: tensors must be contiguous device tensors" % name)
-    return (list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors)),
-            [_tensor_dtype(t) for t in tensors])
+    dtypes, codes = [t.dtype for t in tensors], _tensor_dtypes()
+    if not set(dtypes) <= codes.keys():
+        raise LongerError("%s: tensors are float32 or bfloat16" % name)
+    return list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors)), [codes[t] for t in dtypes]
 
 
 def _filled(struct, count, /, **columns):
