@@ -524,14 +524,14 @@ template <typename T, int V, int LPR, int NV>
 inline void launch_norm(Params& p, int mode, hipStream_t st) {
   if (mode == FULL) launch_norm<T, V, LPR, NV, FULL>(p, st);
   else if (mode == PIECES) launch_norm<T, V, LPR, NV, PIECES>(p, st);
-  else if constexpr (V > 1) launch_norm<T, V, LPR, NV, VALUES>(p, st);
+  else launch_norm<T, V, LPR, NV, VALUES>(p, st);
 }
 
 // (four pieces a lane in one wave before a row takes several, which meet in LDS)
 template <typename T, int V>
 inline void norm(Params& p, hipStream_t st) {
   const Shape s = shape(p.d, V, 4);
-  if (s.v == 1) return launch_norm<T, 1, 8, 1>(p, s.mode, st);
+  if (s.v == 1) return launch_norm<T, 1, 8, 1, PIECES>(p, st);
   switch (s.lpr * 8 + s.nv) {
     case 1 * 8 + 1: return launch_norm<T, V, 1, 1>(p, s.mode, st);
     case 2 * 8 + 1: return launch_norm<T, V, 2, 1>(p, s.mode, st);
@@ -575,15 +575,14 @@ template <typename T, typename U, int V, int LPR, int NV>
 inline unsigned launch_grad(Params& p, int mode, unsigned most, float* only, hipStream_t st) {
   if (mode == FULL) return launch_grad<T, U, V, LPR, NV, FULL>(p, most, only, st);
   if (mode == PIECES) return launch_grad<T, U, V, LPR, NV, PIECES>(p, most, only, st);
-  if constexpr (V > 1) return launch_grad<T, U, V, LPR, NV, VALUES>(p, most, only, st);
-  return 0;
+  return launch_grad<T, U, V, LPR, NV, VALUES>(p, most, only, st);
 }
 
 // (up to 8 or 12 values a lane, beside their column sums and the next turn's; 16 only where a workgroup's lanes are too few)
 template <typename T, typename U, int V>
 inline unsigned grad(Params& p, unsigned most, float* only, hipStream_t st) {
   const Shape s = shape(p.d, V, V == 4 ? 3 : 1);
-  if (s.v == 1) return launch_grad<T, U, 1, 8, 1>(p, s.mode, most, only, st);
+  if (s.v == 1) return launch_grad<T, U, 1, 8, 1, PIECES>(p, most, only, st);
   switch (s.lpr * 8 + s.nv) {
     case 1 * 8 + 1: return launch_grad<T, U, V, 1, 1>(p, s.mode, most, only, st);
     case 2 * 8 + 1: return launch_grad<T, U, V, 2, 1>(p, s.mode, most, only, st);

@@ -28,7 +28,7 @@ __device__ __forceinline__ int find_piece(const uint32_t* first, int count, uint
 #pragma unroll
   for (int k = 0; k < N; k += 64) {
     const int i = k + lane;
-    n += __popcll(__ballot(i < count && first[(i < N ? i : 0) * STRIDE] <= b));
+    n += __popcll(__ballot(i < count && first[i * STRIDE] <= b));         // (count is at most N)
   }
   return n - 1;
 }
@@ -74,7 +74,7 @@ struct ClipArgs {
 // the buffers' addresses: a tensor is an entry of kEntry words from the front of the list (its place in values, 64 bits; its values; its first
 // piece; lr * decay; its buffers and types), the buffers are kBuffers words from the end: 155 tensors of common buffers to a launch,
 // or 58 with buffers of their own.
-constexpr int kStepWords = 940, kEntry = 6, kBuffers = 10, kStepList = 192;
+constexpr int kStepWords = 940, kEntry = 6, kBuffers = 10, kStepList = (kStepWords - kBuffers) / kEntry;
 constexpr uint32_t kHalfG = 1u << 16, kHalfW = 1u << 17, kCopy = 1u << 18, kGroup = 0xffff;
 struct StepArgs {
   uint32_t list[kStepWords];
@@ -456,7 +456,7 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
                   int64_t place = groups ? ((int64_t)(at[0] - last[0])) / 4 : 0;
                   bool joins = groups && kind == last_kind;
                   for (int k = 0; joins && k < (t[i].w ? 5 : 4); ++k) joins = (int64_t)(at[k] - last[k]) == place * size[k];
-                  if (upd::kEntry * (j + 1) + upd::kBuffers * (groups + !joins) > upd::kStepWords || j == upd::kStepList) return false;
+                  if (upd::kEntry * (j + 1) + upd::kBuffers * (groups + !joins) > upd::kStepWords) return false;
                   if (!joins) {
                     uint32_t* b = a.list + upd::kStepWords - upd::kBuffers * ++groups;
                     for (int k = 0; k < 5; ++k) {
