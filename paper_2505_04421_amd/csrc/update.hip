@@ -124,8 +124,8 @@ __device__ __forceinline__ double squares(const T* g, uint32_t n) {
   return s[0];
 }
 
-// Bound by memory: 260 million fp32 values in 171 to 177 us, 5.9 TB/s or more; 1.2 million in 98 tensors: 4.5 us, and 3 for the sums' join, launch and
-// latency.
+// Bound by memory: 260 million fp32 values in 171 to 177 us, 5.9 TB/s or more; 1.2 million in 98 tensors: 4.6 us, and 2 for the sums' join (of
+// 4096 sums 4.7).
 // (from the list's end to its start: what is read last is what a pass behind this one reads first, and may still be near: 128 million
 // parameters, norm and update 858 us for 929)
 __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double* part) {
