@@ -326,7 +326,8 @@ int longer_input_generation_backward(const longer_config* cfg, const longer_inpu
  * inputs, no clipping and no optimizer: these calls are the usual ones, and take part in no call above).
  *
  * Layer norm of token rows: Y = (X - mean) / sqrt(var + eps) * ln_g + ln_b over the d values of each row, biased
- * variance, statistics in fp32 from the centred values (whose squares have to be fp32 numbers: below 1e19).  In
+ * variance, statistics in fp32 from the centred values: right for rows whose values lie within 1e18 of the row's mean
+ * and whose sum is an fp32 number (beyond that the squares overflow, and 1 / sqrt comes out as 0).  In
  * front of longer_forward_backward it normalises the rows of the embeddings (H, G); on the first m rows of each
  * user's Y_out it is the final norm that the pre-norm stack does not have.
  *
@@ -344,7 +345,8 @@ int longer_layer_norm(const longer_rows* x, const void* ln_g, const void* ln_b, 
 
 /* Its backward pass: for q = dy ln_g, xh the normalised row and r = 1 / sqrt(var + eps),
  *   dx = r (q - mean(q) - xh mean(q xh)),   d ln_g = sum over rows of dy xh,   d ln_b = sum over rows of dy.
- * Nothing is kept from the forward call: statistics are formed again from x, which is read anyway.
+ * Nothing is kept from the forward call: statistics are formed again from x, which is read anyway.  Besides what the forward call asks
+ * of x, mean(q xh) / (var + eps) is formed in fp32 and should not fall below 1e-38 where it matters.
  * x and ln_g as in the forward call; dy and dx in fp32 (what longer_forward_backward writes to dH_out and dG_out)
  * or both in x's dtype; padding as above: neither x nor dy is read there, dx is zero.  dx may be dy itself.
  * grads_out fp32 [2][d]: ln_g's gradient, then ln_b's; overwritten, not accumulated into.  The sums over rows are

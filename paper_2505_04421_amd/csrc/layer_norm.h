@@ -2,7 +2,9 @@
 //
 // A row of d values is cut into pieces of V values, at most 16 bytes of the narrower type; LPR lanes hold it, NV pieces each (piece
 // lane + LPR i), so a wave holds 64 / LPR rows at once and a row wider than a wave's pieces has a workgroup's lanes.  The statistics
-// take two sums in lanes, the mean and then the centred squares: no cancellation, and the row is there already.
+// take two sums in lanes, the mean and then the centred squares: no cancellation, and the row is there already.  A lane divides its
+// at most 32 squares by d before lanes meet: at any width they leave fp32 only where single values do, not where d of them would (a
+// value within 1e18 of the row's mean is within 2e18 of its wave's: 32 * 4e36 < 3.4e38).
 //
 // Widths that no piece divides: the last piece is moved back to end with the row, so that every access is whole and inside it; its
 // first values (below `lo`) are also its neighbour's, take no part in sums, and are computed and stored twice, to the same bits.
@@ -61,7 +63,7 @@ __device__ __forceinline__ float lanes_sum(float v) {
 
 // Rows of several waves.  Each wave centres its values on its own mean; then one barrier a row brings the waves' sums together:
 // with n_w values, mean m_w and e_w = m_w - mean, the row's centred squares are sum of (wave's + n_w e_w^2), its sum of q (x - mean)
-// is sum of (wave's q (x - m_w) + e_w wave's q), none of which cancels.  Two places in LDS in turn: a wave that writes one again has
+// is sum of (wave's q (x - m_w) + e_w wave's q), none of which cancels.  Squares are divided by d before they meet.  Two places in LDS in turn: a wave that writes one again has
 // passed the other's barrier, which every wave reaches after its reads.
 struct Shares { float s, squares, q, qx; };
 template <int LPR, int THREADS, bool SEVERAL = (LPR > 64)>
@@ -90,7 +92,7 @@ struct Meeting<LPR, THREADS, true> {
     Shares o = m.at[turn][other];
     turn ^= 1;
     const float mean = lanes_sum<S>(o.s) * inv_d, e = o.s * m.inv_n[other] - mean;
-    v.squares = lanes_sum<S>(fmaf(m.n[other] * e, e, o.squares));
+    v.squares = lanes_sum<S>(fmaf(m.n[other] * inv_d * e, e, o.squares));
     v.q = lanes_sum<S>(o.q);
     v.qx = lanes_sum<S>(fmaf(e, o.q, o.qx));
     return mean;
@@ -270,7 +272,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
           }
       };
       if (masked) squares(std::false_type()); else squares(std::true_type());
-      s.squares = lanes_sum<(LPR < 64 ? LPR : 64)>(s.squares);
+      s.squares = lanes_sum<(LPR < 64 ? LPR : 64)>(s.squares * p.inv_d);
       if constexpr (LPR > 64) {
         const float row_mean = waves.join(s, p.inv_d);
 #pragma unroll
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
 #pragma unroll
           for (int j = 0; j < V; ++j) y[i][j] = (float)x[i][j] - row_mean;
       }
-      const float r = __builtin_amdgcn_rsqf(fmaf(s.squares, p.inv_d, p.eps));
+      const float r = __builtin_amdgcn_rsqf(s.squares + p.eps);
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -379,7 +381,7 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
           }
       };
       if (masked) sums(std::false_type()); else sums(std::true_type());
-      s.squares = lanes_sum<WAVE>(s.squares);
+      s.squares = lanes_sum<WAVE>(s.squares * p.inv_d);
       s.q = lanes_sum<WAVE>(s.q);
       s.qx = lanes_sum<WAVE>(s.qx);
       if constexpr (LPR > 64) {
@@ -389,7 +391,7 @@ __global__ __launch_bounds__(1024) void grad_kernel(Params p) {
 #pragma unroll
           for (int j = 0; j < V; ++j) xc[i][j] = (float)x[i][j] - row_mean;
       }
-      const float r = __builtin_amdgcn_rsqf(fmaf(s.squares, p.inv_d, p.eps));
+      const float r = __builtin_amdgcn_rsqf(s.squares + p.eps);
       const float k1 = -(s.qx * p.inv_d) * r * r * r, k2 = -(s.q * p.inv_d) * r;       // dx = r q + k1 (x - mean) + k2
 #pragma unroll
       for (int i = 0; i < NV; ++i)
