@@ -386,7 +386,8 @@ typedef struct { double lr, beta1, beta2, eps; int64_t step; } longer_adamw;   /
  *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
  *   p <- p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + decay p)        w <- p rounded to w_dtype
  * Clipping is the factor alone: no pass of its own over the gradients, which stay as they are.  A norm that is not
- * finite leaves p, m, v and w as they were (the batch is dropped).  lr >= 0, 0 <= beta1, beta2 < 1, eps > 0. */
+ * finite leaves p, m, v and w as they were (the batch is dropped).  lr >= 0, 0 <= beta1, beta2 < 1, eps a positive normal
+ * fp32 number; lr / (1 - beta1^step) and lr decay are fp32 numbers. */
 int longer_adamw_step(const longer_adamw_tensor* tensors, int count, const longer_adamw* how, const float* norm, void* stream);
 
 /* Measurement aid: when enabled, every kernel launch group of the entry points is bracketed

@@ -4,6 +4,7 @@
 #include "device.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -414,8 +415,10 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
   if (!how) return api_error(LONGER_ERR_ARG, "how is NULL");
   if (!(how->lr >= 0.) || !std::isfinite(how->lr)) return api_error(LONGER_ERR_ARG, "lr=%g: not negative, finite", how->lr);
   if (!(how->beta1 >= 0. && how->beta1 < 1.) || !(how->beta2 >= 0. && how->beta2 < 1.)) return api_error(LONGER_ERR_ARG, "beta1=%g beta2=%g: 0 to below 1", how->beta1, how->beta2);
-  if (!(how->eps > 0.) || !std::isfinite(how->eps)) return api_error(LONGER_ERR_ARG, "eps=%g must be positive", how->eps);
+  if (!(how->eps >= FLT_MIN && how->eps <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "eps=%g must be positive (a normal fp32 number)", how->eps);
   if (how->step < 1) return api_error(LONGER_ERR_ARG, "step=%lld: counts from 1", (long long)how->step);
+  const double rate = how->lr / (1. - std::pow(how->beta1, (double)how->step));
+  if (!(rate <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "lr=%g: lr / (1 - beta1^step) is beyond fp32", how->lr);
   if ((uintptr_t)norm & 3) return api_error(LONGER_ERR_ARG, "norm is not aligned");
   int64_t values = 0;
   for (int i = 0; i < count; ++i) {
@@ -425,7 +428,7 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
     if (!rc) rc = upd::check_tensor(t[i].g, t[i].n, t[i].g_dtype, i, "g");
     if (!rc && t[i].w) rc = upd::check_tensor(t[i].w, t[i].n, t[i].w_dtype, i, "w");
     if (rc) return rc;
-    if (!(t[i].decay >= 0.) || !std::isfinite(t[i].decay)) return api_error(LONGER_ERR_ARG, "tensor %d: decay=%g: not negative, finite", i, t[i].decay);
+    if (!(t[i].decay >= 0.) || !(how->lr * t[i].decay <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "tensor %d: decay=%g: not negative, lr decay an fp32 number", i, t[i].decay);
     const void* at[5] = {t[i].p, t[i].m, t[i].v, t[i].g, t[i].w};
     for (int j = 0; j < 5; ++j)
       for (int k = 0; k < j; ++k)
@@ -440,7 +443,7 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
   a.one_beta1 = (float)(1. - how->beta1);
   a.beta2 = (float)how->beta2;
   a.one_beta2 = (float)(1. - how->beta2);
-  a.rate = (float)(how->lr / (1. - std::pow(how->beta1, (double)how->step)));
+  a.rate = (float)rate;
   a.root = (float)(1. / std::sqrt(1. - std::pow(how->beta2, (double)how->step)));
   a.eps = (float)how->eps;
   int groups = 0;                                     // of the launch at hand, and the last one's buffers, where place 0 would be
