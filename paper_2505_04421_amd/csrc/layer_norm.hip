@@ -98,7 +98,7 @@ int longer_layer_norm(const longer_rows* x, const void* ln_g, const void* ln_b, 
   if (!rc) rc = ln::check_vector(ln_b, x->dtype, "ln_b");
   if (!rc && x->dtype != y->dtype) rc = api_error(LONGER_ERR_ARG, "x and y have one dtype");
   if (!rc) rc = ln::check_alias(x, y, "x and y", B, L);
-  if (!rc && !(eps >= FLT_MIN)) rc = api_error(LONGER_ERR_ARG, "eps must be positive (a normal number)");
+  if (!rc && !(eps >= FLT_MIN && eps <= FLT_MAX)) rc = api_error(LONGER_ERR_ARG, "eps must be positive (a normal number)");
   if (!rc && ((uintptr_t)lens & 3)) rc = api_error(LONGER_ERR_ARG, "lens is not aligned");
   if (rc) return rc;
   ln::Params p = {ln::rows_of(x, B, L), {}, ln::rows_of(y, B, L), ln_g, ln_b, lens, B * L, L, d, 0, 0, 0, eps, 1.f / d, nullptr};
@@ -124,7 +124,7 @@ int longer_layer_norm_backward(const longer_rows* x, const void* ln_g, const lon
     rc = api_error(LONGER_ERR_ARG, "dy and dx are both fp32 or both of x's dtype");
   if (!rc) rc = ln::check_alias(dy, dx, "dy and dx", B, L);
   if (!rc && x->data == dx->data) rc = api_error(LONGER_ERR_ARG, "dx may not be x");
-  if (!rc && !(eps >= FLT_MIN)) rc = api_error(LONGER_ERR_ARG, "eps must be positive (a normal number)");
+  if (!rc && !(eps >= FLT_MIN && eps <= FLT_MAX)) rc = api_error(LONGER_ERR_ARG, "eps must be positive (a normal number)");
   if (!rc && ((uintptr_t)lens & 3)) rc = api_error(LONGER_ERR_ARG, "lens is not aligned");
   if (!rc && (!ws || ((uintptr_t)ws & 255))) rc = api_error(LONGER_ERR_ARG, "ws must be 256-byte aligned and not NULL");
   if (rc) return rc;

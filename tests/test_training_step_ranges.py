@@ -2,7 +2,7 @@
 dereferenced): the kernels work with them in fp32, where they would be 0 or an infinity and make every value NaN."""
 import pytest
 
-from test_training_step_abi import adamw, refused
+from test_training_step_abi import adamw, back, norm, refused
 
 
 @pytest.mark.parametrize("kw,word", [
@@ -11,3 +11,9 @@ from test_training_step_abi import adamw, refused
     (dict(lr=1e20, decay=1e20), "decay"), (dict(decay=1e300), "decay")])
 def test_adamw_scalars_beyond_fp32(kw, word):
     refused(adamw(**kw), word)
+
+
+@pytest.mark.parametrize("call", [norm, back])
+@pytest.mark.parametrize("eps", [float("inf"), 1e39])
+def test_layer_norm_eps_beyond_fp32(call, eps):
+    refused(call(eps=eps), "eps")
