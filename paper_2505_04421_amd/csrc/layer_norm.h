@@ -477,7 +477,7 @@ struct Shape { int lpr, nv, mode, v; };
 
 // Lanes and pieces of a row, for pieces of `v` values: up to `most` pieces a lane, as few places for pieces as hold the row; at equal
 // count as few lanes.  A row wider than 1024 lanes hold that way has as many a lane as it needs.
-inline Shape shape(int d, int v, int most) {
+constexpr Shape shape(int d, int v, int most) {
   if (d < v) return {8, 1, PIECES, 1};
   const int pieces = (d + v - 1) / v;
   Shape s = {1, 1, 0, v};
@@ -492,6 +492,20 @@ inline Shape shape(int d, int v, int most) {
   }
   s.mode = d % v ? VALUES : pieces == s.lpr * s.nv ? FULL : PIECES;
   return s;
+}
+
+// pieces a lane: in the forward pass four in one wave before a row takes several, which meet in LDS; in the backward pass 8 or 12 values,
+// beside their column sums and the next turn's, more only where a workgroup's lanes are too few
+constexpr int most_pieces(int v, bool backward) { return !backward ? 4 : v == 4 ? 3 : 1; }
+
+// whether some width has this shape: every launch below asserts it, so that nothing is built that no call reaches
+constexpr bool reached(int v, bool backward, int lpr, int nv, int mode, int per_piece) {
+  for (int pieces = lpr * nv; pieces > 0; --pieces)
+    for (int d = pieces * v; d > 0 && d >= pieces * v - 1; --d) {
+      const Shape s = shape(d, v, most_pieces(v, backward));
+      if (d <= LONGER_MAX_NORM_WIDTH && s.lpr == lpr && s.nv == nv && s.mode == mode && s.v == per_piece) return true;
+    }
+  return false;
 }
 
 // Workgroups of a launch: as many as the card holds at once, each with its share of the turns (a few more than it holds would take
@@ -512,6 +526,7 @@ inline void set_step(Params& p, unsigned grid, int rows_per_turn, bool spread) {
 
 template <typename T, int V, int LPR, int NV, int MODE>
 inline void launch_norm(Params& p, hipStream_t st) {
+  static_assert(reached(16 / sizeof(T), false, LPR, NV, MODE, V), "no width takes this kernel");
   constexpr int THREADS = LPR > 256 ? LPR : 256, RPB = THREADS / LPR;
   static const unsigned most = resident(norm_kernel<T, V, LPR, NV, MODE, THREADS>, THREADS);
   const unsigned turns = ((unsigned)p.rows + RPB - 1) / RPB;
@@ -524,15 +539,15 @@ inline void launch_norm(Params& p, hipStream_t st) {
 }
 template <typename T, int V, int LPR, int NV>
 inline void launch_norm(Params& p, int mode, hipStream_t st) {
-  if (mode == FULL) launch_norm<T, V, LPR, NV, FULL>(p, st);
-  else if (mode == PIECES) launch_norm<T, V, LPR, NV, PIECES>(p, st);
-  else launch_norm<T, V, LPR, NV, VALUES>(p, st);
+  // (with one lane or two every lane has its piece, and one lane's is whole)
+  if constexpr (LPR > 2) if (mode == PIECES) return launch_norm<T, V, LPR, NV, PIECES>(p, st);
+  if constexpr (LPR > 1) if (mode == VALUES) return launch_norm<T, V, LPR, NV, VALUES>(p, st);
+  launch_norm<T, V, LPR, NV, FULL>(p, st);
 }
 
-// (four pieces a lane in one wave before a row takes several, which meet in LDS)
 template <typename T, int V>
 inline void norm(Params& p, hipStream_t st) {
-  const Shape s = shape(p.d, V, 4);
+  const Shape s = shape(p.d, V, most_pieces(V, false));
   if (s.v == 1) return launch_norm<T, 1, 8, 1, PIECES>(p, st);
   switch (s.lpr * 8 + s.nv) {
     case 1 * 8 + 1: return launch_norm<T, V, 1, 1>(p, s.mode, st);
@@ -561,6 +576,7 @@ inline void norm(Params& p, hipStream_t st) {
 // The backward launch; the workgroups that it takes (at most `most`), each of which leaves its column sums.
 template <typename T, typename U, int V, int LPR, int NV, int MODE>
 inline unsigned launch_grad(Params& p, unsigned most, float* only, hipStream_t st) {
+  static_assert(reached(16 / sizeof(T), true, LPR, NV, MODE, V), "no width takes this kernel");
   static const unsigned held = resident(grad_kernel<T, U, V, LPR, NV, MODE>, 1024);
   const unsigned turns = ((unsigned)p.rows + 1024 / LPR - 1) / (1024 / LPR);
   unsigned grid = turns < held ? turns : held;
@@ -575,15 +591,14 @@ inline unsigned launch_grad(Params& p, unsigned most, float* only, hipStream_t s
 }
 template <typename T, typename U, int V, int LPR, int NV>
 inline unsigned launch_grad(Params& p, int mode, unsigned most, float* only, hipStream_t st) {
-  if (mode == FULL) return launch_grad<T, U, V, LPR, NV, FULL>(p, most, only, st);
-  if (mode == PIECES) return launch_grad<T, U, V, LPR, NV, PIECES>(p, most, only, st);
-  return launch_grad<T, U, V, LPR, NV, VALUES>(p, most, only, st);
+  if constexpr (LPR > 2) if (mode == PIECES) return launch_grad<T, U, V, LPR, NV, PIECES>(p, most, only, st);
+  if constexpr (LPR > 1) if (mode == VALUES) return launch_grad<T, U, V, LPR, NV, VALUES>(p, most, only, st);
+  return launch_grad<T, U, V, LPR, NV, FULL>(p, most, only, st);
 }
 
-// (up to 8 or 12 values a lane, beside their column sums and the next turn's; 16 only where a workgroup's lanes are too few)
 template <typename T, typename U, int V>
 inline unsigned grad(Params& p, unsigned most, float* only, hipStream_t st) {
-  const Shape s = shape(p.d, V, V == 4 ? 3 : 1);
+  const Shape s = shape(p.d, V, most_pieces(V, true));
   if (s.v == 1) return launch_grad<T, U, 1, 8, 1, PIECES>(p, most, only, st);
   switch (s.lpr * 8 + s.nv) {
     case 1 * 8 + 1: return launch_grad<T, U, V, 1, 1>(p, s.mode, most, only, st);
