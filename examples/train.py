@@ -38,7 +38,7 @@ class Trainer:
     """Model, tables, norms, optimizer state and scratch of a run; everything is allocated here."""
 
     def __init__(self, cfg, items, lr=2e-3, beta1=0.9, beta2=0.98, eps=1e-8, decay=0.01, max_norm=1.0, seed=0):
-        self.cfg, self.how, self.max_norm, self.steps = cfg, (lr, beta1, beta2, eps), max_norm, 0
+        self.cfg, self.how, self.max_norm, self.done = cfg, (lr, beta1, beta2, eps), max_norm, 0
         self.model = lg.DeviceModel(cfg, synth.draw_weights(cfg))
         dev = self.model.device
         B, L, d = cfg.B, cfg.L, cfg.d
@@ -82,6 +82,16 @@ class Trainer:
         self.H, self.G1 = self.model.empty(B, L, cfg.d_in), self.model.empty(1, cfg.m, d)
         f32 = lambda *shape: torch.empty(*shape, device=dev)
         self.dH, self.dG, self.loss, self.norm = f32(B, L, cfg.d_in), f32(B, cfg.m, d), f32(4), f32(2)
+        self.last_norm, self.last = torch.empty(2, pin_memory=True), None        # the last step's norm on the host, and when it is there
+
+    def updates(self):
+        """The updates so far, which the moments hold and the bias correction counts: every step but those that longer_adamw_step dropped
+        because the norm was not finite.  Waits for the last step only."""
+        if self.last is not None:
+            self.last.synchronize()
+            self.done += bool(torch.isfinite(self.last_norm[0]))
+            self.last = None
+        return self.done
 
     def step(self, ids, lens, labels):
         """One step on item ids [B, L] (int64), lengths [B] (int32 or None), labels [B]; the loss stays on the GPU."""
@@ -97,8 +107,11 @@ class Trainer:
         self.gv["globals"].copy_(dG[0])
         self.gv["items"].zero_().index_add_(0, ids.reshape(-1), self.dH.reshape(-1, cfg.d_in))
         lg.longer_grad_norm(self.grads, self.max_norm, self.norm, self.ws_n)
-        self.steps += 1
-        lg.longer_adamw_step(self.params, self.norm, *self.how, self.steps)
+        # (here the GPU has this step's passes to do while the host waits for the last step's end)
+        lg.longer_adamw_step(self.params, self.norm, *self.how, self.updates() + 1)
+        self.last_norm.copy_(self.norm, non_blocking=True)
+        self.last = torch.cuda.Event()
+        self.last.record()
 
 
 def batch(cfg, items, seed, device):

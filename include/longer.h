@@ -380,13 +380,14 @@ int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, 
  * in the model's type that the kernels read (fp32 or bf16), or NULL.  n values each; decay = weight decay of this
  * tensor (0 for biases and norms).  The five do not overlap, nor do two tensors of a list. */
 typedef struct { float *p, *m, *v; const void* g; void* w; int64_t n; int32_t g_dtype, w_dtype; double decay; } longer_adamw_tensor;
-typedef struct { double lr, beta1, beta2, eps; int64_t step; } longer_adamw;   /* step counts from 1 */
+typedef struct { double lr, beta1, beta2, eps; int64_t step; } longer_adamw;   /* step: this update's number, from 1 */
 
 /* With g' = norm[1] g (norm NULL: g' = g), for every value of every tensor, in fp32:
  *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
  *   p <- p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + decay p)        w <- p rounded to w_dtype
  * Clipping is the factor alone: no pass of its own over the gradients, which stay as they are.  A norm that is not
- * finite leaves p, m, v and w as they were (the batch is dropped).  lr >= 0, 0 <= beta1, beta2 < 1, eps a positive normal
+ * finite leaves p, m, v and w as they were: the batch is dropped, and as the moments hold nothing of it, it does not
+ * count in `step`; norm[0] tells the caller.  lr >= 0, 0 <= beta1, beta2 < 1, eps a positive normal
  * fp32 number; lr / (1 - beta1^step) and lr decay are fp32 numbers. */
 int longer_adamw_step(const longer_adamw_tensor* tensors, int count, const longer_adamw* how, const float* norm, void* stream);
 

@@ -681,7 +681,8 @@ def longer_clip_gradients(grads: TensorList, norm, out: Optional[TensorList] = N
 
 
 def longer_adamw_step(params: AdamWList, norm, lr, beta1, beta2, eps, step, stream=None):
-    """One AdamW update of every parameter of the list, its gradient scaled by the factor in norm (None: by 1)."""
+    """One AdamW update of every parameter of the list, its gradient scaled by the factor in norm (None: by 1).  step: its number,
+    from 1; where norm is not finite nothing changes, and the batch does not count."""
     import torch
     _require_gpu()
     how = CAdamW(lr, beta1, beta2, eps, step)
