@@ -187,8 +187,9 @@ def _ptr(t) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     import torch
-    if stream is None:           # (the handle itself: a Stream object costs as much time as a launch)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+    if stream is None:           # (the handle itself where torch gives it, no public name: a Stream object costs as much time as a launch)
+        handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return (handle(torch.cuda.current_device()) if handle else torch.cuda.current_stream().cuda_stream) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
