@@ -391,8 +391,8 @@ typedef struct { double lr, beta1, beta2, eps; int64_t step; } longer_adamw;   /
  * fp32 number; lr / (1 - beta1^step) and lr decay are fp32 numbers. */
 int longer_adamw_step(const longer_adamw_tensor* tensors, int count, const longer_adamw* how, const float* norm, void* stream);
 
-/* Measurement aid: when enabled, every kernel launch group of the entry points is bracketed
- * by a pair of HIP events recorded on the caller's stream (at most 4096 pairs between two
+/* Measurement aid: when enabled, every kernel launch group of the forward pass' and serving's entry points (the five stages below;
+ * gradients and the operators of the training step have launches that are none of them and go untimed) is bracketed by a pair of HIP events recorded on the caller's stream (at most 4096 pairs between two
  * reads; later launches go unrecorded).  enable = 0: off; 1: every stage; any other value:
  * bit (s + 1) selects stage s (an event pair costs a few microseconds of launch time, so a
  * caller that wants one kernel's duration inside a timed loop selects that stage alone).  longer_stage_timing_read waits for the recorded
