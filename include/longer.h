@@ -329,7 +329,8 @@ int longer_input_generation_backward(const longer_config* cfg, const longer_inpu
  * variance, statistics in fp32 from the centred values: right for rows whose values lie within 1e18 of the row's mean
  * and whose sum is an fp32 number (beyond that the squares overflow, and 1 / sqrt comes out as 0).  In
  * front of longer_forward_backward it normalises the rows of the embeddings (H, G); on the first m rows of each
- * user's Y_out it is the final norm that the pre-norm stack does not have.
+ * user's Y_out it is the final norm that the pre-norm stack does not have, for a head of the caller's (the model's own
+ * head and loss, inside longer_forward and longer_forward_backward, take the rows as they are).
  *
  * Rows of a [B, L, d] tensor that need not be dense: value c of row l of user b lies at
  * data + b user_stride + l row_stride + c, strides in elements, not negative, aligned to the element only.  An
@@ -387,12 +388,14 @@ typedef struct { double lr, beta1, beta2, eps; int64_t step; } longer_adamw;   /
  *   p <- p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + decay p)        w <- p rounded to w_dtype
  * Clipping is the factor alone: no pass of its own over the gradients, which stay as they are.  A norm that is not
  * finite leaves p, m, v and w as they were: the batch is dropped, and as the moments hold nothing of it, it does not
- * count in `step`; norm[0] tells the caller.  lr >= 0, 0 <= beta1, beta2 < 1, eps a positive normal
- * fp32 number; lr / (1 - beta1^step) and lr decay are fp32 numbers. */
+ * count in `step`; norm[0] tells the caller.  *how goes into the launch by value: a captured graph repeats the rate and
+ * the step number that it was captured with, so the graph of a training step ends in front of this call.
+ * lr >= 0, 0 <= beta1, beta2 < 1, eps a positive normal fp32 number; lr / (1 - beta1^step) and lr decay are fp32 numbers. */
 int longer_adamw_step(const longer_adamw_tensor* tensors, int count, const longer_adamw* how, const float* norm, void* stream);
 
-/* Measurement aid: when enabled, every kernel launch group of the forward pass' and serving's entry points (the five stages below;
- * gradients and the operators of the training step have launches that are none of them and go untimed) is bracketed by a pair of HIP events recorded on the caller's stream (at most 4096 pairs between two
+/* Measurement aid: when enabled, every kernel launch group of the forward pass' and serving's entry points (the five
+ * stages below; gradients and the operators of the training step have launches that are none of them and go untimed)
+ * is bracketed by a pair of HIP events recorded on the caller's stream (at most 4096 pairs between two
  * reads; later launches go unrecorded).  enable = 0: off; 1: every stage; any other value:
  * bit (s + 1) selects stage s (an event pair costs a few microseconds of launch time, so a
  * caller that wants one kernel's duration inside a timed loop selects that stage alone).  longer_stage_timing_read waits for the recorded
