@@ -307,7 +307,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(Params p) {
 
 // dx = r (q - mean(q) - xh mean(q xh)), q = dy g, and the workgroup's share of sum dy xh and sum dy: x and dy are read once for both.
 // Bound by memory (512000 rows of 128, x bf16, gradients fp32: 125 us, 5.2 TB/s; 7161 of 8192: 112, 5.2; gradients bf16: 81, 4.3, where a
-// row's arithmetic no longer hides).  Workgroups stay for the whole launch, so the column sums leave the chip once for each: 16 waves
+// row's arithmetic no longer hides; widths of 16 values a lane: 5461 of 12288, gradients fp32, 138, 4.9; 4096 of 16383, 164, 4.1, one of
+// three kernels that spill, 3 to 9 registers a lane: bf16 rows off a piece past 8192, fp32 rows past 12288 but for 16384).  Workgroups stay for the whole launch, so the column sums leave the chip once for each: 16 waves
 // in one keep those few (256 pairs of rows at width 8192: 17 MB written and read).  Beside the centred squares a
 // row's sums of q and q (x - mean) are taken.
 template <typename T, typename U, int V, int LPR, int NV, int MODE>
@@ -494,7 +495,8 @@ constexpr Shape shape(int d, int v, int most) {
   return s;
 }
 
-// pieces a lane: in the forward pass four in one wave before a row takes several, which meet in LDS; in the backward pass 8 or 12 values,
+// pieces a lane: in the forward pass four in one wave before a row takes several, which meet in LDS (64 million bf16 values in rows of 2500: 53
+// us for 58 with up to two, 58 with one; of 520: 67, 66, 80; of 4096 or 8192 50, 50, 51); in the backward pass 8 or 12 values,
 // beside their column sums and the next turn's, more only where a workgroup's lanes are too few
 constexpr int most_pieces(int v, bool backward) { return !backward ? 4 : v == 4 ? 3 : 1; }
 
@@ -531,7 +533,9 @@ inline void launch_norm(Params& p, hipStream_t st) {
   static const unsigned most = resident(norm_kernel<T, V, LPR, NV, MODE, THREADS>, THREADS);
   const unsigned turns = ((unsigned)p.rows + RPB - 1) / RPB;
   unsigned grid = turns < most ? turns : most;
-  // ragged users: shares of eight turns, dealt as workgroups end (512 users of up to 5000 rows of 128: 177 us for 197)
+  // ragged users: shares of eight turns, dealt as workgroups end, where a workgroup has 32 turns or more (users of up to 5000 bf16 rows,
+  // 1.3 / 2.5 million of 128: 93 / 176 us for 99 / 190, 500000 of 512: 141 for 151, 5 million of 32: 90 for 94; from 8 turns on: 1
+  // million of 128 73 for 75, but 500000 of 128 40.5 for 39.5 and 1.3 million of 32 29 for 26)
   const bool dealt = p.lens && turns >= 32 * most && p.rows < (1 << 30);      // (two steps past the last row stay below 2^31)
   if (dealt) grid = turns / 8;
   set_step(p, grid, RPB, p.lens && !dealt);
@@ -581,8 +585,9 @@ inline unsigned launch_grad(Params& p, unsigned most, float* only, hipStream_t s
   const unsigned turns = ((unsigned)p.rows + 1024 / LPR - 1) / (1024 / LPR);
   unsigned grid = turns < held ? turns : held;
   if (grid > most) grid = most;
-  // (up to two turns one workgroup takes alone, and leaves the sums themselves: 256 rows of 64, 7.7 us a call for 10.9, 6.3 for 7.0 in
-  // a graph; of four turns 8.7 for 11.0, but 8.8 for 7.1)
+  // (up to two turns one workgroup takes alone, and leaves the sums themselves: two turns of rows of 32 to 8192 values, 7.6 to 8.0 us a
+  // call for 9.9 to 10.4, 4.3 to 6.5 for 5.2 to 7.5 in a graph; of four turns 7.7 to 9.4 for 10.2 to 10.6, but 6.5 to 9.4 for 5.2 to
+  // 7.6 in a graph)
   if (turns <= 2) grid = 1;
   set_step(p, grid, 1024 / LPR, p.lens != nullptr);
   if (grid == 1) p.part = only;

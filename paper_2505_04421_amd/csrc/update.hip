@@ -125,7 +125,7 @@ __device__ __forceinline__ double squares(const T* g, uint32_t n) {
   return s[0];
 }
 
-// Bound by memory: 260 million fp32 values in 171 to 177 us, 5.9 TB/s or more; 1.2 million in 98 tensors: 4.6 us, and 2 for the sums' join (of
+// Bound by memory: 260 million fp32 values in 171 to 177 us, 5.9 TB/s or more, 129 million bf16 values in 48, 5.4; 1.2 million in 98 tensors: 4.6 us, and 2 for the sums' join (of
 // 4096 sums 4.7).
 // (from the list's end to its start: what is read last is what a pass behind this one reads first, and may still be near: 128 million
 // parameters, norm and update 858 us for 929)
@@ -196,7 +196,7 @@ __device__ __forceinline__ void step_value(const StepArgs& a, float decay, float
 // Bound by memory: 128 million values in 704 us, 5.4 TB/s; the square root and the quotient are the exact ones, which hide behind the
 // loads.  Four values a lane.  Moments, parameters and their copy pass by once: nontemporal, they leave the last cache to the
 // gradients that the norm has just read, and to the next norm's (128 million parameters in pieces of 2048: norm 87 us for 150, both
-// together 858 us for 916).
+// together 858 us for 916; a reading of times, the traffic itself was not counted).
 template <typename G, typename W, bool COPY>
 __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, uint32_t n, float c, float decay) {
   const G* gs = (const G*)t.g;
