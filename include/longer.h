@@ -393,6 +393,75 @@ typedef struct { double lr, beta1, beta2, eps; int64_t step; } longer_adamw;   /
  * lr >= 0, 0 <= beta1, beta2 < 1, eps a positive normal fp32 number; lr / (1 - beta1^step) and lr decay are fp32 numbers. */
 int longer_adamw_step(const longer_adamw_tensor* tensors, int count, const longer_adamw* how, const float* norm, void* stream);
 
+/* ---- A table of embeddings in front of the model: from item ids to rows E (what longer_input_generation takes as E, or H and G_cand
+ * themselves), from dE back to the rows of the table that a batch names, and their update; dropout of rows.  (Section 3.3 and 3.5.1 begin
+ * with the embeddings; the paper names neither their scale nor dropout.)
+ *
+ * A dropout mask is never stored: it follows from a key, a site and a value's place.  key: device, [0] a seed, [1] the number
+ * of the step, both of 64 bits and read on the GPU, so that a captured step draws a new mask wherever the caller has counted the
+ * step number on.  Value c of row r = b L + l of a [B, L, d] call is kept where h >= t, t = round(65536 p), and then counts 65536 /
+ * (65536 - t) times (p is taken to the next multiple of 2^-16); h is half-word c mod 8 (0: the low half of word 0) of the four words that
+ * Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, 2011) makes of the counter
+ * (c div 8 + 65536 site, r, low word of the step, high word of the step) under the key (low word of the seed, high word).  site tells apart the places
+ * of one step where a mask is drawn.  0 <= p, t <= 65535; 0 <= site <= 65535.  A dropped value is an exact zero, also of an infinity or NaN. */
+typedef struct { double p; int32_t site; const uint64_t* key; } longer_dropout_mask;
+
+/* Y = residual + mask * X, padding rows exact zeros, not read.  residual may be NULL (Y = mask * X); x, residual and y of one
+ * dtype, in fp32 and rounded once; y may be x or residual itself, else it overlaps neither.  The backward pass is the same call on dY
+ * without a residual.  1 <= d <= LONGER_MAX_EMBEDDING_WIDTH, B L < 2^31 - 2^21. */
+#define LONGER_MAX_EMBEDDING_WIDTH 16384
+int longer_dropout(const longer_rows* x, const longer_rows* residual, const int32_t* lens, int B, int L, int d,
+                   const longer_dropout_mask* drop, const longer_rows* y, void* stream);
+
+/* A table of `rows` < 2^31 rows: value c of row i at data + i row_stride + c (elements; aligned to the element only).
+ * Ids of a [B, L] batch: that of place l of user b at data + b user_stride + l row_stride (elements), strides not negative: a view of
+ * a log's records, or one item for all (strides 0).  An id that is no row of the table (a missing item: -1) is nobody's: its token is
+ * treated as padding. */
+typedef struct { const void* data; int64_t rows, row_stride; int32_t dtype; } longer_table;
+enum { LONGER_I32 = 0, LONGER_I64 = 1 };
+typedef struct { const void* data; int64_t user_stride, row_stride; int32_t type; } longer_ids;
+
+/* E[b, l] = scale * mask * table[ids[b, l]], zeros where l >= lens[b] (ids there are not read) and where the id is no row.  table and e of any two
+ * dtypes; drop NULL: no mask; d as above.  Computed in fp32 (scale and the mask's factor as one fp32 number) and rounded once. */
+int longer_embedding(const longer_table* table, const longer_ids* ids, const int32_t* lens, int B, int L, int d, float scale,
+                     const longer_dropout_mask* drop, const longer_rows* e, void* stream);
+
+/* The tokens of a batch by item: what the gradient and the update of a table work from; it depends on the ids alone, so that it may run on another
+ * stream beside the model.  int32, device:
+ *   tokens [B L]              the valid tokens b L + l, by ascending id, those of one id by ascending number;
+ *   runs [B L]                for each of them, which distinct id it has: 0, 1, ...;
+ *   rows [min(B L, table_rows)]  the distinct ids, ascending;
+ *   counts [2]                how many distinct ids, how many valid tokens there are.
+ * What lies behind the counts is left as it was.
+ * ws: device, 256-byte aligned, at least longer_sort_ids_workspace_bytes(B, L, table_rows) bytes (0 = unsupported). */
+typedef struct { int32_t *tokens, *runs, *rows, *counts; } longer_order;
+size_t longer_sort_ids_workspace_bytes(int B, int L, int64_t table_rows);
+int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, int64_t table_rows,
+                    const longer_order* order, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of a table: G[i] = scale * sum of mask * dE[t] over the tokens t that name row i; order is that of the lookup's ids and lengths, scale and
+ * drop (the same key) are the lookup's.  de: fp32 or bf16, not read where a token names no row.  grads_out: fp32, dense rows of d values, overwritten,
+ * not accumulated into:
+ *   dense == 0: grads_out [out_rows][d] holds the rows that the batch names, row i that of order->rows[i]; rows behind the last
+ *     one stay as they were; out_rows >= min(B L, table_rows) (further ones are not written);
+ *   dense == 1: grads_out [out_rows][d] holds every row of the table, zeros where no token names it (ids from out_rows on are dropped).
+ * norms_out [out_rows] fp32, or NULL: the norm of each row of grads_out, zeros behind the last one: in a list of longer_grad_norm it
+ * stands for the table's gradient, of which nothing is read again.
+ * Sums in fp32 in a fixed order, the squares of a norm in 64 bits: the same call gives the same bits.
+ * ws: device, 256-byte aligned, at least longer_embedding_backward_workspace_bytes(B, L, d) bytes (0 = unsupported). */
+size_t longer_embedding_backward_workspace_bytes(int B, int L, int d);
+int longer_embedding_backward(const longer_order* order, const longer_rows* de, int B, int L, int d, float scale,
+                              const longer_dropout_mask* drop, int dense, int64_t out_rows, float* grads_out, float* norms_out,
+                              void* ws, size_t ws_bytes, void* stream);
+
+/* longer_adamw_step on the rows of a table that a batch names, and on no other: their moments, values and copy as that call's, bit for bit, with the
+ * gradients of longer_embedding_backward (dense == 0); the moments of the other rows do not decay, nor do their values (a row that is seldom named
+ * has its moments decayed once for each batch that names it).  p, m, v (fp32) and w (fp32 or bf16, or NULL): dense [rows][d]; g: fp32 [.][d], row i
+ * that of order->rows[i].  None of them overlap.  norm and how as in longer_adamw_step. */
+typedef struct { float *p, *m, *v; void* w; int64_t rows; int32_t d, w_dtype; double decay; } longer_adamw_table;
+int longer_adamw_rows(const longer_adamw_table* table, const longer_order* order, int B, int L, const float* g,
+                      const longer_adamw* how, const float* norm, void* stream);
+
 /* Measurement aid: when enabled, every kernel launch group of the forward pass' and serving's entry points (the five
  * stages below; gradients and the operators of the training step have launches that are none of them and go untimed)
  * is bracketed by a pair of HIP events recorded on the caller's stream (at most 4096 pairs between two

@@ -19,4 +19,6 @@ from .binding import (  # noqa: F401
     longer_input_backward_workspace_bytes, longer_input_grad_floats, longer_input_generation_backward, input_grad_views,
     longer_layer_norm, longer_layer_norm_backward_workspace_bytes, longer_layer_norm_backward,
     TensorList, AdamWList, longer_grad_norm_workspace_bytes, longer_grad_norm, longer_clip_gradients, longer_adamw_step,
+    DropoutMask, longer_dropout, longer_embedding, TokenOrder, longer_sort_ids_workspace_bytes, longer_sort_ids,
+    longer_embedding_backward_workspace_bytes, longer_embedding_backward, AdamWRows, longer_adamw_rows,
 )

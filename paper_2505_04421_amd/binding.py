@@ -21,7 +21,9 @@ ENTRY_POINTS = ("longer_workspace_bytes", "longer_kv_cache_bytes", "longer_inner
                 "longer_model_grad_floats", "longer_forward_backward_workspace_bytes", "longer_forward_backward",
                 "longer_input_backward_workspace_bytes", "longer_input_grad_floats", "longer_input_generation_backward",
                 "longer_layer_norm", "longer_layer_norm_backward_workspace_bytes", "longer_layer_norm_backward",
-                "longer_grad_norm_workspace_bytes", "longer_grad_norm", "longer_clip_gradients", "longer_adamw_step")
+                "longer_grad_norm_workspace_bytes", "longer_grad_norm", "longer_clip_gradients", "longer_adamw_step",
+                "longer_dropout", "longer_embedding", "longer_sort_ids_workspace_bytes", "longer_sort_ids",
+                "longer_embedding_backward_workspace_bytes", "longer_embedding_backward", "longer_adamw_rows")
 
 
 class LongerError(RuntimeError):
@@ -66,6 +68,27 @@ class CAdamWTensor(ctypes.Structure):
 
 class CAdamW(ctypes.Structure):
     _fields_ = [(f, ctypes.c_double) for f in ("lr", "beta1", "beta2", "eps")] + [("step", ctypes.c_int64)]
+
+
+class CDropoutMask(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("site", ctypes.c_int32), ("key", ctypes.c_void_p)]
+
+
+class CTable(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class CIds(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("user_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+class COrder(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("tokens", "runs", "rows", "counts")]
+
+
+class CAdamWTable(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in "pmvw"] + [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("w_dtype", ctypes.c_int32),
+                                                         ("decay", ctypes.c_double)]
 
 
 def library_path() -> str:
@@ -131,6 +154,16 @@ def load_library() -> ctypes.CDLL:
     lib.longer_grad_norm.argtypes = [ctypes.POINTER(CTensor), i32, ctypes.c_float, vp, vp, sz, vp]
     lib.longer_clip_gradients.argtypes = [ctypes.POINTER(CTensor), ctypes.POINTER(CTensor), i32, vp, vp]
     lib.longer_adamw_step.argtypes = [ctypes.POINTER(CAdamWTensor), i32, ctypes.POINTER(CAdamW), vp, vp]
+    maskp, idsp, orderp, i64 = ctypes.POINTER(CDropoutMask), ctypes.POINTER(CIds), ctypes.POINTER(COrder), ctypes.c_int64
+    lib.longer_dropout.argtypes = [rowsp, rowsp, vp, i32, i32, i32, maskp, rowsp, vp]
+    lib.longer_embedding.argtypes = [ctypes.POINTER(CTable), idsp, vp, i32, i32, i32, ctypes.c_float, maskp, rowsp, vp]
+    lib.longer_sort_ids_workspace_bytes.restype = sz
+    lib.longer_sort_ids_workspace_bytes.argtypes = [i32, i32, i64]
+    lib.longer_sort_ids.argtypes = [idsp, vp, i32, i32, i64, orderp, vp, sz, vp]
+    lib.longer_embedding_backward_workspace_bytes.restype = sz
+    lib.longer_embedding_backward_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.longer_embedding_backward.argtypes = [orderp, rowsp, i32, i32, i32, ctypes.c_float, maskp, i32, i64, vp, vp, vp, sz, vp]
+    lib.longer_adamw_rows.argtypes = [ctypes.POINTER(CAdamWTable), orderp, i32, i32, vp, ctypes.POINTER(CAdamW), vp, vp]
     lib.longer_last_error.restype = ctypes.c_char_p
     lib.longer_probe_mfma_layout.argtypes = [vp, vp]
     lib.longer_stage_timing.argtypes = [i32]
@@ -140,7 +173,8 @@ def load_library() -> ctypes.CDLL:
                         "longer_backward_workspace_bytes", "longer_block_grad_floats", "longer_model_grad_floats",
                         "longer_forward_backward_workspace_bytes", "longer_input_backward_workspace_bytes",
                         "longer_input_grad_floats", "longer_layer_norm_backward_workspace_bytes",
-                        "longer_grad_norm_workspace_bytes"):
+                        "longer_grad_norm_workspace_bytes", "longer_sort_ids_workspace_bytes",
+                        "longer_embedding_backward_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     _LIB = lib
     return lib
@@ -690,3 +724,171 @@ def longer_adamw_step(params: AdamWList, norm, lr, beta1, beta2, eps, step, stre
     _check(load_library().longer_adamw_step(params.array, len(params), ctypes.byref(how),
                                             None if norm is None else _vector(norm, 2, torch.float32, "norm"), _stream(stream)),
            "longer_adamw_step")
+
+
+# ----------------------------------------------------------------------------- a table of embeddings, and dropout
+class DropoutMask:
+    """What longer_dropout, longer_embedding and longer_embedding_backward draw their masks from: the share p of values that is dropped
+    (in steps of 2^-16), the device tensor key (int64 [2]: a seed and the step's number, read on the GPU; the caller counts the step
+    on), and the site, 0 to 65535, that tells apart the places of one step."""
+
+    def __init__(self, p, key, site=0):
+        import torch
+        if not isinstance(key, torch.Tensor) or key.dtype != torch.int64 or key.shape != (2,) or not key.is_contiguous() or not key.is_cuda:
+            raise LongerError("key must be a device tensor of two int64 values")
+        if not 0.0 <= p < 1.0 or round(65536 * p) > 65535:
+            raise LongerError("p=%g: 0 to below 1 - 2^-17" % p)
+        if not 0 <= site <= 65535:
+            raise LongerError("site=%d: 0 to 65535" % site)
+        self.p, self.key, self.site = p, key, site
+        self.struct = CDropoutMask(p, site, key.data_ptr())
+
+
+class TokenOrder:
+    """A batch's tokens by item, as longer_sort_ids leaves them: int32 device tensors tokens and runs [B L], rows [min(B L, table's rows)]
+    and counts [2] (distinct items, valid tokens); larger ones may be given."""
+
+    def __init__(self, tokens, runs, rows, counts):
+        import torch
+        for name, t in (("tokens", tokens), ("runs", runs), ("rows", rows), ("counts", counts)):
+            if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda:
+                raise LongerError("%s must be a contiguous device tensor of int32" % name)
+        if counts.numel() != 2 or runs.numel() != tokens.numel():
+            raise LongerError("counts must hold two values, and runs as many as tokens")
+        self.tokens, self.runs, self.rows, self.counts = tokens, runs, rows, counts
+        self.struct = COrder(tokens.data_ptr(), runs.data_ptr(), rows.data_ptr(), counts.data_ptr())
+
+    @classmethod
+    def empty(cls, B, L, table_rows, device="cuda:0"):
+        import torch
+        make = lambda n: torch.empty(n, dtype=torch.int32, device=device)
+        return cls(make(B * L), make(B * L), make(min(B * L, table_rows)), make(2))
+
+    def _holds(self, n, rows):
+        if self.tokens.numel() < n or self.rows.numel() < min(n, rows):
+            raise LongerError("the order holds %d tokens and %d rows, not %d and %d" % (self.tokens.numel(), self.rows.numel(), n, min(n, rows)))
+
+
+class AdamWRows:
+    """A table as longer_adamw_rows takes it: float32 master values p and moments m and v [rows, d], the copy w in the model's type (None:
+    there is none) and its weight decay."""
+
+    def __init__(self, p, m, v, w, decay):
+        import torch
+        self.tensors, self.decay = (p, m, v, w), decay
+        for name, t in zip("pmvw", self.tensors):
+            if t is None and name == "w":
+                continue
+            if p.dim() != 2 or t.shape != p.shape or not t.is_contiguous() or not t.is_cuda or (name != "w" and t.dtype != torch.float32):
+                raise LongerError("%s must be a contiguous device tensor like p [rows, d]%s" % (name, "" if name == "w" else " of float32"))
+        self.rows, self.d = p.shape
+        self.struct = CAdamWTable(p.data_ptr(), m.data_ptr(), v.data_ptr(), _ptr(w), self.rows, self.d, 0 if w is None else _tensor_dtype(w), decay)
+
+
+def _here(*tensors):
+    """Every tensor on the current device, the one whose stream the call goes to."""
+    import torch
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise LongerError("a tensor is not on the current device, cuda:%d" % device)
+
+
+_INT_TYPES = {}
+
+
+def _ids(ids, name="ids"):
+    if not _INT_TYPES:
+        import torch
+        _INT_TYPES.update({torch.int32: 0, torch.int64: 1})
+    if ids.dim() != 2 or ids.dtype not in _INT_TYPES or not ids.is_cuda:
+        raise LongerError("%s must be a device tensor [B, L] of int32 or int64" % name)
+    return CIds(ids.data_ptr(), ids.stride(0), ids.stride(1), _INT_TYPES[ids.dtype])
+
+
+def _mask(drop):
+    return None if drop is None else ctypes.byref(drop.struct)
+
+
+def longer_dropout(X, residual, lens, drop: DropoutMask, Y_out, stream=None):
+    """Y_out [B, L, d] (X itself, or residual, or a tensor that overlaps neither) = residual (None: nothing) + the mask's factors times X.
+    The backward pass is the same call on dY without a residual."""
+    _require_gpu()
+    if X.dim() != 3:
+        raise LongerError("X must be a device tensor [B, L, d]")
+    B, L, d = shape = X.shape
+    _here(X, residual, lens, drop.key, Y_out)
+    x, y = _rows(X, shape, "X"), _rows(Y_out, shape, "Y_out")
+    r = None if residual is None else ctypes.byref(_rows(residual, shape, "residual"))
+    _check(load_library().longer_dropout(ctypes.byref(x), r, _lens(lens, B), B, L, d, _mask(drop), ctypes.byref(y), _stream(stream)),
+           "longer_dropout")
+
+
+def longer_embedding(table, ids, lens, scale, drop: Optional[DropoutMask], E_out, stream=None):
+    """E_out [B, L, d] = scale times the mask's factors (drop None: 1) times the rows of table [rows, d] that ids [B, L] name; zeros behind
+    a user's length and where an id is no row of the table."""
+    _require_gpu()
+    if table.dim() != 2 or not table.is_cuda or (table.stride(1) != 1 and table.shape[1] > 1):
+        raise LongerError("table must be a device tensor [rows, d] whose rows have adjacent values")
+    i, (B, L), d = _ids(ids), ids.shape, table.shape[1]
+    _here(table, ids, lens, E_out, None if drop is None else drop.key)
+    t, e = CTable(table.data_ptr(), table.shape[0], table.stride(0), _tensor_dtype(table)), _rows(E_out, (B, L, d), "E_out")
+    _check(load_library().longer_embedding(ctypes.byref(t), ctypes.byref(i), _lens(lens, B), B, L, d, scale, _mask(drop), ctypes.byref(e),
+                                           _stream(stream)), "longer_embedding")
+
+
+def longer_sort_ids_workspace_bytes(B: int, L: int, table_rows: int) -> int:
+    return int(load_library().longer_sort_ids_workspace_bytes(B, L, table_rows))
+
+
+def longer_sort_ids(ids, lens, table_rows, order: TokenOrder, ws, stream=None):
+    """order = the tokens of ids [B, L] that name one of table_rows rows, by item."""
+    _require_gpu()
+    i, (B, L) = _ids(ids), ids.shape
+    _here(ids, lens, order.tokens, order.runs, order.rows, order.counts, ws)
+    order._holds(B * L, table_rows)
+    _check(load_library().longer_sort_ids(ctypes.byref(i), _lens(lens, B), B, L, table_rows, ctypes.byref(order.struct), _ptr(ws),
+                                          ws.numel() * ws.element_size(), _stream(stream)), "longer_sort_ids")
+
+
+def longer_embedding_backward_workspace_bytes(B: int, L: int, d: int) -> int:
+    return int(load_library().longer_embedding_backward_workspace_bytes(B, L, d))
+
+
+def longer_embedding_backward(order: TokenOrder, dE, scale, drop: Optional[DropoutMask], dense, grads_out, norms_out, ws, stream=None):
+    """Gradient of a table from dE [B, L, d] (scale and drop as in its lookup, order from its ids).  dense: grads_out float32 [rows, d] is that of
+    every row of the table; else its first order.counts[0] rows are those of order.rows, and it has min(B L, table's rows) rows or more.
+    norms_out: float32, the norm of each row of grads_out (None: not asked for)."""
+    import torch
+    _require_gpu()
+    if dE.dim() != 3:
+        raise LongerError("dE must be a device tensor [B, L, d]")
+    B, L, d = shape = dE.shape
+    de = _rows(dE, shape, "dE")
+    if grads_out.dim() != 2 or grads_out.shape[1] != d or grads_out.dtype != torch.float32:
+        raise LongerError("grads_out must be a float32 tensor [rows, %d]" % d)
+    _here(dE, grads_out, norms_out, ws, order.tokens, None if drop is None else drop.key)
+    order._holds(B * L, 0)
+    if not dense and grads_out.shape[0] < min(order.rows.numel(), B * L):
+        raise LongerError("grads_out must have a row for each of the order's %d" % min(order.rows.numel(), B * L))
+    norms = None if norms_out is None else _vector(norms_out, grads_out.shape[0], torch.float32, "norms_out")
+    _check(load_library().longer_embedding_backward(ctypes.byref(order.struct), ctypes.byref(de), B, L, d, scale, _mask(drop), int(bool(dense)),
+                                                    grads_out.shape[0], _ptr(grads_out), norms, _ptr(ws), ws.numel() * ws.element_size(),
+                                                    _stream(stream)), "longer_embedding_backward")
+
+
+def longer_adamw_rows(table: AdamWRows, order: TokenOrder, g, norm, lr, beta1, beta2, eps, step, stream=None):
+    """longer_adamw_step on the rows of a table that order names, and no other; g float32 [., d]: their gradients, as
+    longer_embedding_backward (not dense) leaves them."""
+    import torch
+    _require_gpu()
+    if g.dim() != 2 or g.shape[1] != table.d or g.dtype != torch.float32:
+        raise LongerError("g must be a float32 tensor [rows, %d]" % table.d)
+    _here(table.tensors[0], order.rows, g, norm)
+    most = min(order.rows.numel(), table.rows)
+    if g.shape[0] < most:
+        raise LongerError("g must have a row for each of the order's %d" % most)
+    how = CAdamW(lr, beta1, beta2, eps, step)
+    _check(load_library().longer_adamw_rows(ctypes.byref(table.struct), ctypes.byref(order.struct), 1, order.rows.numel(), _ptr(g), ctypes.byref(how),
+                                            None if norm is None else _vector(norm, 2, torch.float32, "norm"), _stream(stream)),
+           "longer_adamw_rows")

@@ -1,0 +1,209 @@
+// Rows of a table by item id, with scaling and dropout (longer_embedding), and dropout of token rows (longer_dropout).
+#include "embedding.h"
+
+namespace longer {
+namespace emb {
+
+struct Ids { const char* data; int64_t user, row; const int32_t* lens; uint32_t table_rows; int wide; };
+
+struct LookupParams {
+  const char* table;
+  int64_t stride;
+  Ids ids;
+  Rows out;
+  Divider by_L;
+  uint32_t n, L;
+  int d, shift;                     // 2^shift lanes hold a row
+  float factor;
+  Mask mask;
+};
+
+// the row of the table that token (b, l) names, or -1
+__device__ __forceinline__ int64_t item(const Ids& ids, uint32_t b, uint32_t l) {
+  if (ids.lens && (int)l >= ids.lens[b]) return -1;
+  const int64_t at = (int64_t)b * ids.user + (int64_t)l * ids.row;
+  const int64_t id = ids.wide ? ((const int64_t*)ids.data)[at] : ((const int32_t*)ids.data)[at];
+  return (uint64_t)id < ids.table_rows ? id : -1;
+}
+
+// E[r] = factor * mask * table[id of r], zeros where r is padding or names no row.
+template <typename T, typename O, bool DROP>
+__global__ __launch_bounds__(256) void lookup_kernel(LookupParams p) {
+  constexpr int U = 4;
+  const uint32_t lanes = 1u << p.shift, per_turn = 256 >> p.shift, per_group = per_turn * U;
+  const Key key = DROP ? load_key(p.mask) : Key{};
+  for (uint32_t first = blockIdx.x * per_group + (threadIdx.x >> p.shift); first < p.n; first += gridDim.x * per_group) {
+    int64_t id[U];
+    O* to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t r = first + u * per_turn;
+      id[u] = -1;
+      if (r < p.n) {
+        const uint32_t b = p.by_L(r), l = r - b * p.L;
+        id[u] = item(p.ids, b, l);
+        to[u] = (O*)p.out.data + (int64_t)b * p.out.user + (int64_t)l * p.out.row;
+      }
+    }
+    for (uint32_t piece = threadIdx.x & (lanes - 1); (int)piece * 8 < p.d; piece += lanes) {
+      const int c = piece * 8, n = p.d - c;
+      Piece<T, 8> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (id[u] >= 0) x[u] = load8((const T*)p.table + id[u] * p.stride + c, n);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t r = first + u * per_turn;
+        if (r >= p.n) continue;
+        Piece<float, 8> y = 0.f;
+        if (id[u] >= 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
+          if (DROP) drop8(p.mask, key, r, piece, y);
+        }
+        Piece<O, 8> o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = (O)y[j];
+        store8(to[u] + c, n, o);
+      }
+    }
+  }
+}
+
+struct DropParams {
+  Rows x, residual, out;
+  const int32_t* lens;
+  Divider by_L;
+  uint32_t n, L;
+  int d, shift;
+  float factor;
+  Mask mask;
+};
+
+// Y[r] = residual[r] + factor * mask * X[r]; padding zeros, not read.
+template <typename T, bool ADD>
+__global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
+  constexpr int U = 2;
+  const uint32_t lanes = 1u << p.shift, per_turn = 256 >> p.shift, per_group = per_turn * U;
+  const Key key = load_key(p.mask);
+  for (uint32_t first = blockIdx.x * per_group + (threadIdx.x >> p.shift); first < p.n; first += gridDim.x * per_group) {
+    const T *xs[U], *rs[U];
+    T* to[U];
+    bool there[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t r = first + u * per_turn;
+      there[u] = false;
+      if (r < p.n) {
+        const uint32_t b = p.by_L(r), l = r - b * p.L;
+        there[u] = !p.lens || (int)l < p.lens[b];
+        xs[u] = (const T*)p.x.data + (int64_t)b * p.x.user + (int64_t)l * p.x.row;
+        if (ADD) rs[u] = (const T*)p.residual.data + (int64_t)b * p.residual.user + (int64_t)l * p.residual.row;
+        to[u] = (T*)p.out.data + (int64_t)b * p.out.user + (int64_t)l * p.out.row;
+      }
+    }
+    for (uint32_t piece = threadIdx.x & (lanes - 1); (int)piece * 8 < p.d; piece += lanes) {
+      const int c = piece * 8, n = p.d - c;
+      Piece<T, 8> x[U], add[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (there[u]) {
+          x[u] = load8(xs[u] + c, n);
+          if (ADD) add[u] = load8(rs[u] + c, n);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t r = first + u * per_turn;
+        if (r >= p.n) continue;
+        Piece<float, 8> y = 0.f;
+        if (there[u]) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
+          drop8(p.mask, key, r, piece, y);
+          if (ADD)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] += (float)add[u][j];
+        }
+        Piece<T, 8> o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = (T)y[j];
+        store8(to[u] + c, n, o);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ host
+static unsigned groups(uint32_t n, int shift, int turns) {
+  const uint32_t per_group = (256u >> shift) * turns;
+  return std::min<uint32_t>((n + per_group - 1) / per_group, 1u << 22);
+}
+
+template <typename T, typename O>
+static void lookup(const LookupParams& p, hipStream_t st) {
+  const unsigned g = groups(p.n, p.shift, 4);
+  if (p.mask.drop) lookup_kernel<T, O, true><<<g, 256, 0, st>>>(p);
+  else lookup_kernel<T, O, false><<<g, 256, 0, st>>>(p);
+}
+
+template <typename T>
+static void dropout(const DropParams& p, hipStream_t st) {
+  const unsigned g = groups(p.n, p.shift, 2);
+  if (p.residual.data) dropout_kernel<T, true><<<g, 256, 0, st>>>(p);
+  else dropout_kernel<T, false><<<g, 256, 0, st>>>(p);
+}
+
+}  // namespace emb
+}  // namespace longer
+
+using namespace longer;
+
+extern "C" {
+
+int longer_embedding(const longer_table* table, const longer_ids* ids, const int32_t* lens, int B, int L, int d, float scale,
+                     const longer_dropout_mask* drop, const longer_rows* e, void* stream) {
+  int rc = check_tokens(B, L);
+  if (!rc) rc = emb::check_width(d);
+  if (!rc) rc = check_ids(ids, lens, B, L);
+  if (!rc && (!table || !table->data)) rc = api_error(LONGER_ERR_ARG, "table is NULL");
+  if (!rc && !size_of(table->dtype)) rc = api_error(LONGER_ERR_ARG, "table: dtype %d unknown", table->dtype);
+  if (!rc && (uintptr_t)table->data % size_of(table->dtype)) rc = api_error(LONGER_ERR_ARG, "table is not aligned to its elements");
+  if (!rc) rc = check_table_rows(table->rows);
+  if (!rc && (table->row_stride < 0 || table->row_stride > (int64_t)1 << 40)) rc = api_error(LONGER_ERR_ARG, "table: row stride %lld out of range", (long long)table->row_stride);
+  if (!rc) rc = check_rows(e, "e", B, L, d, true);
+  if (!rc && e->data == table->data) rc = api_error(LONGER_ERR_ARG, "e may not be the table");
+  if (!rc) rc = emb::check_mask(drop);
+  const double factor = scale * emb::kept(rc ? nullptr : drop);
+  if (!rc && !std::isfinite((float)factor)) rc = api_error(LONGER_ERR_ARG, "scale=%g: not an fp32 number", scale);
+  if (rc) return rc;
+  const emb::LookupParams p = {(const char*)table->data, table->row_stride,
+                               {(const char*)ids->data, B > 1 ? ids->user_stride : 0, L > 1 ? ids->row_stride : 0, lens, (uint32_t)table->rows, ids->type == LONGER_I64},
+                               emb::rows_of(e, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, emb::lanes_shift((d + 7) / 8, 8), (float)factor, emb::mask_of(drop)};
+  hipStream_t st = (hipStream_t)stream;
+  if (table->dtype == LONGER_F32) e->dtype == LONGER_F32 ? emb::lookup<float, float>(p, st) : emb::lookup<float, __bf16>(p, st);
+  else e->dtype == LONGER_F32 ? emb::lookup<__bf16, float>(p, st) : emb::lookup<__bf16, __bf16>(p, st);
+  return launched("embedding");
+}
+
+int longer_dropout(const longer_rows* x, const longer_rows* residual, const int32_t* lens, int B, int L, int d,
+                   const longer_dropout_mask* drop, const longer_rows* y, void* stream) {
+  int rc = check_tokens(B, L);
+  if (!rc) rc = emb::check_width(d);
+  if (!rc) rc = check_rows(x, "x", B, L, d, false);
+  if (!rc && residual) rc = check_rows(residual, "residual", B, L, d, false);
+  if (!rc) rc = check_rows(y, "y", B, L, d, true);
+  if (!rc && (x->dtype != y->dtype || (residual && residual->dtype != y->dtype))) rc = api_error(LONGER_ERR_ARG, "x, residual and y have one dtype");
+  if (!rc) rc = check_alias(x, y, "x and y", B, L);
+  if (!rc && residual) rc = check_alias(residual, y, "residual and y", B, L);
+  if (!rc && ((uintptr_t)lens & 3)) rc = api_error(LONGER_ERR_ARG, "lens is not aligned");
+  if (!rc && !drop) rc = api_error(LONGER_ERR_ARG, "drop is NULL");
+  if (!rc) rc = emb::check_mask(drop);
+  if (rc) return rc;
+  const emb::DropParams p = {emb::rows_of(x, B, L), residual ? emb::rows_of(residual, B, L) : emb::Rows{}, emb::rows_of(y, B, L), lens, emb::divider(L), (uint32_t)B * L,
+                             (uint32_t)L, d, emb::lanes_shift((d + 7) / 8, 8), (float)emb::kept(drop), emb::mask_of(drop)};
+  if (x->dtype == LONGER_F32) emb::dropout<float>(p, (hipStream_t)stream);
+  else emb::dropout<__bf16>(p, (hipStream_t)stream);
+  return launched("dropout");
+}
+
+}  // extern "C"

@@ -1,0 +1,389 @@
+// The tokens of a batch by item (longer_sort_ids): a stable radix sort of (id, token), lowest digit first, and the runs of equal ids.
+#include "embedding.h"
+
+namespace longer {
+namespace srt {
+
+using emb::Divider;
+
+struct Ids {
+  const char* data;
+  int64_t user, row;
+  const int32_t* lens;
+  Divider by_L;
+  uint32_t n, L, table_rows;
+  int wide;
+};
+
+constexpr uint32_t kNone = 0xffffffffu;              // of a token that names no row (ids are below 2^31)
+
+__device__ __forceinline__ uint32_t id_of(const Ids& a, uint32_t i) {
+  const uint32_t b = a.by_L(i), l = i - b * a.L;
+  if (a.lens && (int)l >= a.lens[b]) return kNone;
+  const int64_t at = (int64_t)b * a.user + (int64_t)l * a.row;
+  const int64_t id = a.wide ? ((const int64_t*)a.data)[at] : ((const int32_t*)a.data)[at];
+  return (uint64_t)id < a.table_rows ? (uint32_t)id : kNone;
+}
+
+// Place of an item among those with its digit, in a wave's order: `count` is the wave's own, one counter a digit.  A lane's peers, the
+// lanes of this step with its digit, come from one ballot a bit; the lowest of them moves the counter on.
+__device__ __forceinline__ uint32_t rank(uint32_t digit, bool there, int bits, volatile uint16_t* count) {
+  uint64_t peers = __ballot(there);
+  for (int b = 0; b < bits; ++b) {
+    const bool set = digit >> b & 1;
+    const uint64_t with = __ballot(set);
+    peers &= set ? with : ~with;
+  }
+  const uint32_t below = __popcll(peers & ((1ull << (threadIdx.x & 63)) - 1));
+  uint32_t at = 0;
+  if (there) {
+    at = count[digit];
+    if (below == 0) count[digit] = (uint16_t)(at + __popcll(peers));
+  }
+  return at + below;
+}
+
+// inclusive sum over a wave
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const uint32_t w = __shfl_up(v, o);
+    if (lane >= o) v += w;
+  }
+  return v;
+}
+
+// exclusive sum over a workgroup, and the sum of all in *sum (lds: a word for each wave); every thread takes part
+template <int THREADS>
+__device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t* lds, uint32_t* sum) {
+  const int wave = threadIdx.x >> 6;
+  const uint32_t in = wave_scan(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) lds[wave] = in;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    before += w < wave ? lds[w] : 0;
+    all += lds[w];
+  }
+  *sum = all;
+  return before + in - v;
+}
+
+// ------------------------------------------------------------------------------------ few tokens: one workgroup
+constexpr int kFewThreads = 1024, kFewItems = 8, kFew = kFewThreads * kFewItems, kFewBits = 8, kFewWaves = kFewThreads / 64;
+
+__global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, longer_order out) {
+  __shared__ uint32_t keys[kFew];
+  __shared__ uint16_t tokens[kFew], count[kFewWaves][1 << kFewBits];
+  __shared__ uint32_t base[1 << kFewBits], lds[kFewWaves];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  uint32_t n = a.n, key[kFewItems], token[kFewItems], at[kFewItems];
+  for (int shift = 0; shift < bits; shift += kFewBits) {
+    const int digits = min(bits - shift, kFewBits);
+    for (int i = threadIdx.x; i < kFewWaves << digits; i += kFewThreads) count[i >> digits][i & ((1 << digits) - 1)] = 0;
+#pragma unroll
+    for (int i = 0; i < kFewItems; ++i) {
+      const uint32_t k = (wave * kFewItems + i) * 64 + lane;
+      key[i] = kNone;
+      if (k < n) {
+        key[i] = shift ? keys[k] : id_of(a, k);
+        token[i] = shift ? tokens[k] : k;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFewItems; ++i) at[i] = rank(key[i] >> shift & ((1u << digits) - 1), key[i] != kNone, digits, count[wave]);
+    __syncthreads();
+    // where each digit begins, and in it each wave
+    uint32_t sum = 0, all;
+    const uint32_t d = threadIdx.x;
+    if (d < 1u << digits)
+      for (int w = 0; w < kFewWaves; ++w) {
+        const uint32_t c = count[w][d];
+        count[w][d] = (uint16_t)sum;
+        sum += c;
+      }
+    const uint32_t before = group_scan<kFewThreads>(sum, lds, &all);
+    if (d < 1u << digits) base[d] = before;
+    __syncthreads();
+    n = all;                                         // the first round drops the tokens that name no row
+#pragma unroll
+    for (int i = 0; i < kFewItems; ++i)
+      if (key[i] != kNone) {
+        const uint32_t d = key[i] >> shift & ((1u << digits) - 1), to = base[d] + count[wave][d] + at[i];
+        keys[to] = key[i];
+        tokens[to] = (uint16_t)token[i];
+      }
+    __syncthreads();
+  }
+  // runs: a thread takes kFewItems neighbours
+  uint32_t first = 0, runs = 0, all;
+#pragma unroll
+  for (int i = 0; i < kFewItems; ++i) {
+    const uint32_t k = threadIdx.x * kFewItems + i;
+    if (k < n) {
+      const bool head = k == 0 || keys[k] != keys[k - 1];
+      runs += head;
+      first |= (uint32_t)head << i;
+    }
+  }
+  uint32_t run = group_scan<kFewThreads>(runs, lds, &all);
+#pragma unroll
+  for (int i = 0; i < kFewItems; ++i) {
+    const uint32_t k = threadIdx.x * kFewItems + i;
+    if (k < n) {
+      if (first >> i & 1) out.rows[run++] = (int)keys[k];
+      out.runs[k] = (int)run - 1;
+      out.tokens[k] = tokens[k];
+    }
+  }
+  if (threadIdx.x == 0) {
+    out.counts[0] = (int)all;
+    out.counts[1] = (int)n;
+  }
+}
+
+// ------------------------------------------------------------------------------------ many tokens
+// A round of the sort takes one digit: every workgroup counts the digits of its stretch of the items, the counts are summed over
+// the workgroups before it, and it moves its items.  The first round reads the ids themselves and drops the tokens that name no row.
+constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostBits = 11, kMostGroups = 512;
+
+struct Round {
+  Ids ids;
+  const uint32_t *keys_in, *tokens_in;               // NULL: the first round
+  uint32_t *keys_out, *tokens_out;
+  uint32_t *counts;                                  // [groups][digits]
+  uint32_t *totals;                                  // [digits]
+  int32_t* n;                                        // the order's counts[1]: written by the first round, read by the others
+  int shift, bits;
+};
+
+// a workgroup's stretch of n items: whole tiles, as even as they can be dealt
+struct Stretch { uint32_t begin, end; };
+__device__ __forceinline__ Stretch stretch(uint32_t n) {
+  const uint32_t tiles = (n + kTile - 1) / kTile, per = (tiles + gridDim.x - 1) / gridDim.x;
+  const uint32_t begin = min((uint64_t)blockIdx.x * per * kTile, (uint64_t)n);
+  return {begin, (uint32_t)min((uint64_t)begin + (uint64_t)per * kTile, (uint64_t)n)};
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
+  __shared__ uint32_t count[1 << kMostBits];
+  const uint32_t digits = 1u << r.bits;
+  for (uint32_t i = threadIdx.x; i < digits; i += kThreads) count[i] = 0;
+  __syncthreads();
+  const Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)*r.n);
+  for (uint32_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) {
+    const uint32_t key = FIRST ? id_of(r.ids, i) : r.keys_in[i];
+    if (!FIRST || key != kNone) atomicAdd(&count[key >> r.shift & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < digits; i += kThreads) r.counts[(size_t)blockIdx.x * digits + i] = count[i];
+}
+
+// counts[g][digit] becomes the sum over the groups before g, totals[digit] that over all: 32 digits a workgroup, 32 shares of the groups
+__global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* totals, int groups, uint32_t digits) {
+  __shared__ uint32_t lds[32][33];
+  const uint32_t digit = blockIdx.x * 32 + (threadIdx.x & 31);
+  const int share = threadIdx.x >> 5, per = (groups + 31) / 32, begin = share * per, end = min(begin + per, groups);
+  uint32_t sum = 0;
+  if (digit < digits)
+    for (int g = begin; g < end; ++g) sum += counts[(size_t)g * digits + digit];
+  lds[share][threadIdx.x & 31] = sum;
+  __syncthreads();
+  if (digit >= digits) return;
+  uint32_t before = 0;
+  for (int i = 0; i < share; ++i) before += lds[i][threadIdx.x & 31];
+  if (share == 31) totals[digit] = before + sum;
+  for (int g = begin; g < end; ++g) {
+    const uint32_t c = counts[(size_t)g * digits + digit];
+    counts[(size_t)g * digits + digit] = before;
+    before += c;
+  }
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
+  __shared__ uint32_t words[kWaves << (kMostBits - 1)], base[1 << kMostBits], lds[kWaves];
+  const uint32_t digits = 1u << r.bits;
+  uint16_t* count = (uint16_t*)words;                // [waves][digits]
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  // where each digit begins for this workgroup
+  uint32_t begin = 0;
+  for (uint32_t d = 0; d < digits; d += kThreads) {
+    const uint32_t i = d + threadIdx.x;
+    uint32_t all;
+    const uint32_t before = group_scan<kThreads>(i < digits ? r.totals[i] : 0, lds, &all);
+    if (i < digits) base[i] = begin + before + r.counts[(size_t)blockIdx.x * digits + i];
+    begin += all;
+  }
+  if (FIRST && blockIdx.x == 0 && threadIdx.x == 0) *r.n = (int)begin;
+  const Stretch s = stretch(FIRST ? r.ids.n : begin);
+  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
+    for (uint32_t i = threadIdx.x; i < kWaves * digits / 2; i += kThreads) words[i] = 0;
+    uint32_t key[kItems], token[kItems], at[kItems], sums[(1 << kMostBits) / kThreads];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const uint32_t k = tile + (wave * kItems + i) * 64 + lane;
+      key[i] = kNone;
+      if (k < s.end) {
+        key[i] = FIRST ? id_of(r.ids, k) : r.keys_in[k];
+        token[i] = FIRST ? k : r.tokens_in[k];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) at[i] = rank(key[i] >> r.shift & (digits - 1), key[i] != kNone, r.bits, count + wave * digits);
+    __syncthreads();
+    // where each wave begins in a digit
+#pragma unroll
+    for (int k = 0; k < (1 << kMostBits) / kThreads; ++k) {
+      const uint32_t d = k * kThreads + threadIdx.x;
+      sums[k] = 0;
+      if (d < digits)
+        for (int w = 0; w < kWaves; ++w) {
+          const uint32_t c = count[w * digits + d];
+          count[w * digits + d] = (uint16_t)sums[k];
+          sums[k] += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      if (key[i] != kNone) {
+        const uint32_t d = key[i] >> r.shift & (digits - 1), to = base[d] + count[wave * digits + d] + at[i];
+        r.keys_out[to] = key[i];
+        r.tokens_out[to] = token[i];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < (1 << kMostBits) / kThreads; ++k)
+      if (k * kThreads + threadIdx.x < digits) base[k * kThreads + threadIdx.x] += sums[k];
+  }
+}
+
+// how many runs begin in each workgroup's stretch
+__global__ __launch_bounds__(kThreads) void heads_kernel(const uint32_t* keys, const int32_t* n, uint32_t* heads) {
+  __shared__ uint32_t lds[kWaves];
+  const Stretch s = stretch((uint32_t)*n);
+  uint32_t mine = 0, all;
+  for (uint32_t k = s.begin + threadIdx.x; k < s.end; k += kThreads) mine += k == 0 || keys[k] != keys[k - 1];
+  group_scan<kThreads>(mine, lds, &all);
+  if (threadIdx.x == 0) heads[blockIdx.x] = all;
+}
+
+__global__ __launch_bounds__(kThreads) void runs_kernel(const uint32_t* keys, const uint32_t* heads, longer_order out) {
+  static_assert(kMostGroups <= kThreads, "a thread adds up one group's runs");
+  __shared__ uint32_t lds[kWaves];
+  uint32_t run, all;
+  group_scan<kThreads>(threadIdx.x < blockIdx.x ? heads[threadIdx.x] : 0, lds, &run);
+  const Stretch s = stretch((uint32_t)out.counts[1]);
+  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
+    const uint32_t first = tile + threadIdx.x * kItems;
+    uint32_t key[kItems], before = first && first < s.end ? keys[first - 1] : kNone, mine = 0;
+    bool head[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      key[i] = first + i < s.end ? keys[first + i] : kNone;
+      head[i] = key[i] != kNone && key[i] != before;
+      mine += head[i];
+      before = key[i];
+    }
+    uint32_t at = run + group_scan<kThreads>(mine, lds, &all);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      if (key[i] != kNone) {
+        if (head[i]) out.rows[at++] = (int)key[i];
+        out.runs[first + i] = (int)at - 1;
+      }
+    run += all;
+  }
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) out.counts[0] = (int)run;
+}
+
+// ------------------------------------------------------------------------------------ host
+static int bits_of(int64_t rows) {
+  int bits = 1;
+  while (((int64_t)1 << bits) < rows) ++bits;
+  return bits;
+}
+
+struct Plan {
+  int bits, rounds, per_round, groups;
+  size_t tokens, counts, totals, heads, bytes;       // places in the workspace; the keys are at its front
+};
+
+static Plan plan(int B, int L, int64_t rows) {
+  const size_t n = (size_t)B * L;
+  Plan p = {};
+  p.bits = bits_of(rows);
+  p.rounds = (p.bits + kMostBits - 1) / kMostBits;
+  p.per_round = (p.bits + p.rounds - 1) / p.rounds;
+  p.groups = (int)std::min<size_t>((n + kTile - 1) / kTile, kMostGroups);
+  if (n <= kFew) {
+    p.bytes = 256;
+    return p;
+  }
+  p.tokens = align256(n * 4);
+  p.counts = p.tokens + (p.rounds > 1 ? align256(n * 4) : 0);
+  p.totals = p.counts + align256(((size_t)p.groups << p.per_round) * 4);
+  p.heads = p.totals + align256((size_t)4 << p.per_round);
+  p.bytes = p.heads + align256((size_t)p.groups * 4);
+  return p;
+}
+
+}  // namespace srt
+}  // namespace longer
+
+using namespace longer;
+
+extern "C" {
+
+size_t longer_sort_ids_workspace_bytes(int B, int L, int64_t table_rows) {
+  return check_tokens(B, L) || check_table_rows(table_rows) ? 0 : srt::plan(B, L, table_rows).bytes;
+}
+
+int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, int64_t table_rows, const longer_order* order,
+                    void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_tokens(B, L);
+  if (!rc) rc = check_ids(ids, lens, B, L);
+  if (!rc) rc = check_table_rows(table_rows);
+  if (!rc) rc = emb::check_order(order);
+  if (!rc && (!ws || ((uintptr_t)ws & 255))) rc = api_error(LONGER_ERR_ARG, "ws must be 256-byte aligned and not NULL");
+  if (rc) return rc;
+  const srt::Plan p = srt::plan(B, L, table_rows);
+  if (ws_bytes < p.bytes) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, p.bytes);
+  hipStream_t st = (hipStream_t)stream;
+  const srt::Ids a = {(const char*)ids->data, B > 1 ? ids->user_stride : 0, L > 1 ? ids->row_stride : 0, lens, emb::divider(L), (uint32_t)B * L, (uint32_t)L,
+                      (uint32_t)table_rows, ids->type == LONGER_I64};
+  if (a.n <= srt::kFew) {
+    srt::few_kernel<<<1, srt::kFewThreads, 0, st>>>(a, p.bits, *order);
+    return launched("sort of ids");
+  }
+  char* w = (char*)ws;
+  uint32_t *keys = (uint32_t*)w, *counts = (uint32_t*)(w + p.counts), *totals = (uint32_t*)(w + p.totals), *heads = (uint32_t*)(w + p.heads);
+  srt::Round r = {a, nullptr, nullptr, nullptr, nullptr, counts, totals, order->counts + 1, 0, 0};
+  for (int i = 0; i < p.rounds; ++i) {
+    const bool last = (p.rounds - 1 - i) % 2 == 0;   // rounds take turns so that the last one ends in the order's tokens and this workspace's keys
+    r.keys_out = last ? keys : (uint32_t*)order->runs;
+    r.tokens_out = last ? (uint32_t*)order->tokens : (uint32_t*)(w + p.tokens);
+    r.shift = i * p.per_round;
+    r.bits = std::min(p.per_round, p.bits - r.shift);
+    const uint32_t digits = 1u << r.bits;
+    if (i == 0) srt::count_kernel<true><<<p.groups, srt::kThreads, 0, st>>>(r);
+    else srt::count_kernel<false><<<p.groups, srt::kThreads, 0, st>>>(r);
+    srt::sum_kernel<<<(digits + 31) / 32, 1024, 0, st>>>(counts, totals, p.groups, digits);
+    if (i == 0) srt::move_kernel<true><<<p.groups, srt::kThreads, 0, st>>>(r);
+    else srt::move_kernel<false><<<p.groups, srt::kThreads, 0, st>>>(r);
+    r.keys_in = r.keys_out;
+    r.tokens_in = r.tokens_out;
+  }
+  srt::heads_kernel<<<p.groups, srt::kThreads, 0, st>>>(keys, order->counts + 1, heads);
+  srt::runs_kernel<<<p.groups, srt::kThreads, 0, st>>>(keys, heads, *order);
+  return launched("sort of ids");
+}
+
+}  // extern "C"

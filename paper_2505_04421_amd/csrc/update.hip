@@ -1,7 +1,6 @@
-// Behind the gradients: their global norm and clipping, and the AdamW update (longer_grad_norm, longer_clip_gradients,
-// longer_adamw_step).
-#include "../../include/longer.h"
-#include "device.h"
+// Behind the gradients: their global norm and clipping, and the AdamW update of whole tensors and of the rows that a batch names
+// (longer_grad_norm, longer_clip_gradients, longer_adamw_step, longer_adamw_rows).
+#include "embedding.h"
 
 #include <algorithm>
 #include <cfloat>
@@ -9,9 +8,6 @@
 #include <cstring>
 
 namespace longer {
-
-int api_error(int code, const char* fmt, ...);   // longer_api.hip
-
 namespace upd {
 
 // A launch takes its tensors in its arguments (under 4 KB of them), so a call needs no table in device memory and
@@ -77,11 +73,12 @@ struct ClipArgs {
 // or 58 with buffers of their own.
 constexpr int kStepWords = 940, kEntry = 6, kBuffers = 10, kStepList = (kStepWords - kBuffers) / kEntry;
 constexpr uint32_t kHalfG = 1u << 16, kHalfW = 1u << 17, kCopy = 1u << 18, kGroup = 0xffff;
+struct How { float beta1, one_beta1, beta2, one_beta2, rate, root, eps; };   // rate = lr / (1 - beta1^t), root = 1 / sqrt(1 - beta2^t)
 struct StepArgs {
   uint32_t list[kStepWords];
   int count;
   const float* norm;
-  float beta1, one_beta1, beta2, one_beta2, rate, root, eps;   // rate = lr / (1 - beta1^t), root = 1 / sqrt(1 - beta2^t)
+  How how;
 };
 
 template <int THREADS>
@@ -187,7 +184,7 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
 struct Place { float *p, *m, *v; const void* g; void* w; };
 
 // one value (one copy of the formula for whole vectors and tails: the same bits whatever the piece)
-__device__ __forceinline__ void step_value(const StepArgs& a, float decay, float g, float& p, float& m, float& v) {
+__device__ __forceinline__ void step_value(const How& a, float decay, float g, float& p, float& m, float& v) {
   m = fmaf(a.beta1, m, a.one_beta1 * g);
   v = fmaf(a.beta2, v, a.one_beta2 * (g * g));
   p -= fmaf(decay, p, a.rate * (m / fmaf(sqrtf(v), a.root, a.eps)));
@@ -211,7 +208,7 @@ __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, ui
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float pj = p[j], mj = m[j], vj = v[j];
-      step_value(a, decay, c * (float)g[j], pj, mj, vj);
+      step_value(a.how, decay, c * (float)g[j], pj, mj, vj);
       p[j] = pj;
       m[j] = mj;
       v[j] = vj;
@@ -224,7 +221,7 @@ __device__ __forceinline__ void step_piece(const StepArgs& a, const Place& t, ui
   } else {
     for (uint32_t k = i; k < n; ++k) {
       float p = t.p[k], m = t.m[k], v = t.v[k];
-      step_value(a, decay, c * (float)gs[k], p, m, v);
+      step_value(a.how, decay, c * (float)gs[k], p, m, v);
       t.p[k] = p;
       t.m[k] = m;
       t.v[k] = v;
@@ -263,13 +260,66 @@ __global__ __launch_bounds__(kStepPiece / 4) void step_kernel(StepArgs a) {
   else step_piece<float>(a, buffers, at, kind, n, c, decay);
 }
 
-// ------------------------------------------------------------------------------------ host
-static int size_of(int dtype) { return dtype == LONGER_F32 ? 4 : dtype == LONGER_BF16 ? 2 : 0; }
+// The rows of a table that a batch names: row i of g is the gradient of row rows[i].  2^shift lanes hold a row, four values each.
+struct RowsArgs {
+  float *p, *m, *v;
+  void* w;
+  const float* g;
+  const int32_t *rows, *counts;
+  const float* norm;
+  uint32_t most, table_rows;                          // rows of g at most, rows of the table
+  int d, shift;
+  float decay;                                        // lr * decay
+  How how;
+};
 
-static int launched(const char* what) {
-  return hipGetLastError() == hipSuccess ? 0 : api_error(LONGER_ERR_HIP, "%s launch failed", what);
+template <typename W, bool COPY>
+__global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
+  float c = 1.f;
+  if (a.norm) {
+    if (!isfinite(a.norm[0])) return;
+    c = a.norm[1];
+  }
+  const uint32_t count = min((uint32_t)max(a.counts[0], 0), a.most), lanes = 1u << a.shift, step = gridDim.x * (256 >> a.shift);
+  for (uint32_t i = blockIdx.x * (256 >> a.shift) + (threadIdx.x >> a.shift); i < count; i += step) {
+    const uint32_t row = (uint32_t)a.rows[i];
+    if (row >= a.table_rows) continue;
+    const size_t at = (size_t)row * a.d;
+    const float* gs = a.g + (size_t)i * a.d;
+    W* ws = (W*)a.w;
+    for (int k = (threadIdx.x & (lanes - 1)) * 4; k < a.d; k += lanes * 4) {
+      if (k + 4 <= a.d) {
+        const Four<float> g = *(const Four<float>*)(gs + k);
+        Four<float> m = *(const Four<float>*)(a.m + at + k), v = *(const Four<float>*)(a.v + at + k), p = *(const Four<float>*)(a.p + at + k);
+        Four<W> w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float pj = p[j], mj = m[j], vj = v[j];
+          step_value(a.how, a.decay, c * g[j], pj, mj, vj);
+          p[j] = pj;
+          m[j] = mj;
+          v[j] = vj;
+          w[j] = (W)pj;
+        }
+        *(Four<float>*)(a.m + at + k) = m;
+        *(Four<float>*)(a.v + at + k) = v;
+        *(Four<float>*)(a.p + at + k) = p;
+        if (COPY) *(Four<W>*)(ws + at + k) = w;
+      } else {
+        for (int j = k; j < a.d; ++j) {
+          float p = a.p[at + j], m = a.m[at + j], v = a.v[at + j];
+          step_value(a.how, a.decay, c * gs[j], p, m, v);
+          a.p[at + j] = p;
+          a.m[at + j] = m;
+          a.v[at + j] = v;
+          if (COPY) ws[at + j] = (W)p;
+        }
+      }
+    }
+  }
 }
 
+// ------------------------------------------------------------------------------------ host
 constexpr int64_t kMostEntry = (int64_t)1 << 30;     // values of one place in a launch's list
 constexpr int64_t kMostValues = (int64_t)1 << 40;    // of a list: more than a GPU's memory holds
 
@@ -290,6 +340,19 @@ static int check_list(const longer_tensor* t, int count, int64_t* values) {
     if (sum > kMostValues) return api_error(LONGER_ERR_ARG, "a list of more than 2^40 values");
   }
   *values = sum;
+  return 0;
+}
+
+static int check_how(const longer_adamw* how, How* h) {
+  if (!how) return api_error(LONGER_ERR_ARG, "how is NULL");
+  if (!(how->lr >= 0.) || !std::isfinite(how->lr)) return api_error(LONGER_ERR_ARG, "lr=%g: not negative, finite", how->lr);
+  if (!(how->beta1 >= 0. && how->beta1 < 1.) || !(how->beta2 >= 0. && how->beta2 < 1.)) return api_error(LONGER_ERR_ARG, "beta1=%g beta2=%g: 0 to below 1", how->beta1, how->beta2);
+  if (!(how->eps >= FLT_MIN && how->eps <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "eps=%g must be positive (a normal fp32 number)", how->eps);
+  if (how->step < 1) return api_error(LONGER_ERR_ARG, "step=%lld: counts from 1", (long long)how->step);
+  const double rate = how->lr / (1. - std::pow(how->beta1, (double)how->step));
+  if (!(rate <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "lr=%g: lr / (1 - beta1^step) is beyond fp32", how->lr);
+  *h = {(float)how->beta1, (float)(1. - how->beta1), (float)how->beta2, (float)(1. - how->beta2), (float)rate,
+        (float)(1. / std::sqrt(1. - std::pow(how->beta2, (double)how->step))), (float)how->eps};
   return 0;
 }
 
@@ -378,7 +441,7 @@ int longer_grad_norm(const longer_tensor* grads, int count, float max_norm, floa
                   done += k;
                 });
   upd::norm_join_kernel<<<1, 1024, 0, st>>>((const double*)ws, done, max_norm, norm_out);
-  return upd::launched("gradient norm");
+  return launched("gradient norm");
 }
 
 int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, int count, const float* norm, void* stream) {
@@ -407,18 +470,13 @@ int longer_clip_gradients(const longer_tensor* grads, const longer_tensor* out, 
                   a.count = entries;
                   upd::clip_kernel<<<k, 256, 0, st>>>(a);
                 });
-  return upd::launched("gradient clipping");
+  return launched("gradient clipping");
 }
 
 int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adamw* how, const float* norm, void* stream) {
   if (!t || count <= 0) return api_error(LONGER_ERR_ARG, "an empty list of tensors");
-  if (!how) return api_error(LONGER_ERR_ARG, "how is NULL");
-  if (!(how->lr >= 0.) || !std::isfinite(how->lr)) return api_error(LONGER_ERR_ARG, "lr=%g: not negative, finite", how->lr);
-  if (!(how->beta1 >= 0. && how->beta1 < 1.) || !(how->beta2 >= 0. && how->beta2 < 1.)) return api_error(LONGER_ERR_ARG, "beta1=%g beta2=%g: 0 to below 1", how->beta1, how->beta2);
-  if (!(how->eps >= FLT_MIN && how->eps <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "eps=%g must be positive (a normal fp32 number)", how->eps);
-  if (how->step < 1) return api_error(LONGER_ERR_ARG, "step=%lld: counts from 1", (long long)how->step);
-  const double rate = how->lr / (1. - std::pow(how->beta1, (double)how->step));
-  if (!(rate <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "lr=%g: lr / (1 - beta1^step) is beyond fp32", how->lr);
+  upd::How h;
+  if (int rc = upd::check_how(how, &h)) return rc;
   if ((uintptr_t)norm & 3) return api_error(LONGER_ERR_ARG, "norm is not aligned");
   int64_t values = 0;
   for (int i = 0; i < count; ++i) {
@@ -439,13 +497,7 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
   hipStream_t st = (hipStream_t)stream;
   upd::StepArgs a;
   a.norm = norm;
-  a.beta1 = (float)how->beta1;
-  a.one_beta1 = (float)(1. - how->beta1);
-  a.beta2 = (float)how->beta2;
-  a.one_beta2 = (float)(1. - how->beta2);
-  a.rate = (float)rate;
-  a.root = (float)(1. / std::sqrt(1. - std::pow(how->beta2, (double)how->step)));
-  a.eps = (float)how->eps;
+  a.how = h;
   int groups = 0;                                     // of the launch at hand, and the last one's buffers, where place 0 would be
   uint64_t last[5];
   uint32_t last_kind = 0;
@@ -485,7 +537,40 @@ int longer_adamw_step(const longer_adamw_tensor* t, int count, const longer_adam
                   a.count = entries;
                   upd::step_kernel<<<k, upd::kStepPiece / 4, 0, st>>>(a);
                 });
-  return upd::launched("AdamW update");
+  return launched("AdamW update");
+}
+
+int longer_adamw_rows(const longer_adamw_table* t, const longer_order* order, int B, int L, const float* g,
+                      const longer_adamw* how, const float* norm, void* stream) {
+  int rc = check_tokens(B, L);
+  if (!rc) rc = emb::check_order(order);
+  if (!rc && !t) rc = api_error(LONGER_ERR_ARG, "table is NULL");
+  if (!rc) rc = emb::check_width(t->d);
+  if (!rc) rc = check_table_rows(t->rows);
+  if (!rc) rc = check_vector(t->p, LONGER_F32, "p");
+  if (!rc) rc = check_vector(t->m, LONGER_F32, "m");
+  if (!rc) rc = check_vector(t->v, LONGER_F32, "v");
+  if (!rc) rc = check_vector(g, LONGER_F32, "g");
+  if (!rc && t->w && !size_of(t->w_dtype)) rc = api_error(LONGER_ERR_ARG, "dtype %d of w unknown", t->w_dtype);
+  if (!rc && t->w) rc = check_vector(t->w, t->w_dtype, "w");
+  if (rc) return rc;
+  const void* at[5] = {t->p, t->m, t->v, g, t->w};
+  for (int j = 0; j < 5; ++j)
+    for (int k = 0; k < j; ++k)
+      if (at[j] == at[k]) return api_error(LONGER_ERR_ARG, "two of p, m, v, g, w are the same memory");
+  upd::How h;
+  if ((rc = upd::check_how(how, &h))) return rc;
+  if (!(t->decay >= 0.) || !(how->lr * t->decay <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "decay=%g: not negative, lr decay an fp32 number", t->decay);
+  if ((uintptr_t)norm & 3) return api_error(LONGER_ERR_ARG, "norm is not aligned");
+  const uint32_t most = (uint32_t)std::min<int64_t>((int64_t)B * L, t->rows);
+  const upd::RowsArgs a = {t->p, t->m, t->v, t->w, g, order->rows, order->counts, norm, most, (uint32_t)t->rows, t->d, emb::lanes_shift((t->d + 3) / 4, 8),
+                           (float)(how->lr * t->decay), h};
+  const unsigned per_group = 256u >> a.shift, groups = std::min((most + per_group - 1) / per_group, 2048u);
+  hipStream_t st = (hipStream_t)stream;
+  if (!t->w) upd::rows_kernel<float, false><<<groups, 256, 0, st>>>(a);
+  else if (t->w_dtype == LONGER_BF16) upd::rows_kernel<__bf16, true><<<groups, 256, 0, st>>>(a);
+  else upd::rows_kernel<float, true><<<groups, 256, 0, st>>>(a);
+  return launched("AdamW update of rows");
 }
 
 }  // extern "C"

@@ -1,0 +1,551 @@
+"""longer_embedding, longer_dropout, longer_sort_ids, longer_embedding_backward and longer_adamw_rows against their formulas in 64 bits: rows
+of one value to 16384, one token to hundreds of thousands, any strides, both id types, missing ids, empty users, masks.
+
+Tolerances.  u = 2^-24, half a step of fp32; half a step of bf16 is 2^-8 of the value.  A looked-up value is a product with the factor,
+itself rounded: 2 u, and the output's rounding.  Dropout adds one sum.  A gradient is a sum of n terms in fp32, in any order at most n u of
+the terms' magnitudes, and the factor's two roundings.  A norm is off by the norm of what its row is off, and one rounding."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_04421_amd as lg
+from embedding_oracle import factors, gradient, named, order
+from gpu_util import guarded_empty
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+TINY = 2.0 ** -126
+
+
+def np64(t):
+    return t.double().cpu().numpy()
+
+
+def mask(p, seed=0x123456789abcdef, step=(7 << 32) + 99, site=3):
+    key = torch.tensor([seed, step], dtype=torch.int64, device=DEV)
+    return lg.DropoutMask(p, key, site), lambda rows, d: factors(rows, d, p, seed, step, site)
+
+
+def draw_ids(r, B, L, rows, skew="even", missing=True):
+    if skew == "one":
+        i = np.where(r.random((B, L)) < 0.9, rows // 2, r.integers(0, rows, (B, L)))
+    elif skew == "popular":
+        i = np.minimum(np.exp(r.random((B, L)) * np.log(rows + 1)).astype(np.int64) - 1, rows - 1)
+    else:
+        i = r.integers(0, rows, (B, L))
+    if missing:
+        bad = np.array([-1, rows, -(1 << 31), (1 << 31) - 1])
+        i = np.where(r.random((B, L)) < 0.05, bad[r.integers(0, 4, (B, L))], i)
+    return i
+
+
+def on_gpu(ids, kind=torch.int64, fields=1):
+    buf = torch.full(ids.shape + (fields,), 1 << 30, dtype=kind, device=DEV)
+    v = buf[:, :, fields // 2]
+    v.copy_(torch.from_numpy(np.ascontiguousarray(ids)))
+    return v
+
+
+def lengths(r, B, L, how):
+    if how == "all":
+        return None, None
+    n = np.zeros(B, np.int32) if how == "none" else r.integers(0, L + 1, B).astype(np.int32)
+    if how == "ragged" and B > 2:
+        n[0], n[1], n[2] = 0, L, 1
+    return n, torch.from_numpy(n).to(DEV)
+
+
+def strided(B, L, d, dtype, pad, fill=float("nan")):
+    """A [B, L, d] view of a larger buffer, rows `pad` values apart from one another and off the 16 bytes, and that buffer."""
+    buf = torch.full((B * (L + 1) * (d + pad) + 1,), fill, dtype=dtype, device=DEV)
+    return buf.as_strided((B, L, d), ((L + 1) * (d + pad), d + pad, 1), 1 if pad else 0), buf
+
+
+SHAPES = [(1, 1, 1, 1), (1, 1, 8, 5), (3, 5, 7, 11), (2, 33, 9, 1000), (4, 64, 32, 1000), (5, 3, 130, 7), (2, 3, 2049, 50), (1, 2, 16384, 3), (17, 96, 64, 400), (1, 700, 15, 65)]
+
+
+@pytest.mark.parametrize("how", ["all", "ragged", "none"])
+@pytest.mark.parametrize("types", ["f32 f32 i32", "f32 bf16 i64", "bf16 f32 i64", "bf16 bf16 i32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_lookup(shape, types, how):
+    B, L, d, R = shape
+    print("  longer_embedding", shape, types, how, flush=True)
+    td, ed, kind = types.split()
+    td, ed, kind = TYPES[td], TYPES[ed], {"i32": torch.int32, "i64": torch.int64}[kind]
+    r = np.random.default_rng(B * L + d)
+    ids = draw_ids(r, B, L, R)
+    lens, glens = lengths(r, B, L, how)
+    for pad, fields, p, scale in ((0, 1, 0.0, 1.0), (3, 3, 0.1, 11.3), (5, 2, 0.5, -0.7)):
+        table = torch.full((R, d + pad), float("nan"), dtype=td, device=DEV)[:, :d]
+        table.copy_(torch.from_numpy(r.standard_normal((R, d))))
+        table[R // 2, d // 2] = float("inf")
+        drop, f = mask(p) if p else (None, None)
+        out, buf = strided(B, L, d, ed, pad)
+        before = buf.clone()
+        lg.longer_embedding(table, on_gpu(ids, kind, fields), glens, scale, drop, out)
+        there = named(ids, lens, R)
+        want = np64(table)[np.where(there, ids, 0)] * scale
+        if p:
+            k = f(np.arange(B * L), d).reshape(B, L, d)
+            want = np.where(k == 0, 0.0, want * np.where(k == 0, 1.0, k))
+        want = np.where(there[..., None], want, 0.0)
+        got = np64(out)
+        fine = np.isfinite(want)
+        assert (np.abs(got - want)[fine] <= (np.abs(want) * (2.01 * U + HALF[ed]) + TINY)[fine]).all()
+        assert (got[~fine] == want[~fine]).all()
+        assert (got[want == 0] == 0).all()
+        inside = torch.zeros_like(buf, dtype=torch.bool)
+        inside.as_strided(out.shape, out.stride(), out.storage_offset()).fill_(True)
+        assert torch.equal(buf[~inside].isnan(), before[~inside].isnan())
+        if scale == 1.0 and td == ed:
+            assert (got == want).all()
+
+
+def test_lookup_of_one_item_for_all_and_of_a_table_with_one_row_for_all():
+    table = torch.randn(9, 40, device=DEV)
+    ids = torch.tensor([[4]], device=DEV).expand(6, 7)
+    out = torch.empty(6, 7, 40, device=DEV)
+    lg.longer_embedding(table, ids, None, 1.0, None, out)
+    assert torch.equal(out, table[4].expand_as(out))
+    lg.longer_embedding(table[2:3].expand(9, 40), ids, None, 1.0, None, out)
+    assert torch.equal(out, table[2].expand_as(out))
+
+
+@pytest.mark.parametrize("how", ["all", "ragged", "none"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_dropout(shape, dtype, how):
+    B, L, d, _ = shape
+    print("  longer_dropout", shape, dtype, how, flush=True)
+    t = TYPES[dtype]
+    r = np.random.default_rng(d)
+    lens, glens = lengths(r, B, L, how)
+    there = np.ones((B, L), bool) if lens is None else np.arange(L) < lens[:, None]
+    gthere = torch.from_numpy(there).to(DEV)[..., None]
+    for pad, p, add, place in ((0, 0.1, False, "new"), (3, 0.5, True, "new"), (3, 0.3, True, "x"), (0, 0.9999, True, "residual"), (1, 0.0, True, "new")):
+        x, _ = strided(B, L, d, t, pad)
+        x.copy_(torch.from_numpy(r.standard_normal((B, L, d))))
+        x[0, 0, d // 2] = float("inf")
+        res, _ = strided(B, L, d, t, pad)
+        res.copy_(torch.from_numpy(r.standard_normal((B, L, d))))
+        x.masked_fill_(~gthere, float("nan"))
+        res.masked_fill_(~gthere, float("nan"))
+        x0, r0 = np64(x), np64(res)
+        out, buf = {"x": (x, None), "residual": (res, None), "new": strided(B, L, d, t, pad)}[place]
+        drop, f = mask(p, seed=-5, step=1, site=65535)
+        lg.longer_dropout(x, res if add else None, glens, drop, out)
+        k = f(np.arange(B * L), d).reshape(B, L, d)
+        kx = np.where(k == 0, 0.0, np.where(there[..., None], x0, 0.0) * np.where(k == 0, 1.0, k))
+        base = np.where(there[..., None], r0, 0.0) if add else 0.0
+        want, got = kx + base, np64(out)
+        fine = np.isfinite(want)
+        tol = 2.01 * U * np.abs(kx) + np.abs(want) * (U + HALF[t]) + TINY
+        assert (np.abs(got - want)[fine] <= tol[fine]).all()
+        assert (got[~fine] == want[~fine]).all() and (got[~there] == 0).all()
+        if not add:
+            assert ((got == 0) == (want == 0)).all()
+        if buf is not None:
+            assert int(torch.isnan(buf).sum()) == buf.numel() - out.numel()
+
+
+def test_dropout_is_its_own_backward_pass_and_counts_what_it_drops():
+    """<mask X, W> = <X, mask W>: each side a sum of values that the other has, to 3 u a term; and a share of p of 2 million values to five
+    standard deviations, at another step or site independently."""
+    B, L, d = 16, 1000, 128
+    x, w = torch.randn(B, L, d, device=DEV), torch.randn(B, L, d, device=DEV)
+    y, b = torch.empty_like(x), torch.empty_like(x)
+    drop, _ = mask(0.1)
+    lg.longer_dropout(x, None, None, drop, y)
+    lg.longer_dropout(w, None, None, drop, b)
+    one, other = (y.double() * w.double()).sum(), (x.double() * b.double()).sum()
+    assert abs(float(one - other)) <= 6 * U * float((y.double() * w.double()).abs().sum())
+    n, p = x.numel(), round(6553.6) / 65536
+    dropped = y == 0
+    assert abs(float(dropped.double().mean()) - p) < 5 * np.sqrt(p * (1 - p) / n)
+    for kw in (dict(step=8), dict(site=4), dict(seed=1)):
+        lg.longer_dropout(x, None, None, mask(0.1, **kw)[0], b)
+        both = float(((b == 0) & dropped).double().mean())
+        assert abs(both - p * p) < 5 * np.sqrt(p * p * (1 - p * p) / n)
+
+
+def fresh_order(n, rows):
+    made = [guarded_empty(DEV, (k,), torch.int32) for k in (n, n, min(n, rows), 2)]
+    for t, _ in made:
+        t.fill_(-77)
+    return lg.TokenOrder(*[t for t, _ in made]), [g for _, g in made]
+
+
+def sort(ids, kind, fields, glens, rows):
+    B, L = ids.shape
+    o, guards = fresh_order(B * L, rows)
+    n = lg.longer_sort_ids_workspace_bytes(B, L, rows)
+    ws, g = guarded_empty(DEV, (n,), torch.uint8)
+    lg.longer_sort_ids(on_gpu(ids, kind, fields), glens, rows, o, ws)
+    torch.cuda.synchronize()
+    for x in guards + [g]:
+        x.check("sort")
+    return o, ws
+
+
+SORTS = [(1, 1, 1), (1, 1, 900), (1, 2, 2), (3, 21, 5), (1, 64, 1), (5, 13, 64), (1, 65, 300), (64, 96, 1000), (1, 8191, 257), (8, 1024, 65536), (1, 8193, 1), (1, 8193, 3),
+         (9, 911, 2048), (3, 4096, 2049), (6, 2049, 70000), (2, 10241, 1 << 22), (64, 2000, (1 << 22) + 1), (31, 3333, (1 << 31) - 1), (256, 2000, 1_000_003), (1, 1_100_001, 2_000_000)]
+
+
+@pytest.mark.parametrize("skew", ["even", "popular", "one"])
+@pytest.mark.parametrize("shape", SORTS)
+def test_sort(shape, skew):
+    B, L, R = shape
+    print("  longer_sort_ids", shape, skew, flush=True)
+    r = np.random.default_rng(B + L)
+    for kind, fields, how, missing in ((torch.int64, 1, "all", False), (torch.int32, 3, "ragged", True), (torch.int64, 2, "none", True)):
+        ids = draw_ids(r, B, L, R, skew, missing)
+        lens, glens = lengths(r, B, L, how)
+        o, _ = sort(ids, kind, fields, glens, R)
+        tokens, runs, distinct = order(ids, lens, R)
+        assert o.counts.tolist() == [len(distinct), len(tokens)]
+        for got, want in ((o.tokens, tokens), (o.runs, runs), (o.rows, distinct)):
+            assert np.array_equal(got[:len(want)].cpu().numpy(), want)
+            assert bool((got[len(want):] == -77).all())
+
+
+def backward(o, de, scale, drop, dense, rows):
+    B, L, d = de.shape
+    n = lg.longer_embedding_backward_workspace_bytes(B, L, d)
+    ws, g0 = guarded_empty(DEV, (n,), torch.uint8)
+    out = rows if dense else min(B * L, rows)
+    grads, g1 = guarded_empty(DEV, (out, d), torch.float32)
+    norms, g2 = guarded_empty(DEV, (out,), torch.float32)
+    grads.fill_(-77.0)
+    lg.longer_embedding_backward(o, de, scale, drop, dense, grads, norms, ws)
+    torch.cuda.synchronize()
+    for g in (g0, g1, g2):
+        g.check("gradient")
+    return grads, norms, ws
+
+
+GRADS = [(1, 1, 1, 1), (1, 1, 8, 900), (2, 3, 7, 5), (1, 9, 16, 1), (3, 21, 33, 5), (1, 64, 32, 20), (64, 96, 64, 1000), (3, 401, 513, 65), (2, 150, 1024, 9), (1, 70, 16384, 12), (4, 4096, 20, 70000),
+         (6, 2049, 128, 300), (40, 500, 130, 3000)]
+
+
+@pytest.mark.parametrize("skew", ["even", "popular", "one"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", GRADS)
+def test_gradient(shape, dtype, skew):
+    B, L, d, R = shape
+    print("  longer_embedding_backward", shape, dtype, skew, flush=True)
+    t = TYPES[dtype]
+    r = np.random.default_rng(B * L * d)
+    for how, pad, p, scale in (("all", 0, 0.0, 1.0), ("ragged", 3, 0.1, 11.3), ("ragged", 0, 0.5, -0.7), ("none", 0, 0.2, 2.0)):
+        ids = draw_ids(r, B, L, R, skew)
+        lens, glens = lengths(r, B, L, how)
+        there = named(ids, lens, R)
+        de, _ = strided(B, L, d, t, pad)
+        de.copy_(torch.from_numpy(r.standard_normal((B, L, d))))
+        de.masked_fill_(torch.from_numpy(~there).to(DEV)[..., None], float("nan"))       # what no row has is not read
+        o, _ = sort(ids, torch.int64, 1, glens, R)
+        drop, f = mask(p) if p else (None, None)
+        distinct, g, mag, count = gradient(ids, lens, R, np64(de), scale, f(np.arange(B * L), d) if p else None)
+        tol = mag * (count[:, None] + 3) * U + TINY
+        norm = np.sqrt((g * g).sum(1))
+        norm_tol = np.sqrt((tol * tol).sum(1)) + 2 * U * norm
+        for dense in (False, True):
+            grads, norms, ws = backward(o, de, scale, drop, dense, R)
+            got, gn = np64(grads), np64(norms)
+            if dense:
+                rest = np.setdiff1d(np.arange(R), distinct)
+                assert (got[rest] == 0).all() and (gn[rest] == 0).all()
+                got, gn = got[distinct], gn[distinct]
+            else:
+                assert (got[len(distinct):] == -77.0).all() and (gn[len(distinct):] == 0).all()
+                got, gn = got[:len(distinct)], gn[:len(distinct)]
+            assert (np.abs(got - g) <= tol).all()
+            assert (np.abs(gn - norm) <= norm_tol).all()
+            again, norms2 = torch.empty_like(grads).fill_(-77.0), torch.empty_like(norms)
+            lg.longer_embedding_backward(o, de, scale, drop, dense, again, norms2, ws)
+            assert torch.equal(again, grads) and torch.equal(norms2, norms)               # the same bits
+            lg.longer_embedding_backward(o, de, scale, drop, dense, again.fill_(-77.0), None, ws)
+            assert torch.equal(again, grads)
+
+
+def test_gradient_of_an_item_in_every_place():
+    """One run through every range: 300000 tokens of one item, and of two whose border lies inside a range."""
+    L, d = 300_000, 24
+    de = torch.randn(1, L, d, device=DEV)
+    for ids in (np.full((1, L), 3), np.where(np.arange(L) % 3 == 0, 2, 3)[None]):
+        o, _ = sort(ids, torch.int32, 1, None, 5)
+        grads, norms, _ = backward(o, de, 1.0, None, False, 5)
+        distinct, g, mag, count = gradient(ids, None, 5, np64(de), 1.0)
+        assert (np.abs(np64(grads)[:len(distinct)] - g) <= mag * (count[:, None] + 3) * U).all()
+
+
+def test_gradient_that_is_not_finite_and_one_beyond_the_norms_square():
+    ids = np.array([[0, 1, 2, 1, 3]])
+    de = torch.ones(1, 5, 40, device=DEV)
+    de[0, 0, 3], de[0, 1, 4], de[0, 4, :] = float("nan"), float("inf"), 1e30
+    o, _ = sort(ids, torch.int64, 1, None, 4)
+    grads, norms, _ = backward(o, de, 1.0, None, False, 4)
+    assert torch.isnan(grads[0]).sum() == 1 and bool(torch.isnan(norms[0]))
+    assert float(grads[1, 4]) == float("inf") and float(norms[1]) == float("inf")
+    assert abs(float(norms[3]) / (1e30 * np.sqrt(40)) - 1) <= 3 * U and float(norms[2]) == pytest.approx(np.sqrt(40), rel=2 * U)
+
+
+def test_gradient_against_differences():
+    """The loss sum(E W) is linear in the table: its difference along D over a step of 1 is <G, D>, but for the roundings of E, 2.01 u of each
+    value on both sides, and of G."""
+    B, L, d, R = 5, 37, 50, 40
+    r = np.random.default_rng(5)
+    ids = draw_ids(r, B, L, R)
+    lens, glens = lengths(r, B, L, "ragged")
+    T, D, W = (torch.randn(*s, device=DEV) for s in ((R, d), (R, d), (B, L, d)))
+    drop, _ = mask(0.3)
+    E = [torch.empty(B, L, d, device=DEV) for _ in range(2)]
+    plus, minus = (T + D / 2), (T - D / 2)
+    for t, e in zip((plus, minus), E):
+        lg.longer_embedding(t, on_gpu(ids), glens, 1.7, drop, e)
+    slope = float(((E[0].double() - E[1].double()) * W.double()).sum())
+    o, _ = sort(ids, torch.int64, 1, glens, R)
+    grads, _, _ = backward(o, W, 1.7, drop, True, R)
+    want = float((grads.double() * (plus.double() - minus.double())).sum())
+    tol = 2.01 * U * float(((E[0].abs() + E[1].abs()).double() * W.abs()).sum()) + (B * L + 3) * U * float((grads.abs() * D.abs()).double().sum()) * 4
+    assert abs(slope - want) <= tol
+
+
+@pytest.mark.parametrize("weights", ["none", "f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (3, 5, 7, 11), (64, 96, 32, 1000), (2, 700, 130, 90), (1, 40, 2049, 70), (20, 1000, 64, 30000), (1, 3, 16384, 4)])
+def test_rows_update(shape, weights):
+    """The rows that a batch names: the bits of longer_adamw_step on the dense gradient; the others as they were."""
+    B, L, d, R = shape
+    print("  longer_adamw_rows", shape, weights, flush=True)
+    r = np.random.default_rng(d)
+    ids = draw_ids(r, B, L, R, "popular")
+    lens, glens = lengths(r, B, L, "ragged")
+    o, _ = sort(ids, torch.int64, 1, glens, R)
+    de = torch.randn(B, L, d, device=DEV)
+    compact, norms, _ = backward(o, de, 0.3, None, False, R)
+    dense, _, _ = backward(o, de, 0.3, None, True, R)
+    start = [torch.randn(R, d, device=DEV) * s for s in (0.05, 0.003, 0.01)]
+    start[2].square_()
+    distinct = torch.from_numpy(order(ids, lens, R)[2]).to(DEV)
+    hit = torch.zeros(R, dtype=torch.bool, device=DEV)
+    hit[distinct] = True
+    norm = torch.zeros(2, device=DEV)
+    tl = lg.TensorList([norms])
+    ws = torch.empty(lg.longer_grad_norm_workspace_bytes(tl), dtype=torch.uint8, device=DEV)
+    for max_norm, step in ((None, 1), (1e-3, 2), (1e9, 1000)):
+        if max_norm is not None:
+            lg.longer_grad_norm(tl, max_norm, norm, ws)
+            exact = float(np.sqrt((np64(norms) ** 2).sum()))
+            assert abs(float(norm[0]) - exact) <= 2 * U * exact
+        a, b = [t.clone() for t in start], [t.clone() for t in start]
+        wa = None if weights == "none" else torch.full((R, d), -5.0, dtype=TYPES[weights], device=DEV)
+        wb = None if wa is None else wa.clone()
+        how = (1e-2, 0.9, 0.999, 1e-8, step)
+        lg.longer_adamw_rows(lg.AdamWRows(*a, wa, 0.1), o, compact, None if max_norm is None else norm, *how)
+        lg.longer_adamw_step(lg.AdamWList(*[[t] for t in b], [dense], None if wb is None else [wb], [0.1]), None if max_norm is None else norm, *how)
+        for x, y, s in zip(a, b, start):
+            assert torch.equal(x[hit], y[hit]) and torch.equal(x[~hit], s[~hit])
+        if wa is not None:
+            assert torch.equal(wa[hit], wb[hit]) and bool((wa[~hit] == -5.0).all())
+    norm.copy_(torch.tensor([float("nan"), 0.0]))                                       # a dropped batch
+    a = [t.clone() for t in start]
+    lg.longer_adamw_rows(lg.AdamWRows(*a, None, 0.1), o, compact, norm, *how)
+    assert all(torch.equal(x, s) for x, s in zip(a, start))
+
+
+def test_a_table_beyond_2_to_the_31_values():
+    R, d, B, L = 17_000_011, 128, 2, 600
+    table = torch.zeros(R, d, dtype=torch.bfloat16, device=DEV)
+    r = np.random.default_rng(3)
+    ids = r.integers(R - 500, R, (B, L))
+    ids[0, :3] = (0, (1 << 31) // d, R - 1)
+    uniq = torch.from_numpy(np.unique(ids)).to(DEV)
+    table[uniq] = torch.randn(len(uniq), d, device=DEV).to(torch.bfloat16)
+    out = torch.empty(B, L, d, dtype=torch.bfloat16, device=DEV)
+    lg.longer_embedding(table, on_gpu(ids), None, 1.0, None, out)
+    assert torch.equal(out, table[torch.from_numpy(ids).to(DEV)])
+    del table
+    o, _ = sort(ids, torch.int64, 1, None, R)
+    de = torch.randn(B, L, d, device=DEV)
+    compact, norms, _ = backward(o, de, 1.0, None, False, R)
+    distinct, g, mag, count = gradient(ids, None, R, np64(de), 1.0)
+    assert (np.abs(np64(compact)[:len(distinct)] - g) <= mag * (count[:, None] + 3) * U).all()
+    ws = torch.empty(lg.longer_embedding_backward_workspace_bytes(B, L, d), dtype=torch.uint8, device=DEV)
+    dense, n2 = torch.empty(R, d, device=DEV), torch.empty(R, device=DEV)
+    lg.longer_embedding_backward(o, de, 1.0, None, True, dense, n2, ws)
+    assert torch.equal(dense[uniq], compact[:len(uniq)]) and torch.equal(n2[uniq], norms[:len(uniq)])
+    assert int((n2 != 0).sum()) == len(uniq)
+    p, m = dense, torch.zeros(R, d, device=DEV)
+    v = torch.zeros(R, d, device=DEV)
+    old = p[uniq].clone()
+    lg.longer_adamw_rows(lg.AdamWRows(p, m, v, None, 0.0), o, compact, None, 1e-2, 0.9, 0.99, 1e-8, 1)
+    assert torch.equal(m[uniq], compact[:len(uniq)] * np.float32(1 - 0.9)) and not torch.equal(p[uniq], old)
+    assert bool((m[1:R - 500][: 1 << 20] == 0).all())
+
+
+def test_rows_beyond_2_to_the_31_values():
+    """E and Y of 2.2 billion values: rows at both ends and on both sides of 2^31."""
+    B, L, d, R = 33, 520_000, 128, 1000
+    assert B * L * d > 1 << 31
+    r = np.random.default_rng(4)
+    table = torch.randn(R, d, device=DEV).to(torch.bfloat16)
+    ids = torch.randint(0, R, (B, L), device=DEV, dtype=torch.int32)
+    drop, f = mask(0.25)
+    E = torch.empty(B, L, d, dtype=torch.bfloat16, device=DEV)
+    lg.longer_embedding(table, ids, None, 1.0, drop, E)
+    at = np.concatenate([[0, 1, (1 << 31) // d - 1, (1 << 31) // d, B * L - 1], r.integers(0, B * L, 500)])
+    k, i = f(at, d), torch.from_numpy(at).to(DEV)
+    t = np64(table)[ids.reshape(-1)[i].cpu().numpy()]
+    rows = np64(E.reshape(-1, d)[i])
+    assert (np.abs(rows - k * t) <= np.abs(k * t) * (2.0 ** -8 + 3 * U)).all()
+    lg.longer_embedding(table, ids, None, 1.0, None, E)
+    lg.longer_dropout(E, None, None, drop, E)
+    assert np.array_equal(np64(E.reshape(-1, d)[i]), rows)
+
+
+def step_of(B, L, d, R, seed):
+    """The run of the operators as a training step has it, on buffers that stay: returns the step and what it writes."""
+    r = np.random.default_rng(seed)
+    table = (torch.from_numpy(r.standard_normal((R, d))) * 0.05).float().to(DEV)
+    ids, lens = on_gpu(draw_ids(r, B, L, R, "popular"), torch.int32), lengths(r, B, L, "ragged")[1]
+    key = torch.tensor([12345, 0], dtype=torch.int64, device=DEV)
+    drop_e, drop_h = lg.DropoutMask(0.1, key, 0), lg.DropoutMask(0.2, key, 1)
+    state = [table, torch.zeros_like(table), torch.zeros_like(table), table.to(torch.bfloat16)]
+    E = torch.empty(B, L, d, dtype=torch.bfloat16, device=DEV)
+    H, W = torch.empty(B, L, d, dtype=torch.bfloat16, device=DEV), torch.from_numpy(r.standard_normal((B, L, d))).float().to(DEV)
+    dE, norm = torch.empty(B, L, d, device=DEV), torch.empty(2, device=DEV)
+    n = min(B * L, R)
+    o, g, norms = lg.TokenOrder.empty(B, L, R, DEV), torch.zeros(n, d, device=DEV), torch.empty(n, device=DEV)
+    tl = lg.TensorList([norms])
+    scratch = lambda k: torch.empty(k, dtype=torch.uint8, device=DEV)
+    w0, w1, w2 = scratch(lg.longer_sort_ids_workspace_bytes(B, L, R)), scratch(lg.longer_embedding_backward_workspace_bytes(B, L, d)), scratch(lg.longer_grad_norm_workspace_bytes(tl))
+    params = lg.AdamWRows(*state, 0.01)
+
+    def gradients(stream=None):
+        lg.longer_embedding(state[3], ids, lens, 8.0, drop_e, E, stream=stream)
+        lg.longer_dropout(E, None, lens, drop_h, H, stream=stream)
+        lg.longer_dropout(W, None, lens, drop_h, dE, stream=stream)                      # the loss is sum(H W)
+        lg.longer_sort_ids(ids, lens, R, o, w0, stream=stream)
+        lg.longer_embedding_backward(o, dE, 8.0, drop_e, False, g, norms, w1, stream=stream)
+        lg.longer_grad_norm(tl, 1.0, norm, w2, stream=stream)
+
+    def update(k, stream=None):
+        lg.longer_adamw_rows(params, o, g, norm, 1e-2, 0.9, 0.99, 1e-8, k, stream=stream)
+
+    return gradients, update, key, dict(E=E, H=H, g=g, norms=norms, norm=norm, tokens=o.tokens, p=state[0], m=state[1], v=state[2], w=state[3]), (ids, lens, W, o)
+
+
+def test_a_step_against_autograd():
+    B, L, d, R = 6, 50, 48, 70
+    gradients, update, key, out, (ids, lens, W, o) = step_of(B, L, d, R, 1)
+    for t in out.values():
+        t.zero_() if t.dtype == torch.int32 else None
+    gradients()
+    there = torch.from_numpy(named(ids.cpu().numpy(), lens.cpu().numpy(), R)).to(DEV)
+    f = [torch.from_numpy(factors(np.arange(B * L), d, p, 12345, 0, site)).to(DEV).view(B, L, d) for p, site in ((0.1, 0), (0.2, 1))]
+    w = out["w"].double().requires_grad_()
+    H = torch.where(there[..., None], w[ids.long().masked_fill(~there, 0)] * 8.0 * f[0] * f[1], 0.0)
+    G, = torch.autograd.grad((H * W.double()).sum(), w)
+    count, n = o.counts.tolist()
+    named_rows = o.rows[:count].long()
+    _, _, mag, terms = gradient(ids.cpu().numpy(), lens.cpu().numpy(), R, np64(W) * np64(f[1]), 8.0, np64(f[0]).reshape(-1, d))
+    off = np.abs(np64(out["g"])[:count] - np64(G[named_rows]))
+    assert (off <= mag * (terms[:, None] + 5) * U + TINY).all()                           # (dE adds the mask's two roundings)
+    assert int((G.abs().sum(1) != 0).sum()) <= count
+    assert (np.abs(np64(out["H"]) - np64(H.detach())) <= np.abs(np64(H.detach())) * (2 * 2.0 ** -8 * 1.01 + 6 * U)).all()
+    norm = float(G.norm())
+    assert abs(float(out["norm"][0]) - norm) <= 400 * U * norm
+    p0 = out["p"].double().clone()
+    update(1)
+    c = min(1.0, 1 / norm)
+    gi = c * G[named_rows]
+    want = p0[named_rows] - 1e-2 * (gi / (gi.abs() + 1e-8) + 0.01 * p0[named_rows])
+    big = gi.abs() > 1e-4                                                                 # (where a gradient nearly cancels its quotient keeps the sign alone)
+    assert bool(((out["p"].double()[named_rows] - want).abs() <= 1e-7)[big].all())
+
+
+@pytest.mark.parametrize("shape", [(6, 50, 48, 70), (40, 700, 64, 5000)])
+def test_a_step_on_another_stream_and_in_a_graph(shape):
+    """Steps, each with the next step's masks: eager, on another stream, and replayed from a graph with eager work between the replays; two
+    graphs of two models in turn."""
+    runs = [step_of(*shape, seed) for seed in (1, 2)]
+    start = [{k: v.clone() for k, v in run[3].items()} for run in runs]
+
+    def back():
+        for run, s in zip(runs, start):
+            run[2].copy_(torch.tensor([12345, 0]))
+            for k, v in run[3].items():
+                v.copy_(s[k])
+
+    def eager(stream=None):
+        kept = []
+        for step in range(1, 4):
+            for gradients, update, key, out, _ in runs:
+                gradients(stream)
+                update(step, stream)
+                if stream is not None:
+                    with torch.cuda.stream(stream):
+                        key[1] += 1
+                        kept.append({k: v.clone() for k, v in out.items()})
+                else:
+                    key[1] += 1
+                    kept.append({k: v.clone() for k, v in out.items()})
+        return kept
+
+    for t in (x for run in runs for x in (run[3]["E"], run[3]["H"])):
+        t.zero_()
+    for run in runs:
+        run[3]["tokens"].fill_(-1)
+    start = [{k: v.clone() for k, v in run[3].items()} for run in runs]
+    back()
+    want = eager()
+    assert not torch.equal(want[0]["E"], want[2]["E"])                                    # another mask, and other weights
+    back()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = eager(s)
+    torch.cuda.synchronize()
+    same = lambda a, b: all(torch.equal(a[k], b[k]) or bool((a[k].isnan() == b[k].isnan()).all() and torch.equal(a[k].nan_to_num(), b[k].nan_to_num())) for k in a)
+    assert all(same(a, b) for a, b in zip(got, want))
+    back()
+    graphs = []
+    for run in runs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run[0]()
+            run[2][1:].add_(1)
+        graphs.append(graph)
+    back()
+    at = 0
+    for step in range(1, 4):
+        for (gradients, update, key, out, _), graph in zip(runs, graphs):
+            out["norms"].fill_(9.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            update(step)
+            assert same({k: v for k, v in out.items()}, want[at]), (step, at)
+            at += 1
+
+
+def test_python_calls_refuse():
+    t, ids = torch.zeros(9, 8, device=DEV), torch.zeros(2, 3, dtype=torch.int64, device=DEV)
+    E, key = torch.zeros(2, 3, 8, device=DEV), torch.zeros(2, dtype=torch.int64, device=DEV)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    o = lg.TokenOrder.empty(2, 3, 9, DEV)
+    drop = lg.DropoutMask(0.1, key)
+    bad = [lambda: lg.DropoutMask(1.0, key), lambda: lg.DropoutMask(0.1, key.int()), lambda: lg.DropoutMask(0.1, key[:1]), lambda: lg.DropoutMask(0.1, key, 70000),
+           lambda: lg.longer_embedding(t, ids.float(), None, 1.0, None, E), lambda: lg.longer_embedding(t, ids[0], None, 1.0, None, E),
+           lambda: lg.longer_embedding(t.half(), ids, None, 1.0, None, E), lambda: lg.longer_embedding(t[:, ::2], ids, None, 1.0, None, E[..., :4]),
+           lambda: lg.longer_embedding(t, ids, None, 1.0, None, E[..., :4]), lambda: lg.longer_embedding(t, ids, ids[0], 1.0, None, E),
+           lambda: lg.longer_embedding(t.cpu(), ids, None, 1.0, None, E), lambda: lg.longer_dropout(E, E[:1], None, drop, E), lambda: lg.longer_dropout(E, None, None, drop, E.bfloat16()),
+           lambda: lg.longer_sort_ids(ids.expand(2, 3).repeat(1, 9), None, 9, o, ws), lambda: lg.longer_sort_ids(ids, None, 0, o, ws),
+           lambda: lg.longer_embedding_backward(o, E, 1.0, None, False, t[:5], None, ws), lambda: lg.longer_embedding_backward(o, E, 1.0, None, True, t, t[0], ws),
+           lambda: lg.longer_embedding_backward(o, E, 1.0, None, True, t.bfloat16(), None, ws), lambda: lg.longer_embedding_backward(o, E, 1.0, None, True, t[:, :4], None, ws),
+           lambda: lg.AdamWRows(t, t.clone(), t[:5].clone(), None, 0.0), lambda: lg.AdamWRows(t, t.clone(), t.bfloat16(), None, 0.0),
+           lambda: lg.longer_adamw_rows(lg.AdamWRows(t, t.clone(), t.clone(), None, 0.0), o, t[:3], None, 1e-3, 0.9, 0.99, 1e-8, 1),
+           lambda: lg.longer_adamw_rows(lg.AdamWRows(t, t.clone(), t.clone(), None, 0.0), o, t.clone(), None, 1e-3, 0.9, 0.99, 1e-8, 0)]
+    for call in bad:
+        with pytest.raises(lg.LongerError):
+            call()
