@@ -227,6 +227,8 @@ def _library(s):
         s["ws_sort"] = scratch(lg.longer_sort_ids_workspace_bytes(B, L, case["table"]))
         s["ws"] = scratch(lg.longer_embedding_backward_workspace_bytes(B, L, d))
     if case["op"] == "rows":
+        if s["w"] is s["p"]:                             # fp32 copies are a buffer of their own
+            s["w"] = s["p"].clone()
         s["params"] = lg.AdamWRows(s["p"], s["m"], s["v"], s["w"], DECAY)
         s["list"] = lg.TensorList([s["norms"]])
         s["ws"] = scratch(lg.longer_grad_norm_workspace_bytes(s["list"]))
