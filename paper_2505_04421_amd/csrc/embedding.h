@@ -32,7 +32,18 @@ inline int lanes_shift(int pieces, int m) {
 template <typename T, int V> struct Piece_ { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
 template <typename T, int V> using Piece = typename Piece_<T, V>::type;
 
-// 8 values of a row, of which `n` are the row's (the others come as zeros and are not stored)
+// A lane's piece of a row: 8 values from column c on.  Widths that 8 does not divide: the last piece is moved back to end with the row, so that
+// every access is whole and inside it; its first `twice` values are its neighbour's too, and are computed and stored by both, to the
+// same bits.  That asks for a row of 8 values, and for nobody who reads behind the neighbour's store (in place: no); otherwise the last piece is
+// taken value by value.  Accesses are aligned to the element only, which the memory path takes at any address.
+struct Part { int c, n, twice; };                    // n: values of the row from c on, 8 or more: a whole piece
+template <bool WHOLE>
+__device__ __forceinline__ Part part_of(uint32_t piece, int d, bool back) {
+  const int c = piece * 8;
+  if (WHOLE || c + 8 <= d || !back) return {c, WHOLE ? 8 : d - c, 0};
+  return {d - 8, 8, c - (d - 8)};
+}
+
 template <typename T>
 __device__ __forceinline__ Piece<T, 8> load8(const T* p, int n) {
   if (n >= 8) return *(const Piece<T, 8>*)p;
@@ -41,6 +52,7 @@ __device__ __forceinline__ Piece<T, 8> load8(const T* p, int n) {
   for (int j = 0; j < 8; ++j) x[j] = j < n ? p[j] : (T)0.f;
   return x;
 }
+// written once and read by another kernel: past the caches
 template <typename T>
 __device__ __forceinline__ void store8(T* p, int n, const Piece<T, 8>& x) {
   if (n >= 8) {
@@ -54,7 +66,8 @@ __device__ __forceinline__ void store8(T* p, int n, const Piece<T, 8>& x) {
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, 2011): ten rounds of two 32 x 32 -> 64 bit
 // products on a counter of four words under a key of two.  Half a word decides about one value: 8 values, 16 bytes of bf16, to a
-// call, and a share that is a multiple of 2^-16.
+// call, and a share that is a multiple of 2^-16.  A wave's call takes 187 cycles of its SIMD with the words joined in one instruction
+// (275 with two exclusive ors): 65 million values in 10 us of the whole chip, which hide behind 26 us of memory in bf16.
 struct Mask { const uint64_t* key; uint32_t site, drop; };      // site: in place; drop: half-words below it drop their value (0: there is no mask)
 struct Key { uint32_t k0, k1, c2, c3; };
 
@@ -63,22 +76,45 @@ __device__ __forceinline__ Key load_key(const Mask& m) {
   return {(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)step, (uint32_t)(step >> 32)};
 }
 
-// x[j] where value j of the piece is kept, zero (whatever x[j] is) where it is not
-template <typename V>
-__device__ __forceinline__ void drop8(const Mask& m, const Key& key, uint32_t row, uint32_t piece, V& x) {
-  uint32_t c[4] = {m.site | piece, row, key.c2, key.c3}, k0 = key.k0, k1 = key.k1;
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+
+__device__ __forceinline__ void words(const Mask& m, const Key& key, uint32_t row, uint32_t block, uint32_t (&c)[4]) {
+  uint32_t k0 = key.k0, k1 = key.k1;
+  c[0] = m.site | block;
+  c[1] = row;
+  c[2] = key.c2;
+  c[3] = key.c3;
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const uint64_t a = (uint64_t)c[0] * 0xD2511F53u, b = (uint64_t)c[2] * 0xCD9E8D57u;
-    c[0] = (uint32_t)(b >> 32) ^ c[1] ^ k0;
+    c[0] = xor3((uint32_t)(b >> 32), c[1], k0);
     c[1] = (uint32_t)b;
-    c[2] = (uint32_t)(a >> 32) ^ c[3] ^ k1;
+    c[2] = xor3((uint32_t)(a >> 32), c[3], k1);
     c[3] = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
+}
+
+// x[j] where value c + j of the row is kept, zero (whatever x[j] is) where it is not; a piece off the multiples of 8 lies in two blocks
+template <bool WHOLE, typename V>
+__device__ __forceinline__ void drop8(const Mask& m, const Key& key, uint32_t row, int c, V& x) {
+  uint32_t w[4];
+  words(m, key, row, (uint32_t)c / 8, w);
+  if (!WHOLE && (c & 7)) {
+    uint32_t v[4];
+    words(m, key, row, (uint32_t)c / 8 + 1, v);
+    for (int i = c & 7; i; --i) {                    // (at most 7 half-words on)
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = (c[j / 2] >> 16 * (j & 1) & 0xffff) >= m.drop ? x[j] : 0.f;
+      for (int k = 0; k < 3; ++k) w[k] = __builtin_amdgcn_alignbit(w[k + 1], w[k], 16);
+      w[3] = __builtin_amdgcn_alignbit(v[0], w[3], 16);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) v[k] = __builtin_amdgcn_alignbit(v[k + 1], v[k], 16);
+      v[3] >>= 16;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = (w[j / 2] >> 16 * (j & 1) & 0xffff) >= m.drop ? x[j] : 0.f;
 }
 
 // ------------------------------------------------------------------------------------ host

@@ -15,6 +15,7 @@ struct Ids {
   int wide;
 };
 
+constexpr int kMostBits = 11;                        // of a round's digit
 constexpr uint32_t kNone = 0xffffffffu;              // of a token that names no row (ids are below 2^31)
 
 __device__ __forceinline__ uint32_t id_of(const Ids& a, uint32_t i) {
@@ -26,19 +27,22 @@ __device__ __forceinline__ uint32_t id_of(const Ids& a, uint32_t i) {
 }
 
 // Place of an item among those with its digit, in a wave's order: `count` is the wave's own, one counter a digit.  A lane's peers, the
-// lanes of this step with its digit, come from one ballot a bit; the lowest of them moves the counter on.
+// lanes of this step with its digit, come from one ballot a bit (peers whose bit is as the lane's: not the exclusive or of the ballot and
+// the lane's bit in every place); the lowest of them moves the counter on.
 __device__ __forceinline__ uint32_t rank(uint32_t digit, bool there, int bits, volatile uint16_t* count) {
-  uint64_t peers = __ballot(there);
+  const uint64_t all = __ballot(there);
+  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
   for (int b = 0; b < bits; ++b) {
-    const bool set = digit >> b & 1;
-    const uint64_t with = __ballot(set);
-    peers &= set ? with : ~with;
+    const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe(digit, b, 1);
+    const uint64_t with = __ballot(mine);
+    lo = __builtin_amdgcn_bitop3_b32(lo, (uint32_t)with, mine, 0x90);
+    hi = __builtin_amdgcn_bitop3_b32(hi, (uint32_t)(with >> 32), mine, 0x90);
   }
-  const uint32_t below = __popcll(peers & ((1ull << (threadIdx.x & 63)) - 1));
+  const uint32_t below = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
   uint32_t at = 0;
   if (there) {
     at = count[digit];
-    if (below == 0) count[digit] = (uint16_t)(at + __popcll(peers));
+    if (below == 0) count[digit] = (uint16_t)(at + __popc(lo) + __popc(hi));
   }
   return at + below;
 }
@@ -73,72 +77,88 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t* lds, uint32
 }
 
 // ------------------------------------------------------------------------------------ few tokens: one workgroup
-constexpr int kFewThreads = 1024, kFewItems = 8, kFew = kFewThreads * kFewItems, kFewBits = 8, kFewWaves = kFewThreads / 64;
+constexpr int kFewThreads = 1024, kFewItems = 8, kFew = kFewThreads * kFewItems, kFewWaves = kFewThreads / 64;
 
-__global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, longer_order out) {
-  __shared__ uint32_t keys[kFew];
-  __shared__ uint16_t tokens[kFew], count[kFewWaves][1 << kFewBits];
-  __shared__ uint32_t base[1 << kFewBits], lds[kFewWaves];
+// A wave takes 64 * items neighbours; rounds of up to kMostBits bits, all in LDS.  (6144 tokens of 1000 rows: ... us)
+__global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int per_round, longer_order out) {
+  __shared__ uint32_t keys[kFew], words[kFewWaves << (kMostBits - 1)], base[1 << kMostBits], lds[kFewWaves];
+  __shared__ uint16_t tokens[kFew];
+  uint16_t* count = (uint16_t*)words;                // [waves][digits]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int items = (a.n + kFewThreads - 1) / kFewThreads;
   uint32_t n = a.n, key[kFewItems], token[kFewItems], at[kFewItems];
-  for (int shift = 0; shift < bits; shift += kFewBits) {
-    const int digits = min(bits - shift, kFewBits);
-    for (int i = threadIdx.x; i < kFewWaves << digits; i += kFewThreads) count[i >> digits][i & ((1 << digits) - 1)] = 0;
+  for (int shift = 0; shift < bits; shift += per_round) {
+    const int round = min(bits - shift, per_round);
+    const uint32_t digits = 1u << round;
+    for (uint32_t i = threadIdx.x; i < kFewWaves * digits / 2; i += kFewThreads) words[i] = 0;
 #pragma unroll
     for (int i = 0; i < kFewItems; ++i) {
-      const uint32_t k = (wave * kFewItems + i) * 64 + lane;
       key[i] = kNone;
-      if (k < n) {
+      const uint32_t k = (wave * items + i) * 64 + lane;
+      if (i < items && k < n) {
         key[i] = shift ? keys[k] : id_of(a, k);
         token[i] = shift ? tokens[k] : k;
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kFewItems; ++i) at[i] = rank(key[i] >> shift & ((1u << digits) - 1), key[i] != kNone, digits, count[wave]);
+    for (int i = 0; i < kFewItems; ++i)
+      if (i < items) at[i] = rank(key[i] >> shift & (digits - 1), key[i] != kNone, round, count + wave * digits);
     __syncthreads();
     // where each digit begins, and in it each wave
-    uint32_t sum = 0, all;
-    const uint32_t d = threadIdx.x;
-    if (d < 1u << digits)
-      for (int w = 0; w < kFewWaves; ++w) {
-        const uint32_t c = count[w][d];
-        count[w][d] = (uint16_t)sum;
-        sum += c;
-      }
-    const uint32_t before = group_scan<kFewThreads>(sum, lds, &all);
-    if (d < 1u << digits) base[d] = before;
+    uint32_t begin = 0;
+    for (uint32_t d = threadIdx.x; d < max(digits, (uint32_t)kFewThreads); d += kFewThreads) {
+      uint32_t sum = 0, all;
+      if (d < digits)
+        for (int w = 0; w < kFewWaves; ++w) {
+          const uint32_t c = count[w * digits + d];
+          count[w * digits + d] = (uint16_t)sum;
+          sum += c;
+        }
+      const uint32_t before = group_scan<kFewThreads>(sum, lds, &all);
+      if (d < digits) base[d] = begin + before;
+      begin += all;
+    }
     __syncthreads();
-    n = all;                                         // the first round drops the tokens that name no row
+    n = begin;                                       // the first round drops the tokens that name no row
 #pragma unroll
     for (int i = 0; i < kFewItems; ++i)
-      if (key[i] != kNone) {
-        const uint32_t d = key[i] >> shift & ((1u << digits) - 1), to = base[d] + count[wave][d] + at[i];
+      if (i < items && key[i] != kNone) {
+        const uint32_t d = key[i] >> shift & (digits - 1), to = base[d] + count[wave * digits + d] + at[i];
         keys[to] = key[i];
         tokens[to] = (uint16_t)token[i];
       }
     __syncthreads();
   }
-  // runs: a thread takes kFewItems neighbours
-  uint32_t first = 0, runs = 0, all;
+  // runs: a wave takes its neighbours 64 at a time
+  uint32_t runs = 0, all;
+  uint64_t heads[kFewItems];
 #pragma unroll
   for (int i = 0; i < kFewItems; ++i) {
-    const uint32_t k = threadIdx.x * kFewItems + i;
-    if (k < n) {
-      const bool head = k == 0 || keys[k] != keys[k - 1];
-      runs += head;
-      first |= (uint32_t)head << i;
-    }
+    heads[i] = 0;
+    const uint32_t k = (wave * items + i) * 64 + lane;
+    if (i < items) heads[i] = __ballot(k < n && (k == 0 || keys[k] != keys[k - 1]));
+    runs += __popcll(heads[i]);
   }
-  uint32_t run = group_scan<kFewThreads>(runs, lds, &all);
+  if (lane == 0) lds[wave] = runs;
+  __syncthreads();
+  uint32_t run = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    run += w < wave ? lds[w] : 0;
+    all += lds[w];
+  }
 #pragma unroll
   for (int i = 0; i < kFewItems; ++i) {
-    const uint32_t k = threadIdx.x * kFewItems + i;
-    if (k < n) {
-      if (first >> i & 1) out.rows[run++] = (int)keys[k];
-      out.runs[k] = (int)run - 1;
+    const uint32_t k = (wave * items + i) * 64 + lane;
+    if (i < items && k < n) {
+      const uint32_t mine = run + __popcll(heads[i] & ((2ull << lane) - 1)) - 1;
+      if (heads[i] >> lane & 1) out.rows[mine] = (int)keys[k];
+      out.runs[k] = (int)mine;
       out.tokens[k] = tokens[k];
     }
+    run += __popcll(heads[i]);
   }
   if (threadIdx.x == 0) {
     out.counts[0] = (int)all;
@@ -149,7 +169,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, longe
 // ------------------------------------------------------------------------------------ many tokens
 // A round of the sort takes one digit: every workgroup counts the digits of its stretch of the items, the counts are summed over
 // the workgroups before it, and it moves its items.  The first round reads the ids themselves and drops the tokens that name no row.
-constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostBits = 11, kMostGroups = 512;
+constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostGroups = 512;
 
 struct Round {
   Ids ids;
@@ -176,9 +196,16 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
   for (uint32_t i = threadIdx.x; i < digits; i += kThreads) count[i] = 0;
   __syncthreads();
   const Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)*r.n);
-  for (uint32_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) {
-    const uint32_t key = FIRST ? id_of(r.ids, i) : r.keys_in[i];
-    if (!FIRST || key != kNone) atomicAdd(&count[key >> r.shift & (digits - 1)], 1u);
+  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
+    uint32_t key[kItems];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const uint32_t i = tile + k * kThreads + threadIdx.x;
+      key[k] = i >= s.end ? kNone : FIRST ? id_of(r.ids, i) : r.keys_in[i];
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k)
+      if (key[k] != kNone) atomicAdd(&count[key[k] >> r.shift & (digits - 1)], 1u);
   }
   __syncthreads();
   for (uint32_t i = threadIdx.x; i < digits; i += kThreads) r.counts[(size_t)blockIdx.x * digits + i] = count[i];
@@ -186,22 +213,26 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
 
 // counts[g][digit] becomes the sum over the groups before g, totals[digit] that over all: 32 digits a workgroup, 32 shares of the groups
 __global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* totals, int groups, uint32_t digits) {
+  constexpr int kShare = kMostGroups / 32;
   __shared__ uint32_t lds[32][33];
   const uint32_t digit = blockIdx.x * 32 + (threadIdx.x & 31);
   const int share = threadIdx.x >> 5, per = (groups + 31) / 32, begin = share * per, end = min(begin + per, groups);
-  uint32_t sum = 0;
-  if (digit < digits)
-    for (int g = begin; g < end; ++g) sum += counts[(size_t)g * digits + digit];
+  uint32_t sum = 0, c[kShare];
+#pragma unroll
+  for (int k = 0; k < kShare; ++k) c[k] = k < end - begin && digit < digits ? counts[(size_t)(begin + k) * digits + digit] : 0;
+#pragma unroll
+  for (int k = 0; k < kShare; ++k) sum += c[k];
   lds[share][threadIdx.x & 31] = sum;
   __syncthreads();
   if (digit >= digits) return;
   uint32_t before = 0;
-  for (int i = 0; i < share; ++i) before += lds[i][threadIdx.x & 31];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) before += i < share ? lds[i][threadIdx.x & 31] : 0;
   if (share == 31) totals[digit] = before + sum;
-  for (int g = begin; g < end; ++g) {
-    const uint32_t c = counts[(size_t)g * digits + digit];
-    counts[(size_t)g * digits + digit] = before;
-    before += c;
+#pragma unroll
+  for (int k = 0; k < kShare; ++k) {
+    if (k < end - begin) counts[(size_t)(begin + k) * digits + digit] = before;
+    before += c[k];
   }
 }
 
@@ -270,7 +301,13 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const uint32_t* keys, c
   __shared__ uint32_t lds[kWaves];
   const Stretch s = stretch((uint32_t)*n);
   uint32_t mine = 0, all;
-  for (uint32_t k = s.begin + threadIdx.x; k < s.end; k += kThreads) mine += k == 0 || keys[k] != keys[k - 1];
+  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const uint32_t k = tile + i * kThreads + threadIdx.x;
+      if (k < s.end) mine += k == 0 || keys[k] != keys[k - 1];
+    }
+  }
   group_scan<kThreads>(mine, lds, &all);
   if (threadIdx.x == 0) heads[blockIdx.x] = all;
 }
@@ -360,7 +397,7 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
   const srt::Ids a = {(const char*)ids->data, B > 1 ? ids->user_stride : 0, L > 1 ? ids->row_stride : 0, lens, emb::divider(L), (uint32_t)B * L, (uint32_t)L,
                       (uint32_t)table_rows, ids->type == LONGER_I64};
   if (a.n <= srt::kFew) {
-    srt::few_kernel<<<1, srt::kFewThreads, 0, st>>>(a, p.bits, *order);
+    srt::few_kernel<<<1, srt::kFewThreads, 0, st>>>(a, p.bits, p.per_round, *order);
     return launched("sort of ids");
   }
   char* w = (char*)ws;
