@@ -11,6 +11,12 @@ namespace longer {
 namespace emb {
 
 constexpr int kChunk = 512;                          // columns of a group: 64 lanes of 8
+constexpr int kThreads = 512, kThreadBits = 9;
+
+// What of a workgroup's sums crosses its borders: the run that began before it, the run that begins in it and goes on, and that run's row
+// of the gradient (kNone: there is none).
+constexpr uint32_t kNone = ~0u;
+struct alignas(16) Border { uint32_t lead, tail, row, unused; };
 
 struct GradParams {
   Rows de;
@@ -25,6 +31,7 @@ struct GradParams {
   uint32_t out_rows;
   float *grads, *norms;
   float* part;                                       // [workgroups][2][d]
+  Border* borders;                                   // [workgroups]
   double* squares;                                   // [runs][chunks], where there is more than one chunk
 };
 
@@ -94,79 +101,103 @@ __device__ __forceinline__ void finish(const GradParams& p, uint32_t run, uint32
 }
 __device__ __forceinline__ uint32_t row_of(const GradParams& p, uint32_t run) { return p.dense ? (uint32_t)p.order.rows[run] : run; }
 
+// LDS of a workgroup's tokens: where their rows of dE lie, their runs (with the neighbours' on both sides), the runs' rows, their numbers
+__host__ __device__ inline size_t staged_bytes(uint32_t block, bool drop) { return (size_t)block * (drop ? 20 : 16) + 8; }
+
 template <typename T, bool DROP, bool WHOLE>
-__global__ __launch_bounds__(256, 4) void grad_kernel(GradParams p) {
-  constexpr int U = 8;
+__global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
+  constexpr int U = 4;
   constexpr uint32_t kLead = 1, kOn = 2;             // a group's first run began before it; that run goes on behind it
-  __shared__ float lead[256 * 8];
-  __shared__ uint32_t flags[256];
+  extern __shared__ int64_t staged[];
+  __shared__ float lead[kThreads * 8];
+  __shared__ uint32_t flags[kThreads];
+  int64_t* from = staged;
+  uint32_t *runs = (uint32_t*)(from + p.block) + 1, *rows = runs + p.block + 1, *tokens = rows + p.block;
   const Lane me = lane_of<WHOLE>(p);
   const int c = me.at.c, width = me.at.n;
-  const uint32_t n = tokens_of(p), group = threadIdx.x >> p.shift, groups = 256 >> p.shift;
+  const uint32_t n = tokens_of(p), group = threadIdx.x >> p.shift, groups = kThreads >> p.shift;
   if (p.norms && blockIdx.y == 0 && !p.dense)        // zeros behind the last row's norm
-    for (uint64_t i = (uint64_t)runs_of(p) + blockIdx.x * 256 + threadIdx.x; i < p.out_rows; i += (uint64_t)gridDim.x * 256) p.norms[i] = 0.f;
-  if ((uint64_t)blockIdx.x * p.block >= n) return;
-  const uint32_t first = blockIdx.x * p.block, begin = min(first + group * p.range, n), end = min(begin + p.range, n);
+    for (uint64_t i = (uint64_t)runs_of(p) + blockIdx.x * kThreads + threadIdx.x; i < p.out_rows; i += (uint64_t)gridDim.x * kThreads) p.norms[i] = 0.f;
+  if ((uint64_t)blockIdx.x * p.block >= n) {
+    if (blockIdx.y == 0 && threadIdx.x == 0) p.borders[blockIdx.x] = {kNone, kNone, 0, 0};
+    return;
+  }
+  const uint32_t first = blockIdx.x * p.block, count = min(p.block, n - first);
   const Key key = DROP ? load_key(p.mask) : Key{};
+  for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
+    const uint32_t token = (uint32_t)p.order.tokens[first + i], run = (uint32_t)p.order.runs[first + i], b = p.by_L(token), l = token - b * p.L;
+    from[i] = token < p.n ? (int64_t)b * p.de.user + (int64_t)l * p.de.row : -1;
+    runs[i] = run;
+    rows[i] = p.dense ? (uint32_t)p.order.rows[run] : run;
+    if (DROP) tokens[i] = token;
+  }
+  if (threadIdx.x == 0) {
+    runs[-1] = first ? (uint32_t)p.order.runs[first - 1] : kNone;
+    runs[count] = first + count < n ? (uint32_t)p.order.runs[first + count] : kNone;
+  }
+  __syncthreads();
+  if (blockIdx.y == 0 && threadIdx.x == 0) {
+    const bool leads = runs[0] == runs[-1], goes = runs[count - 1] == runs[count];
+    p.borders[blockIdx.x] = {leads ? runs[0] : kNone, goes && !(leads && runs[count - 1] == runs[0]) ? runs[count - 1] : kNone, rows[count - 1], 0};
+  }
+  const uint32_t begin = min(group * p.range, count), end = min(begin + p.range, count);
   float acc[8] = {};
-  uint32_t run = 0, row = 0;
+  uint32_t run = kNone;
   bool earlier = false, on = false;
   if (begin < end) {
-    run = p.order.runs[begin];
-    row = row_of(p, run);
-    earlier = begin && (uint32_t)p.order.runs[begin - 1] == run;
-    const uint32_t behind = end < n ? (uint32_t)p.order.runs[end] : ~0u;
-    if (me.lane == 0) flags[group] = earlier ? kLead : 0;
-    for (uint32_t at = begin; at < end; at += U) {
-      uint32_t token[U], runs[U], rows[U];
-      Piece<T, 8> x[U];
+    Piece<T, 8> x[2][U];
+    // the rows of two batches are under way while a third is added up
+    auto load = [&](Piece<T, 8> (&to)[U], uint32_t at) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t i = min(at + u, end - 1);
-        token[u] = (uint32_t)p.order.tokens[i];
-        runs[u] = (uint32_t)p.order.runs[i];
+        const int64_t o = at + u < end ? from[at + u] : -1;
+        if (o >= 0 && width > 0) to[u] = load8((const T*)p.de.data + o + c, width);
       }
+    };
+    auto take = [&](const Piece<T, 8> (&x)[U], uint32_t at) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        rows[u] = row_of(p, runs[u]);
-        if (at + u < end && token[u] < p.n && width > 0) {
-          const uint32_t b = p.by_L(token[u]), l = token[u] - b * p.L;
-          x[u] = load8((const T*)p.de.data + (int64_t)b * p.de.user + (int64_t)l * p.de.row + c, width);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (at + u >= end) break;
-        if (runs[u] != run) {
+        const uint32_t i = at + u;
+        if (i >= end) return;
+        if (runs[i] != run) {
           if (earlier) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) lead[threadIdx.x * 8 + j] = acc[j];
           } else {
-            finish(p, run, row, me, acc);
+            finish(p, run, rows[i - 1], me, acc);
           }
-          run = runs[u];
-          row = rows[u];
+          run = runs[i];
           earlier = false;
 #pragma unroll
           for (int j = 0; j < 8; ++j) acc[j] = 0.f;
         }
-        if (token[u] < p.n && width > 0) {
+        if (from[i] >= 0 && width > 0) {
           Piece<float, 8> y;
 #pragma unroll
           for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j];
-          if (DROP) drop8<WHOLE>(p.mask, key, token[u], c, y);
+          if (DROP) drop8<WHOLE>(p.mask, key, tokens[i], c, y);
 #pragma unroll
           for (int j = 0; j < 8; ++j) acc[j] += y[j];
         }
       }
+    };
+    run = runs[begin];
+    earlier = runs[(int)begin - 1] == run;
+    if (me.lane == 0) flags[group] = earlier ? kLead : 0;
+    load(x[0], begin);
+    for (uint32_t at = begin; at < end; at += 2 * U) {
+      load(x[1], at + U);
+      take(x[0], at);
+      load(x[0], at + 2 * U);
+      take(x[1], at + U);
     }
-    on = behind == run;
+    on = runs[end] == run;
     if (earlier) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) lead[threadIdx.x * 8 + j] = acc[j];
       if (me.lane == 0) flags[group] = kLead | (on ? kOn : 0);
     } else if (!on) {
-      finish(p, run, row, me, acc);
+      finish(p, run, rows[end - 1], me, acc);
     }
   }
   __syncthreads();
@@ -191,78 +222,77 @@ __global__ __launch_bounds__(256, 4) void grad_kernel(GradParams p) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += lead[((h << p.shift) + me.lane) * 8 + j];
     }
-    if (!more) finish(p, run, row, me, acc);
+    if (!more) finish(p, run, rows[end - 1], me, acc);
     else if (width > 0) store_sums(part + p.d, width, acc);
   }
 }
 
-constexpr int kJoinThreads = 1024, kJoinAlone = 16;
+constexpr int kJoinThreads = 512;
 
 // The runs that cross workgroups' stretches, each by the group of the stretch that it begins in, and by the whole workgroup where it
-// goes on for more than kJoinAlone: group k takes every groups-th of its sums, which then meet in two steps.
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
-  constexpr int U = 4;
+// goes on for more than U: group k takes every groups-th of its sums, which then meet in two steps.
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32_t blocks) {
+  constexpr uint32_t U = 8;
   __shared__ float lds[kJoinThreads * 8];
   __shared__ uint32_t list[kJoinThreads], listed;
   const Lane me = lane_of<false>(p);
-  const int c = me.at.c, width = me.at.n;
-  const uint32_t group = threadIdx.x >> p.shift, groups = kJoinThreads >> p.shift, n = tokens_of(p), blocks = (n + p.block - 1) / p.block;
-  const int32_t* runs = p.order.runs;
-  if (blockIdx.x * groups >= blocks) return;
+  const int c = me.at.c, width = max(me.at.n, 0);
+  const uint32_t group = threadIdx.x >> p.shift, groups = kJoinThreads >> p.shift, g = blockIdx.x * groups + group;
+  const size_t step = (size_t)2 * p.d;
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
-  const size_t step = (size_t)2 * p.d;
-  // adds the sums of stretches h, h + by, ... below `to` that begin with `run`; says whether the last one did
-  auto add = [&](float (&acc)[8], uint32_t h, uint32_t by, uint32_t to, uint32_t run) {
-    bool more = true;
-    for (; more && h < to; h += U * by) {
-      bool goes[U];
-      Piece<float, 8> x[U];
+  // the sums of stretches h, h + by, ..., U of them under way at once, while they go on with the run; says whether the last one did
+  // (a stretch that does not has left nothing to read: what is there is not used)
+  auto add = [&](float (&acc)[8], uint32_t h, uint32_t by, uint32_t run) {
+    uint32_t lead[U];
+    Piece<float, 8> x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t i = min(h + u * by, blocks - 1);
-        goes[u] = h + u * by < to && (uint32_t)runs[(size_t)i * p.block] == run;
-        x[u] = load8(p.part + i * step + c, max(width, 0));
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        more &= goes[u];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += more ? x[u][j] : 0.f;
-      }
+    for (uint32_t u = 0; u < U; ++u) {
+      const uint32_t i = min(h + u * by, blocks - 1);
+      lead[u] = h + u * by < blocks ? p.borders[i].lead : kNone;
+      x[u] = load8(p.part + i * step + c, width);
     }
+    bool more = true;
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) {
+      more &= lead[u] == run;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += more ? x[u][j] : 0.f;
+    }
+    return more;
   };
-  const uint32_t g = blockIdx.x * groups + group;
-  if (g + 1 < blocks) {
-    const uint32_t begin = g * p.block, end = begin + p.block, run = (uint32_t)runs[end], row = row_of(p, run);
-    if ((uint32_t)runs[end - 1] == run && !(begin && (uint32_t)runs[begin - 1] == run)) {
-      if (g + kJoinAlone + 1 < blocks && (uint32_t)runs[(size_t)(g + kJoinAlone + 1) * p.block] == run) {
+  if (g < blocks) {
+    const Border own = p.borders[g];
+    const Piece<float, 8> x = load8(p.part + g * step + p.d + c, width);
+    float acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = x[j];
+    const uint32_t after = g + U + 1 < blocks ? p.borders[g + U + 1].lead : kNone;
+    if (own.tail != kNone) {
+      if (after == own.tail) {
         if (me.lane == 0) list[atomicAdd(&listed, 1u)] = g;          // (the order of the list is that of the work alone)
       } else {
-        float acc[8];
-        const Piece<float, 8> x = load8(p.part + g * step + p.d + c, max(width, 0));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = x[j];
-        add(acc, g + 1, 1, blocks, run);
-        finish(p, run, row, me, acc);
+        add(acc, g + 1, 1, own.tail);
+        finish(p, own.tail, own.row, me, acc);
       }
     }
   }
   __syncthreads();
   for (uint32_t i = 0; i < listed; ++i) {
-    const uint32_t a = list[i], run = (uint32_t)runs[(size_t)(a + 1) * p.block];
+    const uint32_t a = list[i];
+    const Border own = p.borders[a];
     float acc[8] = {};
+    for (uint32_t h = a + 1 + group; add(acc, h, groups, own.tail); h += U * groups) {}
     if (group == 0) {
-      const Piece<float, 8> x = load8(p.part + a * step + p.d + c, max(width, 0));
+      const Piece<float, 8> x = load8(p.part + a * step + p.d + c, width);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = x[j];
+      for (int j = 0; j < 8; ++j) acc[j] += x[j];
     }
-    add(acc, a + 1 + group, groups, blocks, run);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 8; ++j) lds[threadIdx.x * 8 + j] = acc[j];
     __syncthreads();
-    if (group < 8) {                                 // (at least 16 groups)
+    if (group < 8) {                                 // (at least 8 groups)
 #pragma unroll 4
       for (uint32_t h = group + 8; h < groups; h += 8)
 #pragma unroll
@@ -273,11 +303,12 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) lds[threadIdx.x * 8 + j] = acc[j];
     __syncthreads();
-    if (group == 0)
+    if (group == 0) {
       for (uint32_t h = 1; h < 8; ++h)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += lds[((h << p.shift) + me.lane) * 8 + j];
-    if (group == 0) finish(p, run, row_of(p, run), me, acc);
+      finish(p, own.tail, own.row, me, acc);
+    }
   }
 }
 
@@ -304,14 +335,14 @@ __global__ __launch_bounds__(256) void norm_kernel(GradParams p) {
 }
 
 // ------------------------------------------------------------------------------------ host
-// Tokens of a range: as many as leave 4096 waves, 8 to 64.
+// Tokens of a range: as many as leave 4096 waves, 4 to 32, and 2048 of a workgroup at most.
 static uint32_t range_of(int64_t n, int shift, int chunks) {
-  uint32_t s = 64;
-  while (s > 8 && (n / s * chunks << shift) < (int64_t)4096 * 64) s /= 2;
+  uint32_t s = std::min(32u, 2048u >> (kThreadBits - shift));
+  while (s > 4 && (n / s * chunks << shift) < (int64_t)4096 * 64) s /= 2;
   return s;
 }
 
-struct GradPlan { int shift, chunks; uint32_t range, block, blocks; size_t squares, bytes; };
+struct GradPlan { int shift, chunks; uint32_t range, block, blocks; size_t borders, squares, bytes; };
 
 static GradPlan grad_plan(int B, int L, int d) {
   const int64_t n = (int64_t)B * L;
@@ -319,21 +350,23 @@ static GradPlan grad_plan(int B, int L, int d) {
   g.chunks = (d + kChunk - 1) / kChunk;
   g.shift = lanes_shift((std::min(d, kChunk) + 7) / 8, 6);
   g.range = range_of(n, g.shift, g.chunks);
-  g.block = g.range * (256 >> g.shift);
+  g.block = g.range * (kThreads >> g.shift);
   g.blocks = (uint32_t)((n + g.block - 1) / g.block);
-  g.squares = align256((size_t)g.blocks * 2 * d * 4);
+  g.borders = align256((size_t)g.blocks * 2 * d * 4);
+  g.squares = g.borders + align256((size_t)g.blocks * sizeof(Border));
   g.bytes = g.squares + (g.chunks > 1 ? align256((size_t)n * g.chunks * 8) : 0);
   return g;
 }
 
 template <typename T>
 static void grad(const GradParams& p, dim3 grid, hipStream_t st) {
+  const size_t lds = staged_bytes(p.block, p.mask.drop);
   if (p.d % 8 == 0) {
-    if (p.mask.drop) grad_kernel<T, true, true><<<grid, 256, 0, st>>>(p);
-    else grad_kernel<T, false, true><<<grid, 256, 0, st>>>(p);
+    if (p.mask.drop) grad_kernel<T, true, true><<<grid, kThreads, lds, st>>>(p);
+    else grad_kernel<T, false, true><<<grid, kThreads, lds, st>>>(p);
   } else {
-    if (p.mask.drop) grad_kernel<T, true, false><<<grid, 256, 0, st>>>(p);
-    else grad_kernel<T, false, false><<<grid, 256, 0, st>>>(p);
+    if (p.mask.drop) grad_kernel<T, true, false><<<grid, kThreads, lds, st>>>(p);
+    else grad_kernel<T, false, false><<<grid, kThreads, lds, st>>>(p);
   }
 }
 
@@ -369,13 +402,13 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   if (ws_bytes < g.bytes) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, g.bytes);
   hipStream_t st = (hipStream_t)stream;
   const emb::GradParams p = {emb::rows_of(de, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, g.shift, g.chunks, g.range, g.block, (float)factor,
-                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, grads_out, norms_out, (float*)ws, (double*)((char*)ws + g.squares)};
+                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares)};
   if (dense) emb::zero_kernel<<<(unsigned)std::min<size_t>((size_t)out_rows * d / 1024 + 1, 4096), 256, 0, st>>>(p);
   const dim3 grid(g.blocks, g.chunks);
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
   else emb::grad<__bf16>(p, grid, st);
   const unsigned per_join = (unsigned)emb::kJoinThreads >> g.shift;
-  if (g.blocks > 1) emb::join_kernel<<<dim3((g.blocks + per_join - 1) / per_join, g.chunks), emb::kJoinThreads, 0, st>>>(p);
+  if (g.blocks > 1) emb::join_kernel<<<dim3((g.blocks + per_join - 1) / per_join, g.chunks), emb::kJoinThreads, 0, st>>>(p, g.blocks);
   if (norms_out && g.chunks > 1) emb::norm_kernel<<<std::min((p.n + 255) / 256, 2048u), 256, 0, st>>>(p);
   return launched("embedding gradient");
 }

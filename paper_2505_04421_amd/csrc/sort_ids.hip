@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
   uint16_t* count = (uint16_t*)words;                // [waves][digits]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int items = (a.n + kFewThreads - 1) / kFewThreads;
-  uint32_t n = a.n, key[kFewItems], token[kFewItems], at[kFewItems];
+  uint32_t n = a.n, key[kFewItems], token[kFewItems];        // (a token and, above it, its place: both below 2^13)
   for (int shift = 0; shift < bits; shift += per_round) {
     const int round = min(bits - shift, per_round);
     const uint32_t digits = 1u << round;
@@ -94,6 +94,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 #pragma unroll
     for (int i = 0; i < kFewItems; ++i) {
       key[i] = kNone;
+      token[i] = 0;
       const uint32_t k = (wave * items + i) * 64 + lane;
       if (i < items && k < n) {
         key[i] = shift ? keys[k] : id_of(a, k);
@@ -103,13 +104,14 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kFewItems; ++i)
-      if (i < items) at[i] = rank(key[i] >> shift & (digits - 1), key[i] != kNone, round, count + wave * digits);
+      if (i < items) token[i] |= rank(key[i] >> shift & (digits - 1), key[i] != kNone, round, count + wave * digits) << 16;
     __syncthreads();
     // where each digit begins, and in it each wave
     uint32_t begin = 0;
     for (uint32_t d = threadIdx.x; d < max(digits, (uint32_t)kFewThreads); d += kFewThreads) {
       uint32_t sum = 0, all;
       if (d < digits)
+#pragma unroll 4
         for (int w = 0; w < kFewWaves; ++w) {
           const uint32_t c = count[w * digits + d];
           count[w * digits + d] = (uint16_t)sum;
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 #pragma unroll
     for (int i = 0; i < kFewItems; ++i)
       if (i < items && key[i] != kNone) {
-        const uint32_t d = key[i] >> shift & (digits - 1), to = base[d] + count[wave * digits + d] + at[i];
+        const uint32_t d = key[i] >> shift & (digits - 1), to = base[d] + count[wave * digits + d] + (token[i] >> 16);
         keys[to] = key[i];
         tokens[to] = (uint16_t)token[i];
       }
@@ -167,27 +169,48 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 }
 
 // ------------------------------------------------------------------------------------ many tokens
-// A round of the sort takes one digit: every workgroup counts the digits of its stretch of the items, the counts are summed over
-// the workgroups before it, and it moves its items.  The first round reads the ids themselves and drops the tokens that name no row.
-constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostGroups = 512;
+// A round of the sort takes one digit, in three launches: every workgroup counts the digits of its stretch of the items, the counts are summed
+// over the workgroups before it, and it moves its items.  The first round reads the ids themselves and drops the tokens that name no
+// row; between rounds an item is a word of eight bytes, id below and token above.  (The sums inside the move, each workgroup reading all
+// counts: the three together 27 us for 18.)
+//
+// The runs' numbers need no pass over the sorted ids where the table has at most 2^22 rows.  One round (up to 2^11 rows): a digit is an id, and its run the
+// number of digits before it whose count is not zero.  Two rounds: the first one's move leaves a byte at each id that it meets, the second
+// one's count makes of them, for every 32 ids, a mask and how many ids there are before it in its 2048, and the second move looks its ids up.
+// Larger tables take three rounds and two launches that number the runs of the sorted ids.
+constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostGroups = 256;
+constexpr int kMaskRows = 32, kSegment = 2048;       // ids of a mask, and of a segment: a wave's
 
 struct Round {
   Ids ids;
-  const uint32_t *keys_in, *tokens_in;               // NULL: the first round
-  uint32_t *keys_out, *tokens_out;
-  uint32_t *counts;                                  // [groups][digits]
-  uint32_t *totals;                                  // [digits]
-  int32_t* n;                                        // the order's counts[1]: written by the first round, read by the others
-  int shift, bits;
+  const uint64_t* in;                                // NULL: the first round
+  uint64_t* out;                                     // NULL: the last one
+  uint32_t *counts, *totals;                         // [groups][digits], [digits]
+  uint8_t* seen;                                     // [2^bits of an id], bytes: whether a token names it (NULL: not asked for)
+  uint64_t* masks;                                   // [2^bits / 32]: a mask below, the ids before it in its segment above
+  uint32_t* segments;                                // [2^bits / 2048]: ids in each
+  uint32_t* keys;                                    // the sorted ids, where the runs are numbered from them
+  longer_order order;
+  int shift, bits, id_bits;
 };
+
+// Workgroups go to the eight chiplets in turn, each with a second-level cache of its own.  Neighbouring stretches, whose items land side by side,
+// go to one chiplet: it has whole lines to write back, not an eighth of each.
+__device__ __forceinline__ uint32_t group_number() {
+  const uint32_t chip = blockIdx.x & 7, each = gridDim.x / 8, more = gridDim.x % 8;
+  return chip * each + min(chip, more) + blockIdx.x / 8;
+}
 
 // a workgroup's stretch of n items: whole tiles, as even as they can be dealt
 struct Stretch { uint32_t begin, end; };
-__device__ __forceinline__ Stretch stretch(uint32_t n) {
+__device__ __forceinline__ Stretch stretch(uint32_t n, uint32_t group) {
   const uint32_t tiles = (n + kTile - 1) / kTile, per = (tiles + gridDim.x - 1) / gridDim.x;
-  const uint32_t begin = min((uint64_t)blockIdx.x * per * kTile, (uint64_t)n);
+  const uint32_t begin = min((uint64_t)group * per * kTile, (uint64_t)n);
   return {begin, (uint32_t)min((uint64_t)begin + (uint64_t)per * kTile, (uint64_t)n)};
 }
+
+// four bytes that are 0 or 1 as four bits
+__device__ __forceinline__ uint32_t four_bits(uint32_t bytes) { return bytes * 0x01020408u >> 24 & 15; }
 
 template <bool FIRST>
 __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
@@ -195,20 +218,38 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
   const uint32_t digits = 1u << r.bits;
   for (uint32_t i = threadIdx.x; i < digits; i += kThreads) count[i] = 0;
   __syncthreads();
-  const Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)*r.n);
+  const uint32_t group = group_number();
+  const Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group);
   for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
     uint32_t key[kItems];
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
       const uint32_t i = tile + k * kThreads + threadIdx.x;
-      key[k] = i >= s.end ? kNone : FIRST ? id_of(r.ids, i) : r.keys_in[i];
+      key[k] = i >= s.end ? kNone : FIRST ? id_of(r.ids, i) : (uint32_t)r.in[i];
     }
 #pragma unroll
     for (int k = 0; k < kItems; ++k)
       if (key[k] != kNone) atomicAdd(&count[key[k] >> r.shift & (digits - 1)], 1u);
   }
+  if (r.seen) {
+    if (FIRST) {
+      for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < 1u << (r.id_bits - 4); i += gridDim.x * kThreads) ((u32x4*)r.seen)[i] = u32x4{};
+    } else {
+      const int lane = threadIdx.x & 63;
+      for (uint32_t i = blockIdx.x * kWaves + (threadIdx.x >> 6); i < 1u << r.id_bits >> 11; i += gridDim.x * kWaves) {
+        const u32x4* from = (const u32x4*)(r.seen + (size_t)i * kSegment) + 2 * lane;
+        const u32x4 lo = from[0], hi = from[1];
+        uint32_t mask = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mask |= four_bits(lo[k]) << 4 * k | four_bits(hi[k]) << (16 + 4 * k);
+        const uint32_t ids = __popc(mask), to = wave_scan(ids);
+        r.masks[i * 64 + lane] = (uint64_t)(to - ids) << 32 | mask;
+        if (lane == 63) r.segments[i] = to;
+      }
+    }
+  }
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < digits; i += kThreads) r.counts[(size_t)blockIdx.x * digits + i] = count[i];
+  for (uint32_t i = threadIdx.x; i < digits; i += kThreads) r.counts[(size_t)group * digits + i] = count[i];
 }
 
 // counts[g][digit] becomes the sum over the groups before g, totals[digit] that over all: 32 digits a workgroup, 32 shares of the groups
@@ -216,10 +257,10 @@ __global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* t
   constexpr int kShare = kMostGroups / 32;
   __shared__ uint32_t lds[32][33];
   const uint32_t digit = blockIdx.x * 32 + (threadIdx.x & 31);
-  const int share = threadIdx.x >> 5, per = (groups + 31) / 32, begin = share * per, end = min(begin + per, groups);
+  const int share = threadIdx.x >> 5, per = (groups + 31) / 32, begin = share * per, mine = max(min(groups - begin, per), 0);
   uint32_t sum = 0, c[kShare];
 #pragma unroll
-  for (int k = 0; k < kShare; ++k) c[k] = k < end - begin && digit < digits ? counts[(size_t)(begin + k) * digits + digit] : 0;
+  for (int k = 0; k < kShare; ++k) c[k] = k < mine && digit < digits ? counts[(size_t)(begin + k) * digits + digit] : 0;
 #pragma unroll
   for (int k = 0; k < kShare; ++k) sum += c[k];
   lds[share][threadIdx.x & 31] = sum;
@@ -231,29 +272,58 @@ __global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* t
   if (share == 31) totals[digit] = before + sum;
 #pragma unroll
   for (int k = 0; k < kShare; ++k) {
-    if (k < end - begin) counts[(size_t)(begin + k) * digits + digit] = before;
+    if (k < mine) counts[(size_t)(begin + k) * digits + digit] = before;
     before += c[k];
   }
 }
 
-template <bool FIRST>
+// LAST: 0 items go on to another round, 1 to the order with their runs, 2 to the order and the sorted ids
+template <bool FIRST, int LAST>
 __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
-  __shared__ uint32_t words[kWaves << (kMostBits - 1)], base[1 << kMostBits], lds[kWaves];
-  const uint32_t digits = 1u << r.bits;
+  __shared__ uint32_t words[kWaves << (kMostBits - 1)], base[1 << kMostBits], runs[1 << kMostBits], lds[kWaves];
+  const uint32_t digits = 1u << r.bits, group = group_number();
   uint16_t* count = (uint16_t*)words;                // [waves][digits]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  // where each digit begins for this workgroup
-  uint32_t begin = 0;
+  // where each digit begins, and in it this workgroup
+  uint32_t n = 0, named = 0;
   for (uint32_t d = 0; d < digits; d += kThreads) {
-    const uint32_t i = d + threadIdx.x;
-    uint32_t all;
-    const uint32_t before = group_scan<kThreads>(i < digits ? r.totals[i] : 0, lds, &all);
-    if (i < digits) base[i] = begin + before + r.counts[(size_t)blockIdx.x * digits + i];
-    begin += all;
+    const uint32_t i = d + threadIdx.x, all = i < digits ? r.totals[i] : 0, mine = i < digits ? r.counts[(size_t)group * digits + i] : 0;
+    uint32_t sum;
+    const uint32_t before = group_scan<kThreads>(all, lds, &sum);
+    if (i < digits) base[i] = n + before + mine;
+    n += sum;
+    if (FIRST && LAST == 1) {                        // a digit is an id
+      const uint32_t run = named + group_scan<kThreads>(all != 0, lds, &sum);
+      if (i < digits) {
+        runs[i] = run;
+        if (blockIdx.x == 0 && all) r.order.rows[run] = (int)i;
+      }
+      named += sum;
+    }
   }
-  if (FIRST && blockIdx.x == 0 && threadIdx.x == 0) *r.n = (int)begin;
-  const Stretch s = stretch(FIRST ? r.ids.n : begin);
+  if (!FIRST && LAST == 1) {                         // the runs before each segment, and the rows themselves
+    const uint32_t segments = 1u << r.id_bits >> 11;
+    for (uint32_t d = 0; d < segments; d += kThreads) {
+      const uint32_t i = d + threadIdx.x;
+      uint32_t sum;
+      const uint32_t before = group_scan<kThreads>(i < segments ? r.segments[i] : 0, lds, &sum);
+      if (i < segments) runs[i] = named + before;
+      named += sum;
+    }
+    __syncthreads();
+    for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < segments * 64; i += gridDim.x * kThreads) {
+      const uint64_t v = r.masks[i];
+      uint32_t run = runs[i / 64] + (uint32_t)(v >> 32);
+      for (uint32_t mask = (uint32_t)v; mask; mask &= mask - 1) r.order.rows[run++] = (int)(i * kMaskRows + __ffs(mask) - 1);
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (FIRST) r.order.counts[1] = (int)n;
+    if (LAST == 1) r.order.counts[0] = (int)named;
+  }
+  const Stretch s = stretch(FIRST ? r.ids.n : n, group);
   for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
+    __syncthreads();                                 // words, base and runs have been read, or written
     for (uint32_t i = threadIdx.x; i < kWaves * digits / 2; i += kThreads) words[i] = 0;
     uint32_t key[kItems], token[kItems], at[kItems], sums[(1 << kMostBits) / kThreads];
 #pragma unroll
@@ -261,8 +331,9 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
       const uint32_t k = tile + (wave * kItems + i) * 64 + lane;
       key[i] = kNone;
       if (k < s.end) {
-        key[i] = FIRST ? id_of(r.ids, k) : r.keys_in[k];
-        token[i] = FIRST ? k : r.tokens_in[k];
+        const uint64_t v = FIRST ? 0 : r.in[k];
+        key[i] = FIRST ? id_of(r.ids, k) : (uint32_t)v;
+        token[i] = FIRST ? k : (uint32_t)(v >> 32);
       }
     }
     __syncthreads();
@@ -286,8 +357,20 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
     for (int i = 0; i < kItems; ++i)
       if (key[i] != kNone) {
         const uint32_t d = key[i] >> r.shift & (digits - 1), to = base[d] + count[wave * digits + d] + at[i];
-        r.keys_out[to] = key[i];
-        r.tokens_out[to] = token[i];
+        if (LAST == 0) {
+          r.out[to] = (uint64_t)token[i] << 32 | key[i];
+          if (FIRST && r.seen) r.seen[key[i]] = 1;
+        } else {
+          r.order.tokens[to] = (int)token[i];
+          if (LAST == 2) {
+            r.keys[to] = key[i];
+          } else if (FIRST) {
+            r.order.runs[to] = (int)runs[d];
+          } else {
+            const uint64_t v = r.masks[key[i] / kMaskRows];
+            r.order.runs[to] = (int)(runs[key[i] / kSegment] + (uint32_t)(v >> 32) + __popc((uint32_t)v & ((1u << key[i] % kMaskRows) - 1)));
+          }
+        }
       }
     __syncthreads();
 #pragma unroll
@@ -296,18 +379,12 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
   }
 }
 
-// how many runs begin in each workgroup's stretch
+// how many runs begin in each workgroup's stretch of the sorted ids
 __global__ __launch_bounds__(kThreads) void heads_kernel(const uint32_t* keys, const int32_t* n, uint32_t* heads) {
   __shared__ uint32_t lds[kWaves];
-  const Stretch s = stretch((uint32_t)*n);
+  const Stretch s = stretch((uint32_t)*n, blockIdx.x);
   uint32_t mine = 0, all;
-  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const uint32_t k = tile + i * kThreads + threadIdx.x;
-      if (k < s.end) mine += k == 0 || keys[k] != keys[k - 1];
-    }
-  }
+  for (uint32_t k = s.begin + threadIdx.x; k < s.end; k += kThreads) mine += k == 0 || keys[k] != keys[k - 1];
   group_scan<kThreads>(mine, lds, &all);
   if (threadIdx.x == 0) heads[blockIdx.x] = all;
 }
@@ -317,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void runs_kernel(const uint32_t* keys, co
   __shared__ uint32_t lds[kWaves];
   uint32_t run, all;
   group_scan<kThreads>(threadIdx.x < blockIdx.x ? heads[threadIdx.x] : 0, lds, &run);
-  const Stretch s = stretch((uint32_t)out.counts[1]);
+  const Stretch s = stretch((uint32_t)out.counts[1], blockIdx.x);
   for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
     const uint32_t first = tile + threadIdx.x * kItems;
     uint32_t key[kItems], before = first && first < s.end ? keys[first - 1] : kNone, mine = 0;
@@ -350,7 +427,7 @@ static int bits_of(int64_t rows) {
 
 struct Plan {
   int bits, rounds, per_round, groups;
-  size_t tokens, counts, totals, heads, bytes;       // places in the workspace; the keys are at its front
+  size_t items, keys, counts, totals, seen, masks, segments, heads, bytes;      // places in the workspace: items of two rounds, at its front
 };
 
 static Plan plan(int B, int L, int64_t rows) {
@@ -359,16 +436,29 @@ static Plan plan(int B, int L, int64_t rows) {
   p.bits = bits_of(rows);
   p.rounds = (p.bits + kMostBits - 1) / kMostBits;
   p.per_round = (p.bits + p.rounds - 1) / p.rounds;
-  p.groups = (int)std::min<size_t>((n + kTile - 1) / kTile, kMostGroups);
   if (n <= kFew) {
     p.bytes = 256;
     return p;
   }
-  p.tokens = align256(n * 4);
-  p.counts = p.tokens + (p.rounds > 1 ? align256(n * 4) : 0);
-  p.totals = p.counts + align256(((size_t)p.groups << p.per_round) * 4);
-  p.heads = p.totals + align256((size_t)4 << p.per_round);
-  p.bytes = p.heads + align256((size_t)p.groups * 4);
+  p.groups = (int)std::min<size_t>((n + kTile - 1) / kTile, kMostGroups);
+  size_t at = 0;
+  auto place = [&](size_t bytes) {
+    const size_t here = at;
+    at += align256(bytes);
+    return here;
+  };
+  if (p.rounds > 1) place(n * 8);
+  if (p.rounds > 2) p.items = place(n * 8);
+  if (p.rounds > 2) p.keys = place(n * 4);
+  p.counts = place(((size_t)p.groups << p.per_round) * 4);
+  p.totals = place((size_t)4 << p.per_round);
+  if (p.rounds == 2) {
+    p.seen = place((size_t)1 << p.bits);
+    p.masks = place((size_t)8 << p.bits >> 5);
+    p.segments = place((size_t)4 << p.bits >> 11);
+  }
+  if (p.rounds > 2) p.heads = place((size_t)p.groups * 4);
+  p.bytes = at;
   return p;
 }
 
@@ -401,25 +491,31 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
     return launched("sort of ids");
   }
   char* w = (char*)ws;
-  uint32_t *keys = (uint32_t*)w, *counts = (uint32_t*)(w + p.counts), *totals = (uint32_t*)(w + p.totals), *heads = (uint32_t*)(w + p.heads);
-  srt::Round r = {a, nullptr, nullptr, nullptr, nullptr, counts, totals, order->counts + 1, 0, 0};
+  uint64_t* items[2] = {(uint64_t*)w, (uint64_t*)(w + p.items)};
+  uint32_t* keys = (uint32_t*)(w + p.keys);
+  srt::Round r = {a, nullptr, items[0], (uint32_t*)(w + p.counts), (uint32_t*)(w + p.totals), p.rounds == 2 ? (uint8_t*)(w + p.seen) : nullptr, (uint64_t*)(w + p.masks), (uint32_t*)(w + p.segments), keys, *order,
+                  0, p.per_round, p.bits};
   for (int i = 0; i < p.rounds; ++i) {
-    const bool last = (p.rounds - 1 - i) % 2 == 0;   // rounds take turns so that the last one ends in the order's tokens and this workspace's keys
-    r.keys_out = last ? keys : (uint32_t*)order->runs;
-    r.tokens_out = last ? (uint32_t*)order->tokens : (uint32_t*)(w + p.tokens);
+    r.in = i ? items[(i - 1) & 1] : nullptr;
+    r.out = items[i & 1];
     r.shift = i * p.per_round;
     r.bits = std::min(p.per_round, p.bits - r.shift);
     const uint32_t digits = 1u << r.bits;
     if (i == 0) srt::count_kernel<true><<<p.groups, srt::kThreads, 0, st>>>(r);
     else srt::count_kernel<false><<<p.groups, srt::kThreads, 0, st>>>(r);
-    srt::sum_kernel<<<(digits + 31) / 32, 1024, 0, st>>>(counts, totals, p.groups, digits);
-    if (i == 0) srt::move_kernel<true><<<p.groups, srt::kThreads, 0, st>>>(r);
-    else srt::move_kernel<false><<<p.groups, srt::kThreads, 0, st>>>(r);
-    r.keys_in = r.keys_out;
-    r.tokens_in = r.tokens_out;
+    srt::sum_kernel<<<(digits + 31) / 32, 1024, 0, st>>>(r.counts, r.totals, p.groups, digits);
+    const int last = i + 1 < p.rounds ? 0 : p.rounds <= 2 ? 1 : 2;
+    if (i == 0 && last) srt::move_kernel<true, 1><<<p.groups, srt::kThreads, 0, st>>>(r);
+    else if (i == 0) srt::move_kernel<true, 0><<<p.groups, srt::kThreads, 0, st>>>(r);
+    else if (last == 0) srt::move_kernel<false, 0><<<p.groups, srt::kThreads, 0, st>>>(r);
+    else if (last == 1) srt::move_kernel<false, 1><<<p.groups, srt::kThreads, 0, st>>>(r);
+    else srt::move_kernel<false, 2><<<p.groups, srt::kThreads, 0, st>>>(r);
   }
-  srt::heads_kernel<<<p.groups, srt::kThreads, 0, st>>>(keys, order->counts + 1, heads);
-  srt::runs_kernel<<<p.groups, srt::kThreads, 0, st>>>(keys, heads, *order);
+  if (p.rounds > 2) {
+    uint32_t* heads = (uint32_t*)(w + p.heads);
+    srt::heads_kernel<<<p.groups, srt::kThreads, 0, st>>>(keys, order->counts + 1, heads);
+    srt::runs_kernel<<<p.groups, srt::kThreads, 0, st>>>(keys, heads, *order);
+  }
   return launched("sort of ids");
 }
 
