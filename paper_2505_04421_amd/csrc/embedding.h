@@ -36,26 +36,35 @@ template <typename T, int V> using Piece = typename Piece_<T, V>::type;
 // every access is whole and inside it; its first `twice` values are its neighbour's too, and are computed and stored by both, to the
 // same bits.  That asks for a row of 8 values, and for nobody who reads behind the neighbour's store (in place: no); otherwise the last piece is
 // taken value by value.  Accesses are aligned to the element only, which the memory path takes at any address.
+enum Kind { WHOLE, BACK, VALUES };                   // rows of whole pieces; the last piece is moved back; the last piece is taken value by value
 struct Part { int c, n, twice; };                    // n: values of the row from c on, 8 or more: a whole piece
-template <bool WHOLE>
-__device__ __forceinline__ Part part_of(uint32_t piece, int d, bool back) {
+template <Kind KIND>
+__device__ __forceinline__ Part part_of(uint32_t piece, int d) {
   const int c = piece * 8;
-  if (WHOLE || c + 8 <= d || !back) return {c, WHOLE ? 8 : d - c, 0};
-  return {d - 8, 8, c - (d - 8)};
+  if (KIND == WHOLE) return {c, 8, 0};
+  if (KIND == VALUES) return {c, d - c, 0};
+  return {min(c, d - 8), 8, max(c - (d - 8), 0)};
 }
+template <typename Go>
+inline void with_kind(Kind kind, Go go) {
+  if (kind == WHOLE) go(std::integral_constant<Kind, WHOLE>());
+  else if (kind == BACK) go(std::integral_constant<Kind, BACK>());
+  else go(std::integral_constant<Kind, VALUES>());
+}
+inline Kind kind_of(int d, bool in_place = false) { return d % 8 == 0 ? WHOLE : d > 8 && !in_place ? BACK : VALUES; }
 
-template <typename T>
+template <typename T, Kind KIND>
 __device__ __forceinline__ Piece<T, 8> load8(const T* p, int n) {
-  if (n >= 8) return *(const Piece<T, 8>*)p;
+  if (KIND != VALUES || n >= 8) return *(const Piece<T, 8>*)p;
   Piece<T, 8> x;
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = j < n ? p[j] : (T)0.f;
   return x;
 }
 // written once and read by another kernel: past the caches
-template <typename T>
+template <typename T, Kind KIND>
 __device__ __forceinline__ void store8(T* p, int n, const Piece<T, 8>& x) {
-  if (n >= 8) {
+  if (KIND != VALUES || n >= 8) {
     __builtin_nontemporal_store(x, (Piece<T, 8>*)p);
     return;
   }
@@ -97,11 +106,11 @@ __device__ __forceinline__ void words(const Mask& m, const Key& key, uint32_t ro
 }
 
 // x[j] where value c + j of the row is kept, zero (whatever x[j] is) where it is not; a piece off the multiples of 8 lies in two blocks
-template <bool WHOLE, typename V>
+template <Kind KIND, typename V>
 __device__ __forceinline__ void drop8(const Mask& m, const Key& key, uint32_t row, int c, V& x) {
   uint32_t w[4];
   words(m, key, row, (uint32_t)c / 8, w);
-  if (!WHOLE && (c & 7)) {
+  if (KIND == BACK && (c & 7)) {
     uint32_t v[4];
     words(m, key, row, (uint32_t)c / 8 + 1, v);
     for (int i = c & 7; i; --i) {                    // (at most 7 half-words on)

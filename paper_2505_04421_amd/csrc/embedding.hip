@@ -27,44 +27,39 @@ __device__ __forceinline__ int64_t item(const Ids& ids, uint32_t b, uint32_t l) 
 }
 
 // E[r] = factor * mask * table[id of r], zeros where r is padding or names no row.  Four rows of a lane are under way at once.
-template <typename T, typename O, bool DROP, bool WHOLE>
+template <typename T, typename O, bool DROP, Kind KIND>
 __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p) {
   constexpr int U = 4;
   const uint32_t lanes = 1u << p.shift, per_turn = 256 >> p.shift, per_group = per_turn * U;
   const Key key = DROP ? load_key(p.mask) : Key{};
   for (uint32_t first = blockIdx.x * per_group + (threadIdx.x >> p.shift); first < p.n; first += gridDim.x * per_group) {
     int64_t from[U], to[U];
+    bool there[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t r = first + u * per_turn;
-      from[u] = -1;
-      to[u] = -1;
-      if (r < p.n) {
-        const uint32_t b = p.by_L(r), l = r - b * p.L;
-        const int64_t id = item(p.ids, b, l);
-        from[u] = id < 0 ? -1 : id * p.stride;
-        to[u] = (int64_t)b * p.out.user + (int64_t)l * p.out.row;
-      }
+      const uint32_t r = min(first + u * per_turn, p.n - 1), b = p.by_L(r), l = r - b * p.L;
+      const int64_t id = item(p.ids, b, l);
+      there[u] = id >= 0;
+      from[u] = there[u] ? id * p.stride : 0;        // (a token that names no row loads the table's first: no branch around a load)
+      to[u] = (int64_t)b * p.out.user + (int64_t)l * p.out.row;
     }
     for (uint32_t piece = threadIdx.x & (lanes - 1); (int)piece * 8 < p.d; piece += lanes) {
-      const Part at = part_of<WHOLE>(piece, p.d, p.d >= 8);
+      const Part at = part_of<KIND>(piece, p.d);
       Piece<T, 8> x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (from[u] >= 0) x[u] = load8((const T*)p.table + from[u] + at.c, at.n);
+      for (int u = 0; u < U; ++u) x[u] = load8<T, KIND>((const T*)p.table + from[u] + at.c, at.n);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (to[u] < 0) continue;
-        Piece<float, 8> y = 0.f;
-        if (from[u] >= 0) {
+        const uint32_t r = first + u * per_turn;
+        if (r >= p.n) break;
+        Piece<float, 8> y;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
-          if (DROP) drop8<WHOLE>(p.mask, key, first + u * per_turn, at.c, y);
-        }
+        for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
+        if (DROP) drop8<KIND>(p.mask, key, r, at.c, y);
         Piece<O, 8> o;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = (O)y[j];
-        store8((O*)p.out.data + to[u] + at.c, at.n, o);
+        for (int j = 0; j < 8; ++j) o[j] = there[u] ? (O)y[j] : (O)0.f;
+        store8<O, KIND>((O*)p.out.data + to[u] + at.c, at.n, o);
       }
     }
   }
@@ -76,13 +71,13 @@ struct DropParams {
   Divider by_L;
   uint32_t n, L;
   int d, shift;
-  bool back;                        // the last piece may be moved back
+  Kind kind;
   float factor;
   Mask mask;
 };
 
 // Y[r] = residual[r] + factor * mask * X[r]; padding zeros, not read.
-template <typename T, bool ADD, bool WHOLE>
+template <typename T, bool ADD, Kind KIND>
 __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
   constexpr int U = 2;
   const uint32_t lanes = 1u << p.shift, per_turn = 256 >> p.shift, per_group = per_turn * U;
@@ -98,13 +93,13 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
       there[u] = first + u * per_turn < p.n && (!p.lens || (int)l[u] < p.lens[b[u]]);
     }
     for (uint32_t piece = threadIdx.x & (lanes - 1); (int)piece * 8 < p.d; piece += lanes) {
-      const Part at = part_of<WHOLE>(piece, p.d, p.back);
+      const Part at = part_of<KIND>(piece, p.d);
       Piece<T, 8> x[U], add[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (there[u]) {
-          x[u] = load8((const T*)p.x.data + (int64_t)b[u] * p.x.user + (int64_t)l[u] * p.x.row + at.c, at.n);
-          if (ADD) add[u] = load8((const T*)p.residual.data + (int64_t)b[u] * p.residual.user + (int64_t)l[u] * p.residual.row + at.c, at.n);
+          x[u] = load8<T, KIND>((const T*)p.x.data + (int64_t)b[u] * p.x.user + (int64_t)l[u] * p.x.row + at.c, at.n);
+          if (ADD) add[u] = load8<T, KIND>((const T*)p.residual.data + (int64_t)b[u] * p.residual.user + (int64_t)l[u] * p.residual.row + at.c, at.n);
         }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -114,7 +109,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
         if (there[u]) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
-          drop8<WHOLE>(p.mask, key, r, at.c, y);
+          drop8<KIND>(p.mask, key, r, at.c, y);
           if (ADD)
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += (float)add[u][j];
@@ -122,7 +117,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
         Piece<T, 8> o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = (T)y[j];
-        store8((T*)p.out.data + (int64_t)b[u] * p.out.user + (int64_t)l[u] * p.out.row + at.c, at.n, o);
+        store8<T, KIND>((T*)p.out.data + (int64_t)b[u] * p.out.user + (int64_t)l[u] * p.out.row + at.c, at.n, o);
       }
     }
   }
@@ -137,25 +132,23 @@ static unsigned groups(uint32_t n, int shift, int turns) {
 template <typename T, typename O>
 static void lookup(const LookupParams& p, hipStream_t st) {
   const unsigned g = groups(p.n, p.shift, 4);
-  if (p.d % 8 == 0) {
-    if (p.mask.drop) lookup_kernel<T, O, true, true><<<g, 256, 0, st>>>(p);
-    else lookup_kernel<T, O, false, true><<<g, 256, 0, st>>>(p);
-  } else {
-    if (p.mask.drop) lookup_kernel<T, O, true, false><<<g, 256, 0, st>>>(p);
-    else lookup_kernel<T, O, false, false><<<g, 256, 0, st>>>(p);
-  }
+  auto go = [&](auto kind) {
+    constexpr Kind KIND = decltype(kind)::value;
+    if (p.mask.drop) lookup_kernel<T, O, true, KIND><<<g, 256, 0, st>>>(p);
+    else lookup_kernel<T, O, false, KIND><<<g, 256, 0, st>>>(p);
+  };
+  with_kind(kind_of(p.d), go);
 }
 
 template <typename T>
 static void dropout(const DropParams& p, hipStream_t st) {
   const unsigned g = groups(p.n, p.shift, 2);
-  if (p.d % 8 == 0) {
-    if (p.residual.data) dropout_kernel<T, true, true><<<g, 256, 0, st>>>(p);
-    else dropout_kernel<T, false, true><<<g, 256, 0, st>>>(p);
-  } else {
-    if (p.residual.data) dropout_kernel<T, true, false><<<g, 256, 0, st>>>(p);
-    else dropout_kernel<T, false, false><<<g, 256, 0, st>>>(p);
-  }
+  auto go = [&](auto kind) {
+    constexpr Kind KIND = decltype(kind)::value;
+    if (p.residual.data) dropout_kernel<T, true, KIND><<<g, 256, 0, st>>>(p);
+    else dropout_kernel<T, false, KIND><<<g, 256, 0, st>>>(p);
+  };
+  with_kind(p.kind, go);
 }
 
 }  // namespace emb
@@ -205,7 +198,7 @@ int longer_dropout(const longer_rows* x, const longer_rows* residual, const int3
   if (!rc) rc = emb::check_mask(drop);
   if (rc) return rc;
   const emb::DropParams p = {emb::rows_of(x, B, L), residual ? emb::rows_of(residual, B, L) : emb::Rows{}, emb::rows_of(y, B, L), lens, emb::divider(L), (uint32_t)B * L,
-                             (uint32_t)L, d, emb::lanes_shift((d + 7) / 8, 8), d >= 8 && x->data != y->data && !(residual && residual->data == y->data), (float)emb::kept(drop), emb::mask_of(drop)};
+                             (uint32_t)L, d, emb::lanes_shift((d + 7) / 8, 8), emb::kind_of(d, x->data == y->data || (residual && residual->data == y->data)), (float)emb::kept(drop), emb::mask_of(drop)};
   if (x->dtype == LONGER_F32) emb::dropout<float>(p, (hipStream_t)stream);
   else emb::dropout<__bf16>(p, (hipStream_t)stream);
   return launched("dropout");

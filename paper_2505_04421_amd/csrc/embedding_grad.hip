@@ -11,7 +11,7 @@ namespace longer {
 namespace emb {
 
 constexpr int kChunk = 512;                          // columns of a group: 64 lanes of 8
-constexpr int kThreads = 512, kThreadBits = 9;
+constexpr int kThreads = 256, kThreadBits = 8;
 
 // What of a workgroup's sums crosses its borders: the run that began before it, the run that begins in it and goes on, and that run's row
 // of the gradient (kNone: there is none).
@@ -39,11 +39,12 @@ __device__ __forceinline__ uint32_t tokens_of(const GradParams& p) { return min(
 __device__ __forceinline__ uint32_t runs_of(const GradParams& p) { return min((uint32_t)max(p.order.counts[0], 0), p.n); }
 
 // (these rows are read again, by the join or the update)
+template <Kind KIND>
 __device__ __forceinline__ void store_sums(float* to, int n, const float (&a)[8]) {
   Piece<float, 8> v;
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = a[j];
-  if (n >= 8) *(Piece<float, 8>*)to = v;
+  if (KIND != VALUES || n >= 8) *(Piece<float, 8>*)to = v;
   else
 #pragma unroll
     for (int j = 0; j < 7; ++j)
@@ -51,52 +52,63 @@ __device__ __forceinline__ void store_sums(float* to, int n, const float (&a)[8]
 }
 
 struct Lane { Part at; int lane, chunk; };           // a lane's columns (n <= 0: it has none)
-template <bool WHOLE>
+template <Kind KIND>
 __device__ __forceinline__ Lane lane_of(const GradParams& p) {
   const int lane = threadIdx.x & ((1 << p.shift) - 1), chunk = blockIdx.y, c = chunk * kChunk + lane * 8;
   if (c >= p.d) return {{0, 0, 0}, lane, chunk};
-  return {part_of<WHOLE>((uint32_t)c / 8, p.d, p.d >= 8), lane, chunk};
+  return {part_of<KIND>((uint32_t)c / 8, p.d), lane, chunk};
 }
 
-template <int CTRL> __device__ __forceinline__ double with_dpp(double v) {
+template <int CTRL> __device__ __forceinline__ float from_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL> __device__ __forceinline__ double from_lane(double v) {
   const uint64_t bits = __builtin_bit_cast(uint64_t, v);
   const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, 0xF, 0xF, true);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(bits >> 32), CTRL, 0xF, 0xF, true);
-  return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
 // sum over the 2^shift lanes of a group (all of them are here, other groups may not be: lanes take from their own group's alone)
-__device__ __forceinline__ double group_sum(double v, int shift) {
-  if (shift >= 1) v = with_dpp<0xB1>(v);             // the neighbour's
-  if (shift >= 2) v = with_dpp<0x4E>(v);             // the other pair's
-  if (shift >= 3) v = with_dpp<0x141>(v);            // mirrored in 8
-  if (shift >= 4) v = with_dpp<0x140>(v);            // mirrored in 16
+template <typename V>
+__device__ __forceinline__ V group_sum(V v, int shift) {
+  if (shift >= 1) v += from_lane<0xB1>(v);           // the neighbour's
+  if (shift >= 2) v += from_lane<0x4E>(v);           // the other pair's
+  if (shift >= 3) v += from_lane<0x141>(v);          // mirrored in 8
+  if (shift >= 4) v += from_lane<0x140>(v);          // mirrored in 16
   if (shift >= 5) v += __shfl_xor(v, 16);
   if (shift >= 6) v += __shfl_xor(v, 32);
   return v;
 }
 
-// The root of a sum of squares, rounded: in fp32 (off by 1.5 half steps) where the sum is a normal number of fp32
-__device__ __forceinline__ float root(double s) { return s > 1e-37 && s < 1e38 ? sqrtf((float)s) : (float)sqrt(s); }
-
-// A run's sums are complete: its row, and its norm's squares.  All lanes of the group are here.
+// A run's sums are complete: its row, and its norm's squares.  All lanes of the group are here.  The squares' sum is taken in fp32, off by at most
+// 8 + 6 roundings of it, so the root by 7 and its own; in 64 bits where it is not well inside fp32's range (512000 tokens of 128: 86 us with 64 bits
+// for all).
+template <Kind KIND>
 __device__ __forceinline__ void finish(const GradParams& p, uint32_t run, uint32_t row, const Lane& me, const float (&acc)[8]) {
   if (row >= p.out_rows) return;
   float g[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) g[j] = p.factor * acc[j];
-  if (me.at.n > 0) store_sums(p.grads + (size_t)row * p.d + me.at.c, me.at.n, g);
+  if (me.at.n > 0) store_sums<KIND>(p.grads + (size_t)row * p.d + me.at.c, me.at.n, g);
   if (!p.norms) return;
-  double s = 0.;
+  float s = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const double v = j >= me.at.twice && j < me.at.n ? g[j] : 0.f;
-    s = fma(v, v, s);
+    g[j] = KIND == WHOLE ? (me.at.n ? g[j] : 0.f) : j >= me.at.twice && j < me.at.n ? g[j] : 0.f;
+    s = fmaf(g[j], g[j], s);
   }
   s = group_sum(s, p.shift);
+  double squares = s;
+  if (!(s > 1e-25f && s < 1e37f)) {
+    squares = 0.;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) squares = fma((double)g[j], (double)g[j], squares);
+    squares = group_sum(squares, p.shift);
+  }
   if (me.lane == 0) {
-    if (p.chunks == 1) p.norms[row] = root(s);
-    else p.squares[(size_t)run * p.chunks + me.chunk] = s;
+    if (p.chunks > 1) p.squares[(size_t)run * p.chunks + me.chunk] = squares;
+    else p.norms[row] = squares == s ? sqrtf(s) : (float)sqrt(squares);
   }
 }
 __device__ __forceinline__ uint32_t row_of(const GradParams& p, uint32_t run) { return p.dense ? (uint32_t)p.order.rows[run] : run; }
@@ -104,16 +116,16 @@ __device__ __forceinline__ uint32_t row_of(const GradParams& p, uint32_t run) { 
 // LDS of a workgroup's tokens: where their rows of dE lie, their runs (with the neighbours' on both sides), the runs' rows, their numbers
 __host__ __device__ inline size_t staged_bytes(uint32_t block, bool drop) { return (size_t)block * (drop ? 20 : 16) + 8; }
 
-template <typename T, bool DROP, bool WHOLE>
+template <typename T, bool DROP, Kind KIND>
 __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
-  constexpr int U = 4;
+  constexpr int U = 2;
   constexpr uint32_t kLead = 1, kOn = 2;             // a group's first run began before it; that run goes on behind it
   extern __shared__ int64_t staged[];
   __shared__ float lead[kThreads * 8];
   __shared__ uint32_t flags[kThreads];
   int64_t* from = staged;
   uint32_t *runs = (uint32_t*)(from + p.block) + 1, *rows = runs + p.block + 1, *tokens = rows + p.block;
-  const Lane me = lane_of<WHOLE>(p);
+  const Lane me = lane_of<KIND>(p);
   const int c = me.at.c, width = me.at.n;
   const uint32_t n = tokens_of(p), group = threadIdx.x >> p.shift, groups = kThreads >> p.shift;
   if (p.norms && blockIdx.y == 0 && !p.dense)        // zeros behind the last row's norm
@@ -126,7 +138,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   const Key key = DROP ? load_key(p.mask) : Key{};
   for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
     const uint32_t token = (uint32_t)p.order.tokens[first + i], run = (uint32_t)p.order.runs[first + i], b = p.by_L(token), l = token - b * p.L;
-    from[i] = token < p.n ? (int64_t)b * p.de.user + (int64_t)l * p.de.row : -1;
+    from[i] = token < p.n ? (int64_t)b * p.de.user + (int64_t)l * p.de.row : 0;
     runs[i] = run;
     rows[i] = p.dense ? (uint32_t)p.order.rows[run] : run;
     if (DROP) tokens[i] = token;
@@ -145,51 +157,51 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   uint32_t run = kNone;
   bool earlier = false, on = false;
   if (begin < end) {
-    Piece<T, 8> x[2][U];
-    // the rows of two batches are under way while a third is added up
-    auto load = [&](Piece<T, 8> (&to)[U], uint32_t at) {
+    struct Batch { Piece<T, 8> x[U]; uint32_t run[U], token[U]; } batch[2];
+    // The rows of one batch are under way while another is added up.  Loads are unconditional (behind the range, its last row again): a
+    // load in a branch makes the compiler wait for all that are under way.
+    auto load = [&](Batch& to, uint32_t at) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t o = at + u < end ? from[at + u] : -1;
-        if (o >= 0 && width > 0) to[u] = load8((const T*)p.de.data + o + c, width);
+        const uint32_t i = min(at + u, end - 1);
+        to.x[u] = load8<T, KIND>((const T*)p.de.data + from[i] + c, width);
+        to.run[u] = runs[i];
+        if (DROP) to.token[u] = tokens[i];
       }
     };
-    auto take = [&](const Piece<T, 8> (&x)[U], uint32_t at) {
+    auto take = [&](const Batch& in, uint32_t at) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t i = at + u;
-        if (i >= end) return;
-        if (runs[i] != run) {
+        if (at + u >= end) return;
+        if (in.run[u] != run) {
           if (earlier) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) lead[threadIdx.x * 8 + j] = acc[j];
           } else {
-            finish(p, run, rows[i - 1], me, acc);
+            finish<KIND>(p, run, rows[at + u - 1], me, acc);
           }
-          run = runs[i];
+          run = in.run[u];
           earlier = false;
 #pragma unroll
           for (int j = 0; j < 8; ++j) acc[j] = 0.f;
         }
-        if (from[i] >= 0 && width > 0) {
-          Piece<float, 8> y;
+        Piece<float, 8> y;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j];
-          if (DROP) drop8<WHOLE>(p.mask, key, tokens[i], c, y);
+        for (int j = 0; j < 8; ++j) y[j] = (float)in.x[u][j];
+        if (DROP) drop8<KIND>(p.mask, key, in.token[u], c, y);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] += y[j];
-        }
+        for (int j = 0; j < 8; ++j) acc[j] += y[j];
       }
     };
     run = runs[begin];
     earlier = runs[(int)begin - 1] == run;
     if (me.lane == 0) flags[group] = earlier ? kLead : 0;
-    load(x[0], begin);
-    for (uint32_t at = begin; at < end; at += 2 * U) {
-      load(x[1], at + U);
-      take(x[0], at);
-      load(x[0], at + 2 * U);
-      take(x[1], at + U);
+    load(batch[0], begin);
+    for (uint32_t k = 0; k < p.range; k += 2 * U) {
+      load(batch[1], begin + k + U);
+      take(batch[0], begin + k);
+      if (k + 2 * U < p.range) load(batch[0], begin + k + 2 * U);
+      take(batch[1], begin + k + U);
     }
     on = runs[end] == run;
     if (earlier) {
@@ -197,7 +209,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
       for (int j = 0; j < 8; ++j) lead[threadIdx.x * 8 + j] = acc[j];
       if (me.lane == 0) flags[group] = kLead | (on ? kOn : 0);
     } else if (!on) {
-      finish(p, run, rows[end - 1], me, acc);
+      finish<KIND>(p, run, rows[end - 1], me, acc);
     }
   }
   __syncthreads();
@@ -213,7 +225,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] = (h ? sum[j] : 0.f) + lead[((h << p.shift) + me.lane) * 8 + j];
     }
-    if (width > 0) store_sums(part, width, sum);
+    if (width > 0) store_sums<KIND>(part, width, sum);
   }
   if (owner) {
     bool more = true;
@@ -222,8 +234,8 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += lead[((h << p.shift) + me.lane) * 8 + j];
     }
-    if (!more) finish(p, run, rows[end - 1], me, acc);
-    else if (width > 0) store_sums(part + p.d, width, acc);
+    if (!more) finish<KIND>(p, run, rows[end - 1], me, acc);
+    else if (width > 0) store_sums<KIND>(part + p.d, width, acc);
   }
 }
 
@@ -231,11 +243,12 @@ constexpr int kJoinThreads = 512;
 
 // The runs that cross workgroups' stretches, each by the group of the stretch that it begins in, and by the whole workgroup where it
 // goes on for more than U: group k takes every groups-th of its sums, which then meet in two steps.
+template <Kind KIND>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32_t blocks) {
   constexpr uint32_t U = 8;
   __shared__ float lds[kJoinThreads * 8];
   __shared__ uint32_t list[kJoinThreads], listed;
-  const Lane me = lane_of<false>(p);
+  const Lane me = lane_of<KIND>(p);
   const int c = me.at.c, width = max(me.at.n, 0);
   const uint32_t group = threadIdx.x >> p.shift, groups = kJoinThreads >> p.shift, g = blockIdx.x * groups + group;
   const size_t step = (size_t)2 * p.d;
@@ -250,7 +263,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32
     for (uint32_t u = 0; u < U; ++u) {
       const uint32_t i = min(h + u * by, blocks - 1);
       lead[u] = h + u * by < blocks ? p.borders[i].lead : kNone;
-      x[u] = load8(p.part + i * step + c, width);
+      x[u] = load8<float, KIND>(p.part + i * step + c, width);
     }
     bool more = true;
 #pragma unroll
@@ -263,7 +276,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32
   };
   if (g < blocks) {
     const Border own = p.borders[g];
-    const Piece<float, 8> x = load8(p.part + g * step + p.d + c, width);
+    const Piece<float, 8> x = load8<float, KIND>(p.part + g * step + p.d + c, width);
     float acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = x[j];
@@ -273,7 +286,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32
         if (me.lane == 0) list[atomicAdd(&listed, 1u)] = g;          // (the order of the list is that of the work alone)
       } else {
         add(acc, g + 1, 1, own.tail);
-        finish(p, own.tail, own.row, me, acc);
+        finish<KIND>(p, own.tail, own.row, me, acc);
       }
     }
   }
@@ -284,7 +297,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32
     float acc[8] = {};
     for (uint32_t h = a + 1 + group; add(acc, h, groups, own.tail); h += U * groups) {}
     if (group == 0) {
-      const Piece<float, 8> x = load8(p.part + a * step + p.d + c, width);
+      const Piece<float, 8> x = load8<float, KIND>(p.part + a * step + p.d + c, width);
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += x[j];
     }
@@ -307,7 +320,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32
       for (uint32_t h = 1; h < 8; ++h)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += lds[((h << p.shift) + me.lane) * 8 + j];
-      finish(p, own.tail, own.row, me, acc);
+      finish<KIND>(p, own.tail, own.row, me, acc);
     }
   }
 }
@@ -330,15 +343,15 @@ __global__ __launch_bounds__(256) void norm_kernel(GradParams p) {
     if (row >= p.out_rows) continue;
     double s = 0.;
     for (int k = 0; k < p.chunks; ++k) s += p.squares[(size_t)i * p.chunks + k];
-    p.norms[row] = root(s);
+    p.norms[row] = (float)sqrt(s);
   }
 }
 
 // ------------------------------------------------------------------------------------ host
-// Tokens of a range: as many as leave 4096 waves, 4 to 32, and 2048 of a workgroup at most.
+// Tokens of a range: as many as leave 8192 waves, 4 to 32, and 2048 of a workgroup at most.
 static uint32_t range_of(int64_t n, int shift, int chunks) {
   uint32_t s = std::min(32u, 2048u >> (kThreadBits - shift));
-  while (s > 4 && (n / s * chunks << shift) < (int64_t)4096 * 64) s /= 2;
+  while (s > 4 && (n / s * chunks << shift) < (int64_t)8192 * 64) s /= 2;
   return s;
 }
 
@@ -361,13 +374,16 @@ static GradPlan grad_plan(int B, int L, int d) {
 template <typename T>
 static void grad(const GradParams& p, dim3 grid, hipStream_t st) {
   const size_t lds = staged_bytes(p.block, p.mask.drop);
-  if (p.d % 8 == 0) {
-    if (p.mask.drop) grad_kernel<T, true, true><<<grid, kThreads, lds, st>>>(p);
-    else grad_kernel<T, false, true><<<grid, kThreads, lds, st>>>(p);
-  } else {
-    if (p.mask.drop) grad_kernel<T, true, false><<<grid, kThreads, lds, st>>>(p);
-    else grad_kernel<T, false, false><<<grid, kThreads, lds, st>>>(p);
-  }
+  auto go = [&](auto kind) {
+    constexpr Kind KIND = decltype(kind)::value;
+    if (p.mask.drop) grad_kernel<T, true, KIND><<<grid, kThreads, lds, st>>>(p);
+    else grad_kernel<T, false, KIND><<<grid, kThreads, lds, st>>>(p);
+  };
+  with_kind(kind_of(p.d), go);
+}
+
+static void join(const GradParams& p, dim3 grid, uint32_t blocks, hipStream_t st) {
+  with_kind(kind_of(p.d), [&](auto kind) { join_kernel<decltype(kind)::value><<<grid, kJoinThreads, 0, st>>>(p, blocks); });
 }
 
 }  // namespace emb
@@ -408,7 +424,7 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
   else emb::grad<__bf16>(p, grid, st);
   const unsigned per_join = (unsigned)emb::kJoinThreads >> g.shift;
-  if (g.blocks > 1) emb::join_kernel<<<dim3((g.blocks + per_join - 1) / per_join, g.chunks), emb::kJoinThreads, 0, st>>>(p, g.blocks);
+  if (g.blocks > 1) emb::join(p, dim3((g.blocks + per_join - 1) / per_join, g.chunks), g.blocks, st);
   if (norms_out && g.chunks > 1) emb::norm_kernel<<<std::min((p.n + 255) / 256, 2048u), 256, 0, st>>>(p);
   return launched("embedding gradient");
 }
