@@ -26,25 +26,59 @@ __device__ __forceinline__ uint32_t id_of(const Ids& a, uint32_t i) {
   return (uint64_t)id < a.table_rows ? (uint32_t)id : kNone;
 }
 
-// Place of an item among those with its digit, in a wave's order: `count` is the wave's own, one counter a digit.  A lane's peers, the
-// lanes of this step with its digit, come from one ballot a bit (peers whose bit is as the lane's: not the exclusive or of the ballot and
-// the lane's bit in every place); the lowest of them moves the counter on.
-__device__ __forceinline__ uint32_t rank(uint32_t digit, bool there, int bits, volatile uint16_t* count) {
-  const uint64_t all = __ballot(there);
-  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+// Places of a wave's items among those with their digit, in the wave's order: item i of lane l comes before item i of lane l + 1, and that
+// before item i + 1 of any lane.  `count`: the wave's own, one 16-bit counter a digit, two to a word, zero before.  An item's peers, the lanes with its
+// digit, come from one ballot a bit (peers whose bit is as the lane's: not the exclusive or of the ballot and the lane's bit in every
+// place); the lowest of them moves the counter on for all, and hands on what it found.  There are `rounds` items (the same for all lanes) of
+// ITEMS; an item that is not there has no place.
+template <int ITEMS>
+__device__ __forceinline__ void rank(const uint32_t* digit, const bool* there, int rounds, int bits, uint32_t* count, uint32_t* at) {
+  uint32_t lo[ITEMS], hi[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    const uint64_t all = __ballot(there[i]);
+    lo[i] = (uint32_t)all;
+    hi[i] = (uint32_t)(all >> 32);
+  }
   for (int b = 0; b < bits; ++b) {
-    const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe(digit, b, 1);
-    const uint64_t with = __ballot(mine);
-    lo = __builtin_amdgcn_bitop3_b32(lo, (uint32_t)with, mine, 0x90);
-    hi = __builtin_amdgcn_bitop3_b32(hi, (uint32_t)(with >> 32), mine, 0x90);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      if (i >= rounds) break;
+      const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe(digit[i], b, 1);
+      const uint64_t with = __ballot(mine);
+      lo[i] = __builtin_amdgcn_bitop3_b32(lo[i], (uint32_t)with, mine, 0x90);
+      hi[i] = __builtin_amdgcn_bitop3_b32(hi[i], (uint32_t)(with >> 32), mine, 0x90);
+    }
   }
-  const uint32_t below = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
-  uint32_t at = 0;
-  if (there) {
-    at = count[digit];
-    if (below == 0) count[digit] = (uint16_t)(at + __popc(lo) + __popc(hi));
+  uint32_t old[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    if (i >= rounds) break;
+    at[i] = __builtin_amdgcn_mbcnt_hi(hi[i], __builtin_amdgcn_mbcnt_lo(lo[i], 0));
+    old[i] = 0;
+    if (there[i] && at[i] == 0) old[i] = atomicAdd(&count[digit[i] >> 1], (uint32_t)(__popc(lo[i]) + __popc(hi[i])) << 16 * (digit[i] & 1));
   }
-  return at + below;
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    if (i >= rounds) break;
+    const int first = lo[i] ? __ffs(lo[i]) - 1 : __ffs(hi[i]) + 31;
+    at[i] += (uint32_t)__shfl((int)old[i], first & 63) >> 16 * (digit[i] & 1) & 0xffff;
+  }
+}
+
+// Of the counts of four neighbouring digits, wave by wave, the sums over the waves before, in their place; returns those over all.  (`words`: [waves][digits / 2])
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <int WAVES>
+__device__ __forceinline__ u32x4 waves_before(uint32_t* words, uint32_t digits, uint32_t four) {
+  u32x2 c[WAVES], sum = {};
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) c[w] = *(const u32x2*)(words + w * (digits / 2) + 2 * four);
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    *(u32x2*)(words + w * (digits / 2) + 2 * four) = sum;
+    sum += c[w];                                     // (no half passes 2^16: a workgroup's items are fewer)
+  }
+  return u32x4{sum[0] & 0xffff, sum[0] >> 16, sum[1] & 0xffff, sum[1] >> 16};
 }
 
 // inclusive sum over a wave
@@ -81,52 +115,57 @@ constexpr int kFewThreads = 1024, kFewItems = 8, kFew = kFewThreads * kFewItems,
 
 // A wave takes 64 * items neighbours; rounds of up to kMostBits bits, all in LDS.  (6144 tokens of 1000 rows: ... us)
 __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int per_round, longer_order out) {
-  __shared__ uint32_t keys[kFew], words[kFewWaves << (kMostBits - 1)], base[1 << kMostBits], lds[kFewWaves];
+  __shared__ alignas(16) uint32_t keys[kFew], words[kFewWaves << (kMostBits - 1)], base[1 << kMostBits];
+  __shared__ uint32_t lds[kFewWaves];
   __shared__ uint16_t tokens[kFew];
-  uint16_t* count = (uint16_t*)words;                // [waves][digits]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int items = (a.n + kFewThreads - 1) / kFewThreads;
   uint32_t n = a.n, key[kFewItems], token[kFewItems];        // (a token and, above it, its place: both below 2^13)
-  for (int shift = 0; shift < bits; shift += per_round) {
-    const int round = min(bits - shift, per_round);
-    const uint32_t digits = 1u << round;
-    for (uint32_t i = threadIdx.x; i < kFewWaves * digits / 2; i += kFewThreads) words[i] = 0;
 #pragma unroll
-    for (int i = 0; i < kFewItems; ++i) {
-      key[i] = kNone;
-      token[i] = 0;
-      const uint32_t k = (wave * items + i) * 64 + lane;
-      if (i < items && k < n) {
-        key[i] = shift ? keys[k] : id_of(a, k);
-        token[i] = shift ? tokens[k] : k;
+  for (int i = 0; i < kFewItems; ++i) {
+    const uint32_t k = (wave * items + i) * 64 + lane;
+    key[i] = i < items && k < n ? id_of(a, k) : kNone;
+    token[i] = k;
+  }
+  for (int shift = 0; shift < bits; shift += per_round) {
+    const int round = per_round;                     // (the last one's digits may pass the ids' bits)
+    const uint32_t digits = 1u << round;
+    if (shift) {
+#pragma unroll
+      for (int i = 0; i < kFewItems; ++i) {
+        const uint32_t k = (wave * items + i) * 64 + lane;
+        key[i] = i < items && k < n ? keys[k] : kNone;
+        token[i] = i < items && k < n ? tokens[k] : 0;
       }
     }
+    for (uint32_t i = threadIdx.x; i < kFewWaves * digits / 2; i += kFewThreads) words[i] = 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kFewItems; ++i)
-      if (i < items) token[i] |= rank(key[i] >> shift & (digits - 1), key[i] != kNone, round, count + wave * digits) << 16;
-    __syncthreads();
-    // where each digit begins, and in it each wave
-    uint32_t begin = 0;
-    for (uint32_t d = threadIdx.x; d < max(digits, (uint32_t)kFewThreads); d += kFewThreads) {
-      uint32_t sum = 0, all;
-      if (d < digits)
-#pragma unroll 4
-        for (int w = 0; w < kFewWaves; ++w) {
-          const uint32_t c = count[w * digits + d];
-          count[w * digits + d] = (uint16_t)sum;
-          sum += c;
-        }
-      const uint32_t before = group_scan<kFewThreads>(sum, lds, &all);
-      if (d < digits) base[d] = begin + before;
-      begin += all;
+    for (int h = 0; h < kFewItems; h += 4) {
+      if (h >= items) break;
+      uint32_t digit[4], at[4];
+      bool there[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        there[i] = key[h + i] != kNone;
+        digit[i] = key[h + i] >> shift & (digits - 1);
+      }
+      rank<4>(digit, there, items - h, round, words + wave * (digits / 2), at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (h + i < items) token[h + i] |= at[i] << 16;
     }
     __syncthreads();
-    n = begin;                                       // the first round drops the tokens that name no row
+    // where each digit begins, and in it each wave
+    const uint32_t four = threadIdx.x;
+    const u32x4 sums = 4 * four < digits ? waves_before<kFewWaves>(words, digits, four) : u32x4{};
+    const uint32_t before = group_scan<kFewThreads>(sums[0] + sums[1] + sums[2] + sums[3], lds, &n);   // (the first round drops the tokens that name no row)
+    if (4 * four < digits) *(u32x4*)(base + 4 * four) = u32x4{before, before + sums[0], before + sums[0] + sums[1], before + sums[0] + sums[1] + sums[2]};
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kFewItems; ++i)
       if (i < items && key[i] != kNone) {
-        const uint32_t d = key[i] >> shift & (digits - 1), to = base[d] + count[wave * digits + d] + (token[i] >> 16);
+        const uint32_t digit = key[i] >> shift & (digits - 1), to = base[digit] + ((const uint16_t*)words)[wave * digits + digit] + (token[i] >> 16);
         keys[to] = key[i];
         tokens[to] = (uint16_t)token[i];
       }
@@ -280,25 +319,47 @@ __global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* t
 // LAST: 0 items go on to another round, 1 to the order with their runs, 2 to the order and the sorted ids
 template <bool FIRST, int LAST>
 __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
-  __shared__ uint32_t words[kWaves << (kMostBits - 1)], base[1 << kMostBits], runs[1 << kMostBits], lds[kWaves];
-  const uint32_t digits = 1u << r.bits, group = group_number();
-  uint16_t* count = (uint16_t*)words;                // [waves][digits]
+  static_assert((1 << kMostBits) <= 4 * kThreads, "a thread has four digits");
+  __shared__ alignas(16) uint32_t words[kWaves << (kMostBits - 1)], base[1 << kMostBits], runs[1 << kMostBits];
+  __shared__ uint32_t lds[kWaves];
+  const uint32_t digits = 1u << r.bits, group = group_number(), four = 4 * threadIdx.x;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  // where each digit begins, and in it this workgroup
-  uint32_t n = 0, named = 0;
-  for (uint32_t d = 0; d < digits; d += kThreads) {
-    const uint32_t i = d + threadIdx.x, all = i < digits ? r.totals[i] : 0, mine = i < digits ? r.counts[(size_t)group * digits + i] : 0;
-    uint32_t sum;
-    const uint32_t before = group_scan<kThreads>(all, lds, &sum);
-    if (i < digits) base[i] = n + before + mine;
-    n += sum;
-    if (FIRST && LAST == 1) {                        // a digit is an id
-      const uint32_t run = named + group_scan<kThreads>(all != 0, lds, &sum);
-      if (i < digits) {
-        runs[i] = run;
-        if (blockIdx.x == 0 && all) r.order.rows[run] = (int)i;
+  uint32_t key[kItems], token[kItems], digit[kItems], at[kItems];
+  bool there[kItems];
+  auto load = [&](uint32_t tile, uint32_t end) {
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const uint32_t k = tile + (wave * kItems + i) * 64 + lane;
+      key[i] = kNone;
+      if (k < end) {
+        const uint64_t v = FIRST ? 0 : r.in[k];
+        key[i] = FIRST ? id_of(r.ids, k) : (uint32_t)v;
+        token[i] = FIRST ? k : (uint32_t)(v >> 32);
       }
-      named += sum;
+    }
+  };
+  Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group);
+  load(s.begin, s.end);                              // (under way while the digits' places are found)
+  // where each digit begins, and in it this workgroup
+  uint32_t n, named = 0;
+  {
+    u32x4 all = {}, mine = {};
+    if (four < digits) {
+      all = *(const u32x4*)(r.totals + four);
+      mine = *(const u32x4*)(r.counts + (size_t)group * digits + four);
+    }
+    const uint32_t before = group_scan<kThreads>(all[0] + all[1] + all[2] + all[3], lds, &n);
+    if (four < digits) *(u32x4*)(base + four) = mine + u32x4{before, before + all[0], before + all[0] + all[1], before + all[0] + all[1] + all[2]};
+    if (FIRST && LAST == 1) {                        // a digit is an id
+      const u32x4 one = {all[0] != 0, all[1] != 0, all[2] != 0, all[3] != 0};
+      uint32_t run = group_scan<kThreads>(one[0] + one[1] + one[2] + one[3], lds, &named);
+      if (four < digits)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          runs[four + k] = run;
+          if (group == 0 && one[k]) r.order.rows[run] = (int)(four + k);
+          run += one[k];
+        }
     }
   }
   if (!FIRST && LAST == 1) {                         // the runs before each segment, and the rows themselves
@@ -317,46 +378,28 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
       for (uint32_t mask = (uint32_t)v; mask; mask &= mask - 1) r.order.rows[run++] = (int)(i * kMaskRows + __ffs(mask) - 1);
     }
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
+  if (group == 0 && threadIdx.x == 0) {
     if (FIRST) r.order.counts[1] = (int)n;
     if (LAST == 1) r.order.counts[0] = (int)named;
   }
-  const Stretch s = stretch(FIRST ? r.ids.n : n, group);
   for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
-    __syncthreads();                                 // words, base and runs have been read, or written
-    for (uint32_t i = threadIdx.x; i < kWaves * digits / 2; i += kThreads) words[i] = 0;
-    uint32_t key[kItems], token[kItems], at[kItems], sums[(1 << kMostBits) / kThreads];
+    if (tile != s.begin) load(tile, s.end);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const uint32_t k = tile + (wave * kItems + i) * 64 + lane;
-      key[i] = kNone;
-      if (k < s.end) {
-        const uint64_t v = FIRST ? 0 : r.in[k];
-        key[i] = FIRST ? id_of(r.ids, k) : (uint32_t)v;
-        token[i] = FIRST ? k : (uint32_t)(v >> 32);
-      }
+      there[i] = key[i] != kNone;
+      digit[i] = key[i] >> r.shift & (digits - 1);
     }
+    for (uint32_t i = threadIdx.x; i < kWaves * digits / 2; i += kThreads) words[i] = 0;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) at[i] = rank(key[i] >> r.shift & (digits - 1), key[i] != kNone, r.bits, count + wave * digits);
+    rank<kItems>(digit, there, kItems, r.bits, words + wave * (digits / 2), at);
     __syncthreads();
     // where each wave begins in a digit
-#pragma unroll
-    for (int k = 0; k < (1 << kMostBits) / kThreads; ++k) {
-      const uint32_t d = k * kThreads + threadIdx.x;
-      sums[k] = 0;
-      if (d < digits)
-        for (int w = 0; w < kWaves; ++w) {
-          const uint32_t c = count[w * digits + d];
-          count[w * digits + d] = (uint16_t)sums[k];
-          sums[k] += c;
-        }
-    }
+    const u32x4 sums = four < digits ? waves_before<kWaves>(words, digits, four / 4) : u32x4{};
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
-      if (key[i] != kNone) {
-        const uint32_t d = key[i] >> r.shift & (digits - 1), to = base[d] + count[wave * digits + d] + at[i];
+      if (there[i]) {
+        const uint32_t to = base[digit[i]] + ((const uint16_t*)words)[wave * digits + digit[i]] + at[i];
         if (LAST == 0) {
           r.out[to] = (uint64_t)token[i] << 32 | key[i];
           if (FIRST && r.seen) r.seen[key[i]] = 1;
@@ -365,7 +408,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
           if (LAST == 2) {
             r.keys[to] = key[i];
           } else if (FIRST) {
-            r.order.runs[to] = (int)runs[d];
+            r.order.runs[to] = (int)runs[digit[i]];
           } else {
             const uint64_t v = r.masks[key[i] / kMaskRows];
             r.order.runs[to] = (int)(runs[key[i] / kSegment] + (uint32_t)(v >> 32) + __popc((uint32_t)v & ((1u << key[i] % kMaskRows) - 1)));
@@ -373,9 +416,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
         }
       }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < (1 << kMostBits) / kThreads; ++k)
-      if (k * kThreads + threadIdx.x < digits) base[k * kThreads + threadIdx.x] += sums[k];
+    if (four < digits) *(u32x4*)(base + four) += sums;
   }
 }
 
@@ -420,7 +461,7 @@ __global__ __launch_bounds__(kThreads) void runs_kernel(const uint32_t* keys, co
 
 // ------------------------------------------------------------------------------------ host
 static int bits_of(int64_t rows) {
-  int bits = 1;
+  int bits = 2;                                      // (a thread has four digits)
   while (((int64_t)1 << bits) < rows) ++bits;
   return bits;
 }
@@ -499,7 +540,7 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
     r.in = i ? items[(i - 1) & 1] : nullptr;
     r.out = items[i & 1];
     r.shift = i * p.per_round;
-    r.bits = std::min(p.per_round, p.bits - r.shift);
+    r.bits = p.per_round;                            // (the last round's digits may pass the ids' bits)
     const uint32_t digits = 1u << r.bits;
     if (i == 0) srt::count_kernel<true><<<p.groups, srt::kThreads, 0, st>>>(r);
     else srt::count_kernel<false><<<p.groups, srt::kThreads, 0, st>>>(r);
