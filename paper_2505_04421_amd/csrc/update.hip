@@ -261,6 +261,8 @@ __global__ __launch_bounds__(kStepPiece / 4) void step_kernel(StepArgs a) {
 }
 
 // The rows of a table that a batch names: row i of g is the gradient of row rows[i].  2^shift lanes hold a row, four values each.
+// Bound by memory: 400 thousand rows of 128 in 292 us, 5.3 TB/s, everything past the caches (305 with ordinary accesses); the grid is as large as
+// pays where the count, which is on the GPU, turns out small (2048 / 16384 / 65536 workgroups: 140 thousand rows 113 / 105 / 114).
 struct RowsArgs {
   float *p, *m, *v;
   void* w;
@@ -289,8 +291,8 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
     W* ws = (W*)a.w;
     for (int k = (threadIdx.x & (lanes - 1)) * 4; k < a.d; k += lanes * 4) {
       if (k + 4 <= a.d) {
-        const Four<float> g = *(const Four<float>*)(gs + k);
-        Four<float> m = *(const Four<float>*)(a.m + at + k), v = *(const Four<float>*)(a.v + at + k), p = *(const Four<float>*)(a.p + at + k);
+        const Four<float> g = __builtin_nontemporal_load((const Four<float>*)(gs + k));
+        Four<float> m = __builtin_nontemporal_load((const Four<float>*)(a.m + at + k)), v = __builtin_nontemporal_load((const Four<float>*)(a.v + at + k)), p = __builtin_nontemporal_load((const Four<float>*)(a.p + at + k));
         Four<W> w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -301,10 +303,10 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
           v[j] = vj;
           w[j] = (W)pj;
         }
-        *(Four<float>*)(a.m + at + k) = m;
-        *(Four<float>*)(a.v + at + k) = v;
-        *(Four<float>*)(a.p + at + k) = p;
-        if (COPY) *(Four<W>*)(ws + at + k) = w;
+        __builtin_nontemporal_store(m, (Four<float>*)(a.m + at + k));
+        __builtin_nontemporal_store(v, (Four<float>*)(a.v + at + k));
+        __builtin_nontemporal_store(p, (Four<float>*)(a.p + at + k));
+        if (COPY) __builtin_nontemporal_store(w, (Four<W>*)(ws + at + k));
       } else {
         for (int j = k; j < a.d; ++j) {
           float p = a.p[at + j], m = a.m[at + j], v = a.v[at + j];
@@ -565,7 +567,7 @@ int longer_adamw_rows(const longer_adamw_table* t, const longer_order* order, in
   const uint32_t most = (uint32_t)std::min<int64_t>((int64_t)B * L, t->rows);
   const upd::RowsArgs a = {t->p, t->m, t->v, t->w, g, order->rows, order->counts, norm, most, (uint32_t)t->rows, t->d, emb::lanes_shift((t->d + 3) / 4, 8),
                            (float)(how->lr * t->decay), h};
-  const unsigned per_group = 256u >> a.shift, groups = std::min((most + per_group - 1) / per_group, 2048u);
+  const unsigned per_group = 256u >> a.shift, groups = std::min((most + per_group - 1) / per_group, 16384u);
   hipStream_t st = (hipStream_t)stream;
   if (!t->w) upd::rows_kernel<float, false><<<groups, 256, 0, st>>>(a);
   else if (t->w_dtype == LONGER_BF16) upd::rows_kernel<__bf16, true><<<groups, 256, 0, st>>>(a);
