@@ -1,14 +1,19 @@
 """Training a small model end to end on one GPU: a table of item embeddings, layer norms in front of the model, the model's loss and
 gradients, their global norm, and AdamW.
 
-    python examples/train.py [--steps 40] [--users 64] [--max-norm 1.0] [--lr 2e-3]
+    python examples/train.py [--steps 40] [--users 64] [--max-norm 1.0] [--lr 2e-3] [--dropout 0.1] [--rows]
 
 A step is
-    H = norm(E[items])                     longer_layer_norm (and G likewise, from a table of global tokens)
+    E = mask * table[items]                longer_embedding (the mask of --dropout follows from the step's number, nothing is kept)
+    H = norm(E)                            longer_layer_norm (and G likewise, from a table of global tokens)
     loss, gradients                        longer_forward_backward
-    dE, d norm                             longer_layer_norm_backward, then a sum over the places where an item stands
+    dE, d norm                             longer_layer_norm_backward
+    d table                                longer_sort_ids, longer_embedding_backward: a sum over the places where an item stands
     |gradients|, the factor that bounds it longer_grad_norm, over every parameter at once
     p, m, v, weights                       longer_adamw_step, the factor read on the GPU
+
+With --rows the table's gradient is that of the items in the batch alone, its norm goes into the global one row by row, and longer_adamw_rows
+updates these rows and no other.
 
 Master values and moments are fp32, in one buffer each, in the order of longer_forward_backward's gradients; the kernels read bf16
 copies.  The data is synthetic: a user's label says whether a few marked items are among the items of the history."""
@@ -37,7 +42,7 @@ def leaves(tree):
 class Trainer:
     """Model, tables, norms, optimizer state and scratch of a run; everything is allocated here."""
 
-    def __init__(self, cfg, items, lr=2e-3, beta1=0.9, beta2=0.98, eps=1e-8, decay=0.01, max_norm=1.0, seed=0):
+    def __init__(self, cfg, items, lr=2e-3, beta1=0.9, beta2=0.98, eps=1e-8, decay=0.01, max_norm=1.0, seed=0, dropout=0.0, rows=False):
         self.cfg, self.how, self.max_norm, self.done = cfg, (lr, beta1, beta2, eps), max_norm, 0
         self.model = lg.DeviceModel(cfg, synth.draw_weights(cfg))
         dev = self.model.device
@@ -64,23 +69,34 @@ class Trainer:
         for name in ("norm_h", "norm_g"):
             self.pv[name][0].fill_(1.0)
         weights = leaves(self.model.parameters)
-        cut = lambda flat: leaves(lg.model_grad_views(cfg, flat[:n_model])) + [views(flat)[k] for k, _ in self.extra]
+        self.rows = rows
+        listed = [k for k, _ in self.extra if not (rows and k == "items")]
+        cut = lambda flat: leaves(lg.model_grad_views(cfg, flat[:n_model])) + [views(flat)[k] for k in listed]
         p, m, v, g = (cut(t) for t in (self.p, self.m, self.v, self.g))
-        w = weights + [self.wv[k] for k, _ in self.extra]
+        w = weights + [self.wv[k] for k in listed]
         for a, b in zip(p[:len(weights)], weights):
             a.copy_(b.view(a.shape))                                     # the model starts from its bf16 weights
         for k, _ in self.extra:
             self.wv[k].copy_(self.pv[k])
         # matrices and tables decay, vectors (biases, gains) do not
         self.params = lg.AdamWList(p, m, v, g, w, [decay if min(t.shape) > 2 else 0.0 for t in (x.view(1, -1) if x.dim() < 2 else x for x in p)])
-        self.grads = lg.TensorList(g)
+        # the table: the batch's items in order, its gradient (of every row, in the common buffer, or of the batch's) and the rows' norms
+        most = min(B * L, items) if rows else items
+        f32 = lambda *shape: torch.empty(*shape, device=dev)
+        self.order, self.row_norms = lg.TokenOrder.empty(B, L, items, dev), f32(most)
+        self.table_g = f32(most, cfg.d_in) if rows else self.gv["items"]
+        self.table = lg.AdamWRows(self.pv["items"], views(self.m)["items"], views(self.v)["items"], self.wv["items"], decay) if rows else None
+        self.grads = lg.TensorList(g + ([self.row_norms] if rows else []))
+        self.key = torch.tensor([seed, 0], dtype=torch.int64, device=dev)
+        self.drop = lg.DropoutMask(dropout, self.key) if dropout else None
         scratch = lambda n: torch.empty(n, dtype=torch.uint8, device=dev)
         self.ws = scratch(lg.longer_forward_backward_workspace_bytes(self.model.ccfg, B, L))
         self.ws_h = scratch(lg.longer_layer_norm_backward_workspace_bytes(B, L, cfg.d_in))
         self.ws_g = scratch(lg.longer_layer_norm_backward_workspace_bytes(1, cfg.m, d))
         self.ws_n = scratch(lg.longer_grad_norm_workspace_bytes(self.grads))
-        self.H, self.G1 = self.model.empty(B, L, cfg.d_in), self.model.empty(1, cfg.m, d)
-        f32 = lambda *shape: torch.empty(*shape, device=dev)
+        self.ws_o = scratch(lg.longer_sort_ids_workspace_bytes(B, L, items))
+        self.ws_e = scratch(lg.longer_embedding_backward_workspace_bytes(B, L, cfg.d_in))
+        self.E, self.H, self.G1 = self.model.empty(B, L, cfg.d_in), self.model.empty(B, L, cfg.d_in), self.model.empty(1, cfg.m, d)
         self.dH, self.dG, self.loss, self.norm = f32(B, L, cfg.d_in), f32(B, cfg.m, d), f32(4), f32(2)
         self.last_norm, self.last = torch.empty(2, pin_memory=True), None        # the last step's norm on the host, and when it is there
 
@@ -96,7 +112,9 @@ class Trainer:
     def step(self, ids, lens, labels):
         """One step on item ids [B, L] (int64), lengths [B] (int32 or None), labels [B]; the loss stays on the GPU."""
         cfg, w, eps = self.cfg, self.wv, self.cfg.ln_eps
-        E, G = w["items"][ids], w["globals"][None]
+        E, G = self.E, w["globals"][None]
+        self.key[1:].add_(1)
+        lg.longer_embedding(w["items"], ids, lens, 1.0, self.drop, E)
         lg.longer_layer_norm(E, w["norm_h"][0], w["norm_h"][1], lens, eps, self.H)
         lg.longer_layer_norm(G, w["norm_g"][0], w["norm_g"][1], None, eps, self.G1)
         lg.longer_forward_backward(self.model.ccfg, self.model.weights, self.H, self.G1.expand(cfg.B, -1, -1).contiguous(), lens, cfg.B, cfg.L,
@@ -105,10 +123,14 @@ class Trainer:
         dG = self.dG.sum(0, keepdim=True)
         lg.longer_layer_norm_backward(G, w["norm_g"][0], dG, None, eps, dG, self.gv["norm_g"], self.ws_g)
         self.gv["globals"].copy_(dG[0])
-        self.gv["items"].zero_().index_add_(0, ids.reshape(-1), self.dH.reshape(-1, cfg.d_in))
+        lg.longer_sort_ids(ids, lens, w["items"].shape[0], self.order, self.ws_o)
+        lg.longer_embedding_backward(self.order, self.dH, 1.0, self.drop, not self.rows, self.table_g, self.row_norms, self.ws_e)
         lg.longer_grad_norm(self.grads, self.max_norm, self.norm, self.ws_n)
         # (here the GPU has this step's passes to do while the host waits for the last step's end)
-        lg.longer_adamw_step(self.params, self.norm, *self.how, self.updates() + 1)
+        update = self.updates() + 1
+        lg.longer_adamw_step(self.params, self.norm, *self.how, update)
+        if self.rows:
+            lg.longer_adamw_rows(self.table, self.order, self.table_g, self.norm, *self.how, update)
         self.last_norm.copy_(self.norm, non_blocking=True)
         self.last = torch.cuda.Event()
         self.last.record()
@@ -137,9 +159,11 @@ def main():
     ap.add_argument("--items", type=int, default=1000)
     ap.add_argument("--max-norm", type=float, default=1.0)
     ap.add_argument("--lr", type=float, default=2e-3)
+    ap.add_argument("--dropout", type=float, default=0.0)
+    ap.add_argument("--rows", action="store_true")
     a = ap.parse_args()
     cfg = small_config(a.users)
-    t = Trainer(cfg, a.items, lr=a.lr, max_norm=a.max_norm)
+    t = Trainer(cfg, a.items, lr=a.lr, max_norm=a.max_norm, dropout=a.dropout, rows=a.rows)
     data = [batch(cfg, a.items, k, t.model.device) for k in range(4)]
     for k in range(a.steps):
         t.step(*data[k % len(data)])

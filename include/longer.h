@@ -447,7 +447,7 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
  *   dense == 1: grads_out [out_rows][d] holds every row of the table, zeros where no token names it (ids from out_rows on are dropped).
  * norms_out [out_rows] fp32, or NULL: the norm of each row of grads_out, zeros behind the last one: in a list of longer_grad_norm it
  * stands for the table's gradient, of which nothing is read again.
- * Sums in fp32 in a fixed order, the squares of a norm in 64 bits: the same call gives the same bits.
+ * Sums in fp32 in a fixed order: the same call gives the same bits.  A norm is within 8 half steps of fp32 of its row's, whatever its size.
  * ws: device, 256-byte aligned, at least longer_embedding_backward_workspace_bytes(B, L, d) bytes (0 = unsupported). */
 size_t longer_embedding_backward_workspace_bytes(int B, int L, int d);
 int longer_embedding_backward(const longer_order* order, const longer_rows* de, int B, int L, int d, float scale,

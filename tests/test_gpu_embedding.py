@@ -3,7 +3,9 @@ of one value to 16384, one token to hundreds of thousands, any strides, both id 
 
 Tolerances.  u = 2^-24, half a step of fp32; half a step of bf16 is 2^-8 of the value.  A looked-up value is a product with the factor,
 itself rounded: 2 u, and the output's rounding.  Dropout adds one sum.  A gradient is a sum of n terms in fp32, in any order at most n u of
-the terms' magnitudes, and the factor's two roundings.  A norm is off by the norm of what its row is off, and one rounding."""
+the terms' magnitudes, and the factor's two roundings.  A norm is off by the norm of what its row is off, by 7 u for the sum of its squares
+(a fused step for each of a lane's 8, 6 joins of lanes: 14 u of the sum, half of that of the root; chunks of 512 columns join in 64 bits) and by its own
+rounding: 8 u."""
 import numpy as np
 import pytest
 import torch
@@ -94,7 +96,7 @@ def test_lookup(shape, types, how):
         want = np.where(there[..., None], want, 0.0)
         got = np64(out)
         fine = np.isfinite(want)
-        assert (np.abs(got - want)[fine] <= (np.abs(want) * (2.01 * U + HALF[ed]) + TINY)[fine]).all()
+        assert (np.abs(got[fine] - want[fine]) <= np.abs(want[fine]) * (2.01 * U + HALF[ed]) + TINY).all()
         assert (got[~fine] == want[~fine]).all()
         assert (got[want == 0] == 0).all()
         inside = torch.zeros_like(buf, dtype=torch.bool)
@@ -143,7 +145,7 @@ def test_dropout(shape, dtype, how):
         want, got = kx + base, np64(out)
         fine = np.isfinite(want)
         tol = 2.01 * U * np.abs(kx) + np.abs(want) * (U + HALF[t]) + TINY
-        assert (np.abs(got - want)[fine] <= tol[fine]).all()
+        assert (np.abs(got[fine] - want[fine]) <= tol[fine]).all()
         assert (got[~fine] == want[~fine]).all() and (got[~there] == 0).all()
         if not add:
             assert ((got == 0) == (want == 0)).all()
@@ -250,7 +252,7 @@ def test_gradient(shape, dtype, skew):
         distinct, g, mag, count = gradient(ids, lens, R, np64(de), scale, f(np.arange(B * L), d) if p else None)
         tol = mag * (count[:, None] + 3) * U + TINY
         norm = np.sqrt((g * g).sum(1))
-        norm_tol = np.sqrt((tol * tol).sum(1)) + 2 * U * norm
+        norm_tol = np.sqrt((tol * tol).sum(1)) + 8 * U * norm
         for dense in (False, True):
             grads, norms, ws = backward(o, de, scale, drop, dense, R)
             got, gn = np64(grads), np64(norms)
@@ -289,7 +291,7 @@ def test_gradient_that_is_not_finite_and_one_beyond_the_norms_square():
     grads, norms, _ = backward(o, de, 1.0, None, False, 4)
     assert torch.isnan(grads[0]).sum() == 1 and bool(torch.isnan(norms[0]))
     assert float(grads[1, 4]) == float("inf") and float(norms[1]) == float("inf")
-    assert abs(float(norms[3]) / (1e30 * np.sqrt(40)) - 1) <= 3 * U and float(norms[2]) == pytest.approx(np.sqrt(40), rel=2 * U)
+    assert abs(float(norms[3]) / (1e30 * np.sqrt(40)) - 1) <= 8 * U and abs(float(norms[2]) / np.sqrt(40) - 1) <= 8 * U
 
 
 def test_gradient_against_differences():
@@ -440,15 +442,13 @@ def step_of(B, L, d, R, seed):
 def test_a_step_against_autograd():
     B, L, d, R = 6, 50, 48, 70
     gradients, update, key, out, (ids, lens, W, o) = step_of(B, L, d, R, 1)
-    for t in out.values():
-        t.zero_() if t.dtype == torch.int32 else None
     gradients()
     there = torch.from_numpy(named(ids.cpu().numpy(), lens.cpu().numpy(), R)).to(DEV)
     f = [torch.from_numpy(factors(np.arange(B * L), d, p, 12345, 0, site)).to(DEV).view(B, L, d) for p, site in ((0.1, 0), (0.2, 1))]
     w = out["w"].double().requires_grad_()
     H = torch.where(there[..., None], w[ids.long().masked_fill(~there, 0)] * 8.0 * f[0] * f[1], 0.0)
     G, = torch.autograd.grad((H * W.double()).sum(), w)
-    count, n = o.counts.tolist()
+    count = int(o.counts[0])
     named_rows = o.rows[:count].long()
     _, _, mag, terms = gradient(ids.cpu().numpy(), lens.cpu().numpy(), R, np64(W) * np64(f[1]), 8.0, np64(f[0]).reshape(-1, d))
     off = np.abs(np64(out["g"])[:count] - np64(G[named_rows]))
@@ -471,6 +471,10 @@ def test_a_step_on_another_stream_and_in_a_graph(shape):
     """Steps, each with the next step's masks: eager, on another stream, and replayed from a graph with eager work between the replays; two
     graphs of two models in turn."""
     runs = [step_of(*shape, seed) for seed in (1, 2)]
+    for run in runs:                                                                      # (what no call has written compares as well)
+        for k in ("E", "H", "norms", "norm"):
+            run[3][k].zero_()
+        run[3]["tokens"].fill_(-1)
     start = [{k: v.clone() for k, v in run[3].items()} for run in runs]
 
     def back():
@@ -485,21 +489,11 @@ def test_a_step_on_another_stream_and_in_a_graph(shape):
             for gradients, update, key, out, _ in runs:
                 gradients(stream)
                 update(step, stream)
-                if stream is not None:
-                    with torch.cuda.stream(stream):
-                        key[1] += 1
-                        kept.append({k: v.clone() for k, v in out.items()})
-                else:
+                with torch.cuda.stream(stream or torch.cuda.current_stream()):
                     key[1] += 1
                     kept.append({k: v.clone() for k, v in out.items()})
         return kept
 
-    for t in (x for run in runs for x in (run[3]["E"], run[3]["H"])):
-        t.zero_()
-    for run in runs:
-        run[3]["tokens"].fill_(-1)
-    start = [{k: v.clone() for k, v in run[3].items()} for run in runs]
-    back()
     want = eager()
     assert not torch.equal(want[0]["E"], want[2]["E"])                                    # another mask, and other weights
     back()
@@ -507,7 +501,7 @@ def test_a_step_on_another_stream_and_in_a_graph(shape):
     s.wait_stream(torch.cuda.current_stream())
     got = eager(s)
     torch.cuda.synchronize()
-    same = lambda a, b: all(torch.equal(a[k], b[k]) or bool((a[k].isnan() == b[k].isnan()).all() and torch.equal(a[k].nan_to_num(), b[k].nan_to_num())) for k in a)
+    same = lambda a, b: all(torch.equal(a[k], b[k]) for k in a)
     assert all(same(a, b) for a, b in zip(got, want))
     back()
     graphs = []
@@ -525,7 +519,7 @@ def test_a_step_on_another_stream_and_in_a_graph(shape):
             graph.replay()
             torch.cuda.synchronize()
             update(step)
-            assert same({k: v for k, v in out.items()}, want[at]), (step, at)
+            assert same(out, want[at]), (step, at)
             at += 1
 
 
