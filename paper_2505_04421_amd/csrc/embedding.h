@@ -152,6 +152,8 @@ inline Rows rows_of(const longer_rows* r, int B, int L) { return {(char*)r->data
 // an order's arrays (what they hold is the caller's contract, but for what a kernel checks)
 inline int check_order(const longer_order* o) {
   if (!o || !o->tokens || !o->runs || !o->rows || !o->counts) return api_error(LONGER_ERR_ARG, "order: a NULL pointer");
+  if (o->tokens == o->runs || o->tokens == o->rows || o->tokens == o->counts || o->runs == o->rows || o->runs == o->counts || o->rows == o->counts)
+    return api_error(LONGER_ERR_ARG, "order: two of its arrays are the same memory");
   if (((uintptr_t)o->tokens | (uintptr_t)o->runs | (uintptr_t)o->rows | (uintptr_t)o->counts) & 3) return api_error(LONGER_ERR_ARG, "order is not aligned to its elements");
   return 0;
 }

@@ -28,7 +28,7 @@ struct GradParams {
   Mask mask;
   longer_order order;
   int dense;
-  uint32_t out_rows;
+  uint32_t out_rows, blocks, zero_rows;              // blocks: workgroups with tokens; the others write zeros, zero_rows of a dense gradient each
   float *grads, *norms;
   float* part;                                       // [workgroups][2][d]
   Border* borders;                                   // [workgroups]
@@ -113,6 +113,49 @@ __device__ __forceinline__ void finish(const GradParams& p, uint32_t run, uint32
 }
 __device__ __forceinline__ uint32_t row_of(const GradParams& p, uint32_t run) { return p.dense ? (uint32_t)p.order.rows[run] : run; }
 
+// The first of `count` ascending numbers that is not below `from`: 64 places at a time.
+__device__ __forceinline__ uint32_t lower_bound(const int32_t* rows, uint32_t count, uint32_t from) {
+  uint32_t lo = 0, hi = count;
+  while (lo < hi) {
+    const uint32_t step = (hi - lo + 63) / 64, at = lo + (threadIdx.x & 63) * step;
+    const uint32_t below = __popcll(__ballot(at < hi && (uint32_t)rows[min(at, hi - 1)] < from));
+    if (!below) break;
+    hi = min(hi, lo + below * step);
+    lo += (below - 1) * step + 1;
+  }
+  return lo;
+}
+
+// Zeros in the rows of a dense gradient that no token names, and in their norms, beside the workgroups that add up the others': the named rows of this
+// workgroup's share come from the order.  16 KB to a workgroup (300007 rows of 96, 256000 tokens, shares of 4 / 16 / 32 / 64 KB: 47 / 30 / 35 / 36 us
+// in all; zeros in a launch of their own: 35 and that launch's time; 1000003 rows of 128: 103 us for 97 and the launch).
+constexpr uint32_t kMostZeroRows = 2048;
+__device__ __forceinline__ void zero_rows(const GradParams& p, uint32_t part, uint8_t* named) {
+  const uint32_t a = part * p.zero_rows, b = min(a + p.zero_rows, p.out_rows), count = runs_of(p);
+  for (uint32_t i = threadIdx.x; i < p.zero_rows; i += kThreads) named[i] = 0;
+  const uint32_t first = lower_bound(p.order.rows, count, a);
+  __syncthreads();
+  for (uint32_t i = first + threadIdx.x; i < count; i += kThreads) {
+    const uint32_t row = (uint32_t)p.order.rows[i];
+    if (row >= b) break;
+    named[row - a] = 1;
+  }
+  __syncthreads();
+  int shift = 0;                                     // lanes of a row, four values each
+  while (shift < kThreadBits && 4 << shift < p.d) ++shift;
+  const int lane = threadIdx.x & ((1 << shift) - 1);
+  for (uint32_t row = a + (threadIdx.x >> shift); row < b; row += kThreads >> shift) {
+    if (named[row - a]) continue;
+    float* to = p.grads + (size_t)row * p.d;
+    for (int c = 4 * lane; c < p.d; c += 4 << shift) {
+      if (c + 4 <= p.d) __builtin_nontemporal_store(Piece<float, 4>(0.f), (Piece<float, 4>*)(to + c));
+      else
+        for (int k = c; k < p.d; ++k) to[k] = 0.f;
+    }
+    if (p.norms && lane == 0) p.norms[row] = 0.f;
+  }
+}
+
 // LDS of a workgroup's tokens: where their rows of dE lie, their runs (with the neighbours' on both sides), the runs' rows, their numbers
 __host__ __device__ inline size_t staged_bytes(uint32_t block, bool drop) { return (size_t)block * (drop ? 20 : 16) + 8; }
 
@@ -125,11 +168,16 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   __shared__ uint32_t flags[kThreads];
   int64_t* from = staged;
   uint32_t *runs = (uint32_t*)(from + p.block) + 1, *rows = runs + p.block + 1, *tokens = rows + p.block;
+  if (blockIdx.x >= p.blocks) {
+    static_assert(kMostZeroRows <= sizeof(lead), "a byte for each row");
+    if (blockIdx.y == 0) zero_rows(p, blockIdx.x - p.blocks, (uint8_t*)lead);
+    return;
+  }
   const Lane me = lane_of<KIND>(p);
   const int c = me.at.c, width = me.at.n;
   const uint32_t n = tokens_of(p), group = threadIdx.x >> p.shift, groups = kThreads >> p.shift;
   if (p.norms && blockIdx.y == 0 && !p.dense)        // zeros behind the last row's norm
-    for (uint64_t i = (uint64_t)runs_of(p) + blockIdx.x * kThreads + threadIdx.x; i < p.out_rows; i += (uint64_t)gridDim.x * kThreads) p.norms[i] = 0.f;
+    for (uint64_t i = (uint64_t)runs_of(p) + blockIdx.x * kThreads + threadIdx.x; i < p.out_rows; i += (uint64_t)p.blocks * kThreads) p.norms[i] = 0.f;
   if ((uint64_t)blockIdx.x * p.block >= n) {
     if (blockIdx.y == 0 && threadIdx.x == 0) p.borders[blockIdx.x] = {kNone, kNone, 0, 0};
     return;
@@ -244,7 +292,8 @@ constexpr int kJoinThreads = 512;
 // The runs that cross workgroups' stretches, each by the group of the stretch that it begins in, and by the whole workgroup where it
 // goes on for more than U: group k takes every groups-th of its sums, which then meet in two steps.
 template <Kind KIND>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32_t blocks) {
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
+  const uint32_t blocks = p.blocks;
   constexpr uint32_t U = 8;
   __shared__ float lds[kJoinThreads * 8];
   __shared__ uint32_t list[kJoinThreads], listed;
@@ -325,16 +374,6 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p, uint32
   }
 }
 
-// zeros in grads and norms of a dense gradient, a piece of 16 bytes a thread (1000003 rows of 128: 79 us, 6.5 TB/s; 4096 workgroups that take turns: 120)
-__global__ __launch_bounds__(256) void zero_kernel(GradParams p) {
-  const size_t first = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)gridDim.x * 256;
-  const size_t values = (size_t)p.out_rows * p.d, pieces = values / 4;
-  for (size_t i = first; i < pieces; i += step) __builtin_nontemporal_store(Piece<float, 4>(0.f), (Piece<float, 4>*)p.grads + i);
-  if (first < values % 4) p.grads[pieces * 4 + first] = 0.f;
-  if (p.norms)
-    for (size_t i = first; i < p.out_rows; i += step) p.norms[i] = 0.f;
-}
-
 // a row's norm from its chunks' squares
 __global__ __launch_bounds__(256) void norm_kernel(GradParams p) {
   const uint32_t runs = runs_of(p);
@@ -382,8 +421,8 @@ static void grad(const GradParams& p, dim3 grid, hipStream_t st) {
   with_kind(kind_of(p.d), go);
 }
 
-static void join(const GradParams& p, dim3 grid, uint32_t blocks, hipStream_t st) {
-  with_kind(kind_of(p.d), [&](auto kind) { join_kernel<decltype(kind)::value><<<grid, kJoinThreads, 0, st>>>(p, blocks); });
+static void join(const GradParams& p, dim3 grid, hipStream_t st) {
+  with_kind(kind_of(p.d), [&](auto kind) { join_kernel<decltype(kind)::value><<<grid, kJoinThreads, 0, st>>>(p); });
 }
 
 }  // namespace emb
@@ -418,13 +457,12 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   if (ws_bytes < g.bytes) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, g.bytes);
   hipStream_t st = (hipStream_t)stream;
   const emb::GradParams p = {emb::rows_of(de, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, g.shift, g.chunks, g.range, g.block, (float)factor,
-                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares)};
-  if (dense) emb::zero_kernel<<<(unsigned)std::min<size_t>((size_t)out_rows * d / 1024 + 1, 1u << 20), 256, 0, st>>>(p);
-  const dim3 grid(g.blocks, g.chunks);
+                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, g.blocks, std::min(std::max(4096u / (uint32_t)d, 1u), emb::kMostZeroRows), grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares)};
+  const dim3 grid(g.blocks + (dense ? (p.out_rows + p.zero_rows - 1) / p.zero_rows : 0), g.chunks);
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
   else emb::grad<__bf16>(p, grid, st);
   const unsigned per_join = (unsigned)emb::kJoinThreads >> g.shift;
-  if (g.blocks > 1) emb::join(p, dim3((g.blocks + per_join - 1) / per_join, g.chunks), g.blocks, st);
+  if (g.blocks > 1) emb::join(p, dim3((g.blocks + per_join - 1) / per_join, g.chunks), st);
   if (norms_out && g.chunks > 1) emb::norm_kernel<<<std::min((p.n + 255) / 256, 2048u), 256, 0, st>>>(p);
   return launched("embedding gradient");
 }

@@ -123,6 +123,8 @@ def test_sort():
     for f in ("tokens", "runs", "rows", "counts"):
         refused(sort(o=some_order(**{f: None})), "NULL")
         refused(sort(o=some_order(**{f: FAKE + 2})), "not aligned")
+    refused(sort(o=some_order(runs=FAKE)), "the same memory")
+    refused(back(o=some_order(counts=FAKE * 3)), "the same memory")
     refused(sort(ws=None), "ws")
     refused(sort(ws=WS + 64), "ws")
     for B, L, n in ((4, 10, 100), (100, 1000, 7), (100, 1000, 1 << 20), (1000, 1000, (1 << 31) - 1)):
