@@ -219,11 +219,12 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device=None) -> Optional[int]:
+    """The handle of `stream`; None: of the current stream (of `device`, the current one, where the caller has its number)."""
     import torch
     if stream is None:           # (the handle itself where torch gives it, no public name: a Stream object costs as much time as a launch)
         handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return (handle(torch.cuda.current_device()) if handle else torch.cuda.current_stream().cuda_stream) or None
+        return (handle(torch.cuda.current_device() if device is None else device) if handle else torch.cuda.current_stream().cuda_stream) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
@@ -786,12 +787,13 @@ class AdamWRows:
 
 
 def _here(*tensors):
-    """Every tensor on the current device, the one whose stream the call goes to."""
+    """The current device's number, whose stream the call goes to; every tensor has to be there."""
     import torch
     device = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise LongerError("a tensor is not on the current device, cuda:%d" % device)
+    return device
 
 
 _INT_TYPES = {}
@@ -817,10 +819,10 @@ def longer_dropout(X, residual, lens, drop: DropoutMask, Y_out, stream=None):
     if X.dim() != 3:
         raise LongerError("X must be a device tensor [B, L, d]")
     B, L, d = shape = X.shape
-    _here(X, residual, lens, drop.key, Y_out)
+    device = _here(X, residual, lens, drop.key, Y_out)
     x, y = _rows(X, shape, "X"), _rows(Y_out, shape, "Y_out")
     r = None if residual is None else ctypes.byref(_rows(residual, shape, "residual"))
-    _check(load_library().longer_dropout(ctypes.byref(x), r, _lens(lens, B), B, L, d, _mask(drop), ctypes.byref(y), _stream(stream)),
+    _check(load_library().longer_dropout(ctypes.byref(x), r, _lens(lens, B), B, L, d, _mask(drop), ctypes.byref(y), _stream(stream, device)),
            "longer_dropout")
 
 
@@ -831,10 +833,10 @@ def longer_embedding(table, ids, lens, scale, drop: Optional[DropoutMask], E_out
     if table.dim() != 2 or not table.is_cuda or (table.stride(1) != 1 and table.shape[1] > 1):
         raise LongerError("table must be a device tensor [rows, d] whose rows have adjacent values")
     i, (B, L), d = _ids(ids), ids.shape, table.shape[1]
-    _here(table, ids, lens, E_out, None if drop is None else drop.key)
+    device = _here(table, ids, lens, E_out, None if drop is None else drop.key)
     t, e = CTable(table.data_ptr(), table.shape[0], table.stride(0), _tensor_dtype(table)), _rows(E_out, (B, L, d), "E_out")
     _check(load_library().longer_embedding(ctypes.byref(t), ctypes.byref(i), _lens(lens, B), B, L, d, scale, _mask(drop), ctypes.byref(e),
-                                           _stream(stream)), "longer_embedding")
+                                           _stream(stream, device)), "longer_embedding")
 
 
 def longer_sort_ids_workspace_bytes(B: int, L: int, table_rows: int) -> int:
@@ -845,10 +847,10 @@ def longer_sort_ids(ids, lens, table_rows, order: TokenOrder, ws, stream=None):
     """order = the tokens of ids [B, L] that name one of table_rows rows, by item."""
     _require_gpu()
     i, (B, L) = _ids(ids), ids.shape
-    _here(ids, lens, order.tokens, order.runs, order.rows, order.counts, ws)
+    device = _here(ids, lens, order.tokens, order.runs, order.rows, order.counts, ws)
     order._holds(B * L, table_rows)
     _check(load_library().longer_sort_ids(ctypes.byref(i), _lens(lens, B), B, L, table_rows, ctypes.byref(order.struct), _ptr(ws),
-                                          ws.numel() * ws.element_size(), _stream(stream)), "longer_sort_ids")
+                                          ws.numel() * ws.element_size(), _stream(stream, device)), "longer_sort_ids")
 
 
 def longer_embedding_backward_workspace_bytes(B: int, L: int, d: int) -> int:
@@ -867,14 +869,14 @@ def longer_embedding_backward(order: TokenOrder, dE, scale, drop: Optional[Dropo
     de = _rows(dE, shape, "dE")
     if grads_out.dim() != 2 or grads_out.shape[1] != d or grads_out.dtype != torch.float32:
         raise LongerError("grads_out must be a float32 tensor [rows, %d]" % d)
-    _here(dE, grads_out, norms_out, ws, order.tokens, None if drop is None else drop.key)
+    device = _here(dE, grads_out, norms_out, ws, order.tokens, None if drop is None else drop.key)
     order._holds(B * L, 0)
     if not dense and grads_out.shape[0] < min(order.rows.numel(), B * L):
         raise LongerError("grads_out must have a row for each of the order's %d" % min(order.rows.numel(), B * L))
     norms = None if norms_out is None else _vector(norms_out, grads_out.shape[0], torch.float32, "norms_out")
     _check(load_library().longer_embedding_backward(ctypes.byref(order.struct), ctypes.byref(de), B, L, d, scale, _mask(drop), int(bool(dense)),
                                                     grads_out.shape[0], _ptr(grads_out), norms, _ptr(ws), ws.numel() * ws.element_size(),
-                                                    _stream(stream)), "longer_embedding_backward")
+                                                    _stream(stream, device)), "longer_embedding_backward")
 
 
 def longer_adamw_rows(table: AdamWRows, order: TokenOrder, g, norm, lr, beta1, beta2, eps, step, stream=None):
@@ -884,11 +886,11 @@ def longer_adamw_rows(table: AdamWRows, order: TokenOrder, g, norm, lr, beta1, b
     _require_gpu()
     if g.dim() != 2 or g.shape[1] != table.d or g.dtype != torch.float32:
         raise LongerError("g must be a float32 tensor [rows, %d]" % table.d)
-    _here(table.tensors[0], order.rows, g, norm)
+    device = _here(table.tensors[0], order.rows, g, norm)
     most = min(order.rows.numel(), table.rows)
     if g.shape[0] < most:
         raise LongerError("g must have a row for each of the order's %d" % most)
     how = CAdamW(lr, beta1, beta2, eps, step)
     _check(load_library().longer_adamw_rows(ctypes.byref(table.struct), ctypes.byref(order.struct), 1, order.rows.numel(), _ptr(g), ctypes.byref(how),
-                                            None if norm is None else _vector(norm, 2, torch.float32, "norm"), _stream(stream)),
+                                            None if norm is None else _vector(norm, 2, torch.float32, "norm"), _stream(stream, device)),
            "longer_adamw_rows")

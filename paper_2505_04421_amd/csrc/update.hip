@@ -261,7 +261,8 @@ __global__ __launch_bounds__(kStepPiece / 4) void step_kernel(StepArgs a) {
 }
 
 // The rows of a table that a batch names: row i of g is the gradient of row rows[i].  2^shift lanes hold a row, four values each.
-// Bound by memory: 400 thousand rows of 128 in 292 us, 5.3 TB/s, everything past the caches (305 with ordinary accesses); the grid is as large as
+// Bound by memory: 400 thousand rows of 128 in 292 us, 5.3 TB/s, p, m, v and w past the caches (305 with ordinary accesses), g, which the gradient's pass
+// has left there, not.  The grid is as large as
 // pays where the count, which is on the GPU, turns out small (2048 / 16384 / 65536 workgroups: 140 thousand rows 113 / 105 / 114).
 struct RowsArgs {
   float *p, *m, *v;
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
     W* ws = (W*)a.w;
     for (int k = (threadIdx.x & (lanes - 1)) * 4; k < a.d; k += lanes * 4) {
       if (k + 4 <= a.d) {
-        const Four<float> g = __builtin_nontemporal_load((const Four<float>*)(gs + k));
+        const Four<float> g = *(const Four<float>*)(gs + k);
         Four<float> m = __builtin_nontemporal_load((const Four<float>*)(a.m + at + k)), v = __builtin_nontemporal_load((const Four<float>*)(a.v + at + k)), p = __builtin_nontemporal_load((const Four<float>*)(a.p + at + k));
         Four<W> w;
 #pragma unroll
