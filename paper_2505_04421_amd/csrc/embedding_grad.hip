@@ -289,12 +289,34 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
 
 constexpr int kJoinThreads = 512;
 
+// The sums of stretches h, h + by, ..., U of them under way at once, while they go on with the run; says whether the last one did.  (A
+// stretch that does not has left nothing to read: what is there is not used.)
+template <Kind KIND, uint32_t U>
+__device__ __forceinline__ bool add_leads(const GradParams& p, float (&acc)[8], uint32_t h, uint32_t by, uint32_t run, int c, int width) {
+  uint32_t lead[U];
+  Piece<float, 8> x[U];
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    const uint32_t i = min(h + u * by, p.blocks - 1);
+    lead[u] = h + u * by < p.blocks ? p.borders[i].lead : kNone;
+    x[u] = load8<float, KIND>(p.part + (size_t)i * 2 * p.d + c, width);
+  }
+  bool more = true;
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    more &= lead[u] == run;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] += more ? x[u][j] : 0.f;
+  }
+  return more;
+}
+
 // The runs that cross workgroups' stretches, each by the group of the stretch that it begins in, and by the whole workgroup where it
-// goes on for more than U: group k takes every groups-th of its sums, which then meet in two steps.
+// goes on for more than ALONE: group k takes every groups-th of its sums, which then meet in two steps.  Bound by its loads' latency: 512000 tokens of
+// 128 in 10.6 us with ALONE 4, 11.8 with 8; 230 thousand tokens of one item in 11.4 us with 8 sums of a group under way, 14.2 with 4.
 template <Kind KIND>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
-  const uint32_t blocks = p.blocks;
-  constexpr uint32_t U = 8;
+  constexpr uint32_t ALONE = 4;
   __shared__ float lds[kJoinThreads * 8];
   __shared__ uint32_t list[kJoinThreads], listed;
   const Lane me = lane_of<KIND>(p);
@@ -303,38 +325,18 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
   const size_t step = (size_t)2 * p.d;
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
-  // the sums of stretches h, h + by, ..., U of them under way at once, while they go on with the run; says whether the last one did
-  // (a stretch that does not has left nothing to read: what is there is not used)
-  auto add = [&](float (&acc)[8], uint32_t h, uint32_t by, uint32_t run) {
-    uint32_t lead[U];
-    Piece<float, 8> x[U];
-#pragma unroll
-    for (uint32_t u = 0; u < U; ++u) {
-      const uint32_t i = min(h + u * by, blocks - 1);
-      lead[u] = h + u * by < blocks ? p.borders[i].lead : kNone;
-      x[u] = load8<float, KIND>(p.part + i * step + c, width);
-    }
-    bool more = true;
-#pragma unroll
-    for (uint32_t u = 0; u < U; ++u) {
-      more &= lead[u] == run;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += more ? x[u][j] : 0.f;
-    }
-    return more;
-  };
-  if (g < blocks) {
+  if (g < p.blocks) {
     const Border own = p.borders[g];
     const Piece<float, 8> x = load8<float, KIND>(p.part + g * step + p.d + c, width);
     float acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = x[j];
-    const uint32_t after = g + U + 1 < blocks ? p.borders[g + U + 1].lead : kNone;
+    const uint32_t after = g + ALONE + 1 < p.blocks ? p.borders[g + ALONE + 1].lead : kNone;
     if (own.tail != kNone) {
       if (after == own.tail) {
         if (me.lane == 0) list[atomicAdd(&listed, 1u)] = g;          // (the order of the list is that of the work alone)
       } else {
-        add(acc, g + 1, 1, own.tail);
+        add_leads<KIND, ALONE>(p, acc, g + 1, 1, own.tail, c, width);
         finish<KIND>(p, own.tail, own.row, me, acc);
       }
     }
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
     const uint32_t a = list[i];
     const Border own = p.borders[a];
     float acc[8] = {};
-    for (uint32_t h = a + 1 + group; add(acc, h, groups, own.tail); h += U * groups) {}
+    for (uint32_t h = a + 1 + group; add_leads<KIND, 8>(p, acc, h, groups, own.tail, c, width); h += 8 * groups) {}
     if (group == 0) {
       const Piece<float, 8> x = load8<float, KIND>(p.part + a * step + p.d + c, width);
 #pragma unroll
@@ -387,10 +389,14 @@ __global__ __launch_bounds__(256) void norm_kernel(GradParams p) {
 }
 
 // ------------------------------------------------------------------------------------ host
-// Tokens of a range: as many as leave 8192 waves, 4 to 32, and 2048 of a workgroup at most.
+// Tokens of a range: 32 where that leaves 8192 waves (and a workgroup at most 2048), down to 8 for as many, 4 where 8 leave less than 4096.
+// (512000 tokens of 128, ranges of 8 / 16 / 32: 74 / 82 / 85 us; 2.6 million: 312 / 320 / 330, but crossings 20 / 18 / 13, and of one item in
+// most places 170 / 85 / 50; 4503 tokens of 4099, 4 / 8 / 16: with the crossings 21.7 / 19.3 / 19.0.)
 static uint32_t range_of(int64_t n, int shift, int chunks) {
+  auto waves = [&](uint32_t s) { return (n / s * chunks << shift) / 64; };
   uint32_t s = std::min(32u, 2048u >> (kThreadBits - shift));
-  while (s > 4 && (n / s * chunks << shift) < (int64_t)8192 * 64) s /= 2;
+  while (s > 8 && waves(s) < 8192) s /= 2;
+  if (s == 8 && waves(s) < 4096) s = 4;
   return s;
 }
 
