@@ -111,8 +111,6 @@ __device__ __forceinline__ void finish(const GradParams& p, uint32_t run, uint32
     else p.norms[row] = squares == s ? sqrtf(s) : (float)sqrt(squares);
   }
 }
-__device__ __forceinline__ uint32_t row_of(const GradParams& p, uint32_t run) { return p.dense ? (uint32_t)p.order.rows[run] : run; }
-
 // The first of `count` ascending numbers that is not below `from`: 64 places at a time.
 __device__ __forceinline__ uint32_t lower_bound(const int32_t* rows, uint32_t count, uint32_t from) {
   uint32_t lo = 0, hi = count;
@@ -131,14 +129,14 @@ __device__ __forceinline__ uint32_t lower_bound(const int32_t* rows, uint32_t co
 // in all; zeros in a launch of their own: 35 and that launch's time; 1000003 rows of 128: 103 us for 97 and the launch).
 constexpr uint32_t kMostZeroRows = 2048;
 __device__ __forceinline__ void zero_rows(const GradParams& p, uint32_t part, uint8_t* named) {
-  const uint32_t a = part * p.zero_rows, b = min(a + p.zero_rows, p.out_rows), count = runs_of(p);
+  const uint32_t a = part * p.zero_rows, b = min(a + p.zero_rows, p.out_rows), count = min(runs_of(p), p.out_rows);
   for (uint32_t i = threadIdx.x; i < p.zero_rows; i += kThreads) named[i] = 0;
   const uint32_t first = lower_bound(p.order.rows, count, a);
   __syncthreads();
   for (uint32_t i = first + threadIdx.x; i < count; i += kThreads) {
     const uint32_t row = (uint32_t)p.order.rows[i];
     if (row >= b) break;
-    named[row - a] = 1;
+    if (row >= a) named[row - a] = 1;
   }
   __syncthreads();
   int shift = 0;                                     // lanes of a row, four values each
@@ -184,11 +182,13 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   }
   const uint32_t first = blockIdx.x * p.block, count = min(p.block, n - first);
   const Key key = DROP ? load_key(p.mask) : Key{};
+  // (whatever the order holds, nothing outside the buffers is read or written: rows ascend, so that a run has no row below its number)
+  const uint32_t most = min(p.n, p.out_rows);
   for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
     const uint32_t token = (uint32_t)p.order.tokens[first + i], run = (uint32_t)p.order.runs[first + i], b = p.by_L(token), l = token - b * p.L;
     from[i] = token < p.n ? (int64_t)b * p.de.user + (int64_t)l * p.de.row : 0;
     runs[i] = run;
-    rows[i] = p.dense ? (uint32_t)p.order.rows[run] : run;
+    rows[i] = run >= most ? kNone : p.dense ? (uint32_t)p.order.rows[run] : run;
     if (DROP) tokens[i] = token;
   }
   if (threadIdx.x == 0) {
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
 
 // a row's norm from its chunks' squares
 __global__ __launch_bounds__(256) void norm_kernel(GradParams p) {
-  const uint32_t runs = runs_of(p);
+  const uint32_t runs = min(runs_of(p), p.out_rows);
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < runs; i += gridDim.x * 256) {
     const uint32_t row = p.dense ? (uint32_t)p.order.rows[i] : i;
     if (row >= p.out_rows) continue;

@@ -113,7 +113,8 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t* lds, uint32
 // ------------------------------------------------------------------------------------ few tokens: one workgroup
 constexpr int kFewThreads = 1024, kFewItems = 8, kFew = kFewThreads * kFewItems, kFewWaves = kFewThreads / 64;
 
-// A wave takes 64 * items neighbours; rounds of up to kMostBits bits, all in LDS.  (6144 tokens of 1000 rows: ... us)
+// A wave takes 64 * items neighbours; rounds of up to kMostBits bits, all in LDS.  (6144 tokens of 1000 rows: 11.4 us, 256
+// tokens 5.6: bound by the one compute unit that they are on)
 __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int per_round, longer_order out) {
   __shared__ alignas(16) uint32_t keys[kFew], words[kFewWaves << (kMostBits - 1)], base[1 << kMostBits];
   __shared__ uint32_t lds[kFewWaves];
@@ -210,8 +211,9 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 // ------------------------------------------------------------------------------------ many tokens
 // A round of the sort takes one digit, in three launches: every workgroup counts the digits of its stretch of the items, the counts are summed
 // over the workgroups before it, and it moves its items.  The first round reads the ids themselves and drops the tokens that name no
-// row; between rounds an item is a word of eight bytes, id below and token above.  (The sums inside the move, each workgroup reading all
-// counts: the three together 27 us for 18.)
+// row; between rounds an item is a word of eight bytes, id below and token above.  (The sums inside the move, each workgroup reading
+// all counts: 30 us a round for 24.)  512000 tokens of 1000003 rows take 38 us, of which each launch's own time is a third: count 4.5, sums 5, move 13
+// and 10, bound by latency and the scattered stores; 14 MB have to move.
 //
 // The runs' numbers need no pass over the sorted ids where the table has at most 2^22 rows.  One round (up to 2^11 rows): a digit is an id, and its run the
 // number of digits before it whose count is not zero.  Two rounds: the first one's move leaves a byte at each id that it meets, the second

@@ -283,6 +283,29 @@ def test_gradient_of_an_item_in_every_place():
         assert (np.abs(np64(grads)[:len(distinct)] - g) <= mag * (count[:, None] + 3) * U).all()
 
 
+@pytest.mark.parametrize("width", [24, 33, 600])
+def test_an_order_that_was_never_sorted(width):
+    """What an order holds is the caller's contract, but whatever it holds, reads and writes stay inside the buffers."""
+    B, L, R = 4, 300, 90
+    r = np.random.default_rng(9)
+    o, guards = fresh_order(B * L, R)
+    de = torch.randn(B, L, width, device=DEV)
+    p, g0 = guarded_empty(DEV, (R, width), torch.float32)
+    m, g1 = guarded_empty(DEV, (R, width), torch.float32)
+    v = torch.zeros(R, width, device=DEV)
+    for low, high in ((-(1 << 31), 1 << 31), (-5, 2 * R), (0, B * L)):
+        for t in (o.tokens, o.runs, o.rows):
+            t.copy_(torch.from_numpy(r.integers(low, high, t.numel()).astype(np.int32)))
+        for counts in ((1 << 30, 1 << 30), (-7, -7), (50, 1 << 30), (1 << 30, 700)):
+            o.counts.copy_(torch.tensor(counts, dtype=torch.int32))
+            for dense in (False, True):
+                backward(o, de, 1.0, None, dense, R)
+            lg.longer_adamw_rows(lg.AdamWRows(p, m, v, None, 0.0), o, torch.zeros(R, width, device=DEV), None, 1e-3, 0.9, 0.99, 1e-8, 1)
+            torch.cuda.synchronize()
+            for g in guards + [g0, g1]:
+                g.check("order")
+
+
 def test_gradient_that_is_not_finite_and_one_beyond_the_norms_square():
     ids = np.array([[0, 1, 2, 1, 3]])
     de = torch.ones(1, 5, 40, device=DEV)
