@@ -220,6 +220,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 // one's count makes of them, for every 32 ids, a mask and how many ids there are before it in its 2048, and the second move looks its ids up.
 // Larger tables take three rounds and two launches that number the runs of the sorted ids.
 constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostGroups = 256;
+constexpr int kSumAlone = 64;                        // groups whose counts each workgroup adds up itself, for want of anything to do
 constexpr int kMaskRows = 32, kSegment = 2048;       // ids of a mask, and of a segment: a wave's
 
 struct Round {
@@ -233,19 +234,21 @@ struct Round {
   uint32_t* keys;                                    // the sorted ids, where the runs are numbered from them
   longer_order order;
   int shift, bits, id_bits;
+  uint32_t groups;                                   // workgroups with items; those behind them help with the ids that were seen
+  int summed;                                     // summed: counts and totals are sums; else each workgroup adds up the counts itself
 };
 
 // Workgroups go to the eight chiplets in turn, each with a second-level cache of its own.  Neighbouring stretches, whose items land side by side,
 // go to one chiplet: it has whole lines to write back, not an eighth of each.
-__device__ __forceinline__ uint32_t group_number() {
-  const uint32_t chip = blockIdx.x & 7, each = gridDim.x / 8, more = gridDim.x % 8;
-  return chip * each + min(chip, more) + blockIdx.x / 8;
+__device__ __forceinline__ uint32_t group_number(uint32_t groups) {
+  const uint32_t chip = blockIdx.x & 7, each = groups / 8, more = groups % 8;
+  return blockIdx.x < groups ? chip * each + min(chip, more) + blockIdx.x / 8 : blockIdx.x;
 }
 
-// a workgroup's stretch of n items: whole tiles, as even as they can be dealt
+// a workgroup's stretch of n items: whole tiles, as even as they can be dealt (behind the last group: none)
 struct Stretch { uint32_t begin, end; };
-__device__ __forceinline__ Stretch stretch(uint32_t n, uint32_t group) {
-  const uint32_t tiles = (n + kTile - 1) / kTile, per = (tiles + gridDim.x - 1) / gridDim.x;
+__device__ __forceinline__ Stretch stretch(uint32_t n, uint32_t group, uint32_t groups) {
+  const uint32_t tiles = (n + kTile - 1) / kTile, per = (tiles + groups - 1) / groups;
   const uint32_t begin = min((uint64_t)group * per * kTile, (uint64_t)n);
   return {begin, (uint32_t)min((uint64_t)begin + (uint64_t)per * kTile, (uint64_t)n)};
 }
@@ -259,8 +262,8 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
   const uint32_t digits = 1u << r.bits;
   for (uint32_t i = threadIdx.x; i < digits; i += kThreads) count[i] = 0;
   __syncthreads();
-  const uint32_t group = group_number();
-  const Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group);
+  const uint32_t group = group_number(r.groups);
+  const Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group, r.groups);
   for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
     uint32_t key[kItems];
 #pragma unroll
@@ -290,7 +293,8 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
     }
   }
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < digits; i += kThreads) r.counts[(size_t)group * digits + i] = count[i];
+  if (group < r.groups)
+    for (uint32_t i = threadIdx.x; i < digits; i += kThreads) r.counts[(size_t)group * digits + i] = count[i];
 }
 
 // counts[g][digit] becomes the sum over the groups before g, totals[digit] that over all: 32 digits a workgroup, 32 shares of the groups
@@ -324,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
   static_assert((1 << kMostBits) <= 4 * kThreads, "a thread has four digits");
   __shared__ alignas(16) uint32_t words[kWaves << (kMostBits - 1)], base[1 << kMostBits], runs[1 << kMostBits];
   __shared__ uint32_t lds[kWaves];
-  const uint32_t digits = 1u << r.bits, group = group_number(), four = 4 * threadIdx.x;
+  const uint32_t digits = 1u << r.bits, group = group_number(r.groups), four = 4 * threadIdx.x;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   uint32_t key[kItems], token[kItems], digit[kItems], at[kItems];
   bool there[kItems];
@@ -340,15 +344,29 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
       }
     }
   };
-  Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group);
+  Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group, r.groups);
   load(s.begin, s.end);                              // (under way while the digits' places are found)
   // where each digit begins, and in it this workgroup
   uint32_t n, named = 0;
   {
     u32x4 all = {}, mine = {};
     if (four < digits) {
-      all = *(const u32x4*)(r.totals + four);
-      mine = *(const u32x4*)(r.counts + (size_t)group * digits + four);
+      if (r.summed) {
+        all = *(const u32x4*)(r.totals + four);
+        mine = *(const u32x4*)(r.counts + (size_t)min(group, r.groups - 1) * digits + four);
+      } else {
+        constexpr uint32_t U = 16;
+        for (uint32_t g = 0; g < r.groups; g += U) {
+          u32x4 c[U];
+#pragma unroll
+          for (uint32_t u = 0; u < U; ++u) c[u] = *(const u32x4*)(r.counts + (size_t)min(g + u, r.groups - 1) * digits + four);
+#pragma unroll
+          for (uint32_t u = 0; u < U; ++u) {
+            all += g + u < r.groups ? c[u] : u32x4{};
+            mine += g + u < group ? c[u] : u32x4{};
+          }
+        }
+      }
     }
     const uint32_t before = group_scan<kThreads>(all[0] + all[1] + all[2] + all[3], lds, &n);
     if (four < digits) *(u32x4*)(base + four) = mine + u32x4{before, before + all[0], before + all[0] + all[1], before + all[0] + all[1] + all[2]};
@@ -425,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
 // how many runs begin in each workgroup's stretch of the sorted ids
 __global__ __launch_bounds__(kThreads) void heads_kernel(const uint32_t* keys, const int32_t* n, uint32_t* heads) {
   __shared__ uint32_t lds[kWaves];
-  const Stretch s = stretch((uint32_t)*n, blockIdx.x);
+  const Stretch s = stretch((uint32_t)*n, blockIdx.x, gridDim.x);
   uint32_t mine = 0, all;
   for (uint32_t k = s.begin + threadIdx.x; k < s.end; k += kThreads) mine += k == 0 || keys[k] != keys[k - 1];
   group_scan<kThreads>(mine, lds, &all);
@@ -437,7 +455,7 @@ __global__ __launch_bounds__(kThreads) void runs_kernel(const uint32_t* keys, co
   __shared__ uint32_t lds[kWaves];
   uint32_t run, all;
   group_scan<kThreads>(threadIdx.x < blockIdx.x ? heads[threadIdx.x] : 0, lds, &run);
-  const Stretch s = stretch((uint32_t)out.counts[1], blockIdx.x);
+  const Stretch s = stretch((uint32_t)out.counts[1], blockIdx.x, gridDim.x);
   for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
     const uint32_t first = tile + threadIdx.x * kItems;
     uint32_t key[kItems], before = first && first < s.end ? keys[first - 1] : kNone, mine = 0;
@@ -537,21 +555,23 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
   uint64_t* items[2] = {(uint64_t*)w, (uint64_t*)(w + p.items)};
   uint32_t* keys = (uint32_t*)(w + p.keys);
   srt::Round r = {a, nullptr, items[0], (uint32_t*)(w + p.counts), (uint32_t*)(w + p.totals), p.rounds == 2 ? (uint8_t*)(w + p.seen) : nullptr, (uint64_t*)(w + p.masks), (uint32_t*)(w + p.segments), keys, *order,
-                  0, p.per_round, p.bits};
+                  0, p.per_round, p.bits, (uint32_t)p.groups, p.groups > srt::kSumAlone};
+  // (a wave for each segment of the ids that may have been seen: 9000 tokens of 1000003 rows 37 us with the items' 5 workgroups alone)
+  const int grid = p.rounds == 2 ? std::max(p.groups, (1 << p.bits >> 11) / srt::kWaves) : p.groups;
   for (int i = 0; i < p.rounds; ++i) {
     r.in = i ? items[(i - 1) & 1] : nullptr;
     r.out = items[i & 1];
     r.shift = i * p.per_round;
     r.bits = p.per_round;                            // (the last round's digits may pass the ids' bits)
     const uint32_t digits = 1u << r.bits;
-    if (i == 0) srt::count_kernel<true><<<p.groups, srt::kThreads, 0, st>>>(r);
-    else srt::count_kernel<false><<<p.groups, srt::kThreads, 0, st>>>(r);
-    srt::sum_kernel<<<(digits + 31) / 32, 1024, 0, st>>>(r.counts, r.totals, p.groups, digits);
+    if (i == 0) srt::count_kernel<true><<<grid, srt::kThreads, 0, st>>>(r);
+    else srt::count_kernel<false><<<grid, srt::kThreads, 0, st>>>(r);
+    if (r.summed) srt::sum_kernel<<<(digits + 31) / 32, 1024, 0, st>>>(r.counts, r.totals, p.groups, digits);
     const int last = i + 1 < p.rounds ? 0 : p.rounds <= 2 ? 1 : 2;
     if (i == 0 && last) srt::move_kernel<true, 1><<<p.groups, srt::kThreads, 0, st>>>(r);
     else if (i == 0) srt::move_kernel<true, 0><<<p.groups, srt::kThreads, 0, st>>>(r);
     else if (last == 0) srt::move_kernel<false, 0><<<p.groups, srt::kThreads, 0, st>>>(r);
-    else if (last == 1) srt::move_kernel<false, 1><<<p.groups, srt::kThreads, 0, st>>>(r);
+    else if (last == 1) srt::move_kernel<false, 1><<<grid, srt::kThreads, 0, st>>>(r);
     else srt::move_kernel<false, 2><<<p.groups, srt::kThreads, 0, st>>>(r);
   }
   if (p.rounds > 2) {
