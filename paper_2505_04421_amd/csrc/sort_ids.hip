@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 // number of digits before it whose count is not zero.  Two rounds: the first one's move leaves a byte at each id that it meets, the second
 // one's count makes of them, for every 32 ids, a mask and how many ids there are before it in its 2048, and the second move looks its ids up.
 // Larger tables take three rounds and two launches that number the runs of the sorted ids.
-constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostGroups = 256;
+constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostGroups = 512;
 constexpr int kSumAlone = 64;                        // groups whose counts each workgroup adds up itself, for want of anything to do
 constexpr int kMaskRows = 32, kSegment = 2048;       // ids of a mask, and of a segment: a wave's
 
@@ -297,17 +297,17 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
     for (uint32_t i = threadIdx.x; i < digits; i += kThreads) r.counts[(size_t)group * digits + i] = count[i];
 }
 
-// counts[g][digit] becomes the sum over the groups before g, totals[digit] that over all: 32 digits a workgroup, 32 shares of the groups
+// counts[g][digit] becomes the sum over the groups before g, totals[digit] that over all: 32 digits a workgroup, 32 shares of SHARE groups at most
+template <int SHARE>
 __global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* totals, int groups, uint32_t digits) {
-  constexpr int kShare = kMostGroups / 32;
   __shared__ uint32_t lds[32][33];
   const uint32_t digit = blockIdx.x * 32 + (threadIdx.x & 31);
   const int share = threadIdx.x >> 5, per = (groups + 31) / 32, begin = share * per, mine = max(min(groups - begin, per), 0);
-  uint32_t sum = 0, c[kShare];
+  uint32_t sum = 0, c[SHARE];
 #pragma unroll
-  for (int k = 0; k < kShare; ++k) c[k] = k < mine && digit < digits ? counts[(size_t)(begin + k) * digits + digit] : 0;
+  for (int k = 0; k < SHARE; ++k) c[k] = k < mine && digit < digits ? counts[(size_t)(begin + k) * digits + digit] : 0;
 #pragma unroll
-  for (int k = 0; k < kShare; ++k) sum += c[k];
+  for (int k = 0; k < SHARE; ++k) sum += c[k];
   lds[share][threadIdx.x & 31] = sum;
   __syncthreads();
   if (digit >= digits) return;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* t
   for (int i = 0; i < 32; ++i) before += i < share ? lds[i][threadIdx.x & 31] : 0;
   if (share == 31) totals[digit] = before + sum;
 #pragma unroll
-  for (int k = 0; k < kShare; ++k) {
+  for (int k = 0; k < SHARE; ++k) {
     if (k < mine) counts[(size_t)(begin + k) * digits + digit] = before;
     before += c[k];
   }
@@ -566,7 +566,10 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
     const uint32_t digits = 1u << r.bits;
     if (i == 0) srt::count_kernel<true><<<grid, srt::kThreads, 0, st>>>(r);
     else srt::count_kernel<false><<<grid, srt::kThreads, 0, st>>>(r);
-    if (r.summed) srt::sum_kernel<<<(digits + 31) / 32, 1024, 0, st>>>(r.counts, r.totals, p.groups, digits);
+    if (r.summed) {
+      auto sum = p.groups > 256 ? srt::sum_kernel<srt::kMostGroups / 32> : srt::sum_kernel<8>;
+      sum<<<(digits + 31) / 32, 1024, 0, st>>>(r.counts, r.totals, p.groups, digits);
+    }
     const int last = i + 1 < p.rounds ? 0 : p.rounds <= 2 ? 1 : 2;
     if (i == 0 && last) srt::move_kernel<true, 1><<<p.groups, srt::kThreads, 0, st>>>(r);
     else if (i == 0) srt::move_kernel<true, 0><<<p.groups, srt::kThreads, 0, st>>>(r);
