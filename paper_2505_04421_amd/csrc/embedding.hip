@@ -6,6 +6,15 @@ namespace emb {
 
 struct Ids { const char* data; int64_t user, row; const int32_t* lens; uint32_t table_rows; int wide; };
 
+// The lanes of a workgroup that hold a row, 8 values each: as many as it has pieces (a wider row: all of them, in turns), so that no power of two
+// has to be filled; what is left over of a workgroup idles.  A lane's piece is the same in all its rows.
+struct Deal { Divider by_lanes; uint32_t lanes, per_turn; };
+struct Seat { uint32_t lane, row; bool taken; };
+__device__ __forceinline__ Seat seat(const Deal& d) {
+  const uint32_t row = d.by_lanes(threadIdx.x);
+  return {threadIdx.x - row * d.lanes, row, row < d.per_turn};
+}
+
 struct LookupParams {
   const char* table;
   int64_t stride;
@@ -13,7 +22,8 @@ struct LookupParams {
   Rows out;
   Divider by_L;
   uint32_t n, L;
-  int d, shift;                     // 2^shift lanes hold a row
+  int d;
+  Deal deal;
   float factor;
   Mask mask;
 };
@@ -30,9 +40,11 @@ __device__ __forceinline__ int64_t item(const Ids& ids, uint32_t b, uint32_t l) 
 template <typename T, typename O, bool DROP, Kind KIND>
 __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p) {
   constexpr int U = 4;
-  const uint32_t lanes = 1u << p.shift, per_turn = 256 >> p.shift, per_group = per_turn * U;
+  const uint32_t per_turn = p.deal.per_turn, per_group = per_turn * U;
+  const Seat me = seat(p.deal);
+  if (!me.taken) return;
   const Key key = DROP ? load_key(p.mask) : Key{};
-  for (uint32_t first = blockIdx.x * per_group + (threadIdx.x >> p.shift); first < p.n; first += gridDim.x * per_group) {
+  for (uint32_t first = blockIdx.x * per_group + me.row; first < p.n; first += gridDim.x * per_group) {
     int64_t from[U], to[U];
     bool there[U];
 #pragma unroll
@@ -43,7 +55,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p) {
       from[u] = there[u] ? id * p.stride : 0;        // (a token that names no row loads the table's first: no branch around a load)
       to[u] = (int64_t)b * p.out.user + (int64_t)l * p.out.row;
     }
-    for (uint32_t piece = threadIdx.x & (lanes - 1); (int)piece * 8 < p.d; piece += lanes) {
+    for (uint32_t piece = me.lane; (int)piece * 8 < p.d; piece += p.deal.lanes) {
       const Part at = part_of<KIND>(piece, p.d);
       Piece<T, 8> x[U];
 #pragma unroll
@@ -70,7 +82,8 @@ struct DropParams {
   const int32_t* lens;
   Divider by_L;
   uint32_t n, L;
-  int d, shift;
+  int d;
+  Deal deal;
   Kind kind;
   float factor;
   Mask mask;
@@ -80,9 +93,11 @@ struct DropParams {
 template <typename T, bool ADD, Kind KIND>
 __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
   constexpr int U = 2;
-  const uint32_t lanes = 1u << p.shift, per_turn = 256 >> p.shift, per_group = per_turn * U;
+  const uint32_t per_turn = p.deal.per_turn, per_group = per_turn * U;
+  const Seat me = seat(p.deal);
+  if (!me.taken) return;
   const Key key = load_key(p.mask);
-  for (uint32_t first = blockIdx.x * per_group + (threadIdx.x >> p.shift); first < p.n; first += gridDim.x * per_group) {
+  for (uint32_t first = blockIdx.x * per_group + me.row; first < p.n; first += gridDim.x * per_group) {
     uint32_t b[U], l[U];
     bool there[U];
 #pragma unroll
@@ -92,7 +107,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
       l[u] = r - b[u] * p.L;
       there[u] = first + u * per_turn < p.n && (!p.lens || (int)l[u] < p.lens[b[u]]);
     }
-    for (uint32_t piece = threadIdx.x & (lanes - 1); (int)piece * 8 < p.d; piece += lanes) {
+    for (uint32_t piece = me.lane; (int)piece * 8 < p.d; piece += p.deal.lanes) {
       const Part at = part_of<KIND>(piece, p.d);
       Piece<T, 8> x[U], add[U];
 #pragma unroll
@@ -124,14 +139,17 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
 }
 
 // ------------------------------------------------------------------------------------ host
-static unsigned groups(uint32_t n, int shift, int turns) {
-  const uint32_t per_group = (256u >> shift) * turns;
-  return std::min<uint32_t>((n + per_group - 1) / per_group, 1u << 22);
+static Deal deal(int d) {
+  const uint32_t lanes = std::min((uint32_t)(d + 7) / 8, 256u);
+  return {divider(lanes), lanes, 256 / lanes};
+}
+static unsigned groups(uint32_t n, const Deal& deal, uint32_t turns) {
+  return std::min((n + deal.per_turn * turns - 1) / (deal.per_turn * turns), 1u << 22);      // (a grid counts threads in 32 bits)
 }
 
 template <typename T, typename O>
 static void lookup(const LookupParams& p, hipStream_t st) {
-  const unsigned g = groups(p.n, p.shift, 4);
+  const unsigned g = groups(p.n, p.deal, 4);
   auto go = [&](auto kind) {
     constexpr Kind KIND = decltype(kind)::value;
     if (p.mask.drop) lookup_kernel<T, O, true, KIND><<<g, 256, 0, st>>>(p);
@@ -142,7 +160,7 @@ static void lookup(const LookupParams& p, hipStream_t st) {
 
 template <typename T>
 static void dropout(const DropParams& p, hipStream_t st) {
-  const unsigned g = groups(p.n, p.shift, 2);
+  const unsigned g = groups(p.n, p.deal, 2);
   auto go = [&](auto kind) {
     constexpr Kind KIND = decltype(kind)::value;
     if (p.residual.data) dropout_kernel<T, true, KIND><<<g, 256, 0, st>>>(p);
@@ -176,7 +194,7 @@ int longer_embedding(const longer_table* table, const longer_ids* ids, const int
   if (rc) return rc;
   const emb::LookupParams p = {(const char*)table->data, table->row_stride,
                                {(const char*)ids->data, B > 1 ? ids->user_stride : 0, L > 1 ? ids->row_stride : 0, lens, (uint32_t)table->rows, ids->type == LONGER_I64},
-                               emb::rows_of(e, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, emb::lanes_shift((d + 7) / 8, 8), (float)factor, emb::mask_of(drop)};
+                               emb::rows_of(e, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, emb::deal(d), (float)factor, emb::mask_of(drop)};
   hipStream_t st = (hipStream_t)stream;
   if (table->dtype == LONGER_F32) e->dtype == LONGER_F32 ? emb::lookup<float, float>(p, st) : emb::lookup<float, __bf16>(p, st);
   else e->dtype == LONGER_F32 ? emb::lookup<__bf16, float>(p, st) : emb::lookup<__bf16, __bf16>(p, st);
@@ -198,7 +216,7 @@ int longer_dropout(const longer_rows* x, const longer_rows* residual, const int3
   if (!rc) rc = emb::check_mask(drop);
   if (rc) return rc;
   const emb::DropParams p = {emb::rows_of(x, B, L), residual ? emb::rows_of(residual, B, L) : emb::Rows{}, emb::rows_of(y, B, L), lens, emb::divider(L), (uint32_t)B * L,
-                             (uint32_t)L, d, emb::lanes_shift((d + 7) / 8, 8), emb::kind_of(d, x->data == y->data || (residual && residual->data == y->data)), (float)emb::kept(drop), emb::mask_of(drop)};
+                             (uint32_t)L, d, emb::deal(d), emb::kind_of(d, x->data == y->data || (residual && residual->data == y->data)), (float)emb::kept(drop), emb::mask_of(drop)};
   if (x->dtype == LONGER_F32) emb::dropout<float>(p, (hipStream_t)stream);
   else emb::dropout<__bf16>(p, (hipStream_t)stream);
   return launched("dropout");
