@@ -36,44 +36,49 @@ __device__ __forceinline__ int64_t item(const Ids& ids, uint32_t b, uint32_t l) 
   return (uint64_t)id < ids.table_rows ? id : -1;
 }
 
-// E[r] = factor * mask * table[id of r], zeros where r is padding or names no row.  Four rows of a lane are under way at once.
+// E[r] = factor * mask * table[id of r], zeros where r is padding or names no row.  A thread finds where a row's values come from and go to, for all
+// lanes that hold the row; four rows of a lane are under way at once.
 template <typename T, typename O, bool DROP, Kind KIND>
 __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p) {
-  constexpr int U = 4;
+  constexpr uint32_t U = 4;
+  struct alignas(16) Way { int64_t from, to; };      // from < 0: nowhere
+  __shared__ Way way[256 * U];
   const uint32_t per_turn = p.deal.per_turn, per_group = per_turn * U;
   const Seat me = seat(p.deal);
-  if (!me.taken) return;
   const Key key = DROP ? load_key(p.mask) : Key{};
-  for (uint32_t first = blockIdx.x * per_group + me.row; first < p.n; first += gridDim.x * per_group) {
-    int64_t from[U], to[U];
-    bool there[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t r = min(first + u * per_turn, p.n - 1), b = p.by_L(r), l = r - b * p.L;
+  for (uint32_t first = blockIdx.x * per_group; first < p.n; first += gridDim.x * per_group) {
+    const uint32_t rows = min(per_group, p.n - first);
+    if (first != blockIdx.x * per_group) __syncthreads();
+    for (uint32_t i = threadIdx.x; i < rows; i += 256) {
+      const uint32_t b = p.by_L(first + i), l = first + i - b * p.L;
       const int64_t id = item(p.ids, b, l);
-      there[u] = id >= 0;
-      from[u] = there[u] ? id * p.stride : 0;        // (a token that names no row loads the table's first: no branch around a load)
-      to[u] = (int64_t)b * p.out.user + (int64_t)l * p.out.row;
+      way[i] = {id < 0 ? -1 : id * p.stride, (int64_t)b * p.out.user + (int64_t)l * p.out.row};
     }
-    for (uint32_t piece = me.lane; (int)piece * 8 < p.d; piece += p.deal.lanes) {
-      const Part at = part_of<KIND>(piece, p.d);
-      Piece<T, 8> x[U];
+    __syncthreads();
+    if (me.taken)
+      for (uint32_t piece = me.lane; (int)piece * 8 < p.d; piece += p.deal.lanes) {
+        const Part at = part_of<KIND>(piece, p.d);
+        Way w[U];
+        Piece<T, 8> x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = load8<T, KIND>((const T*)p.table + from[u] + at.c, at.n);
+        for (uint32_t u = 0; u < U; ++u) w[u] = way[min(me.row + u * per_turn, rows - 1)];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t r = first + u * per_turn;
-        if (r >= p.n) break;
-        Piece<float, 8> y;
+        for (uint32_t u = 0; u < U; ++u)             // (a token that names no row loads the table's first: no branch around a load)
+          x[u] = load8<T, KIND>((const T*)p.table + max(w[u].from, (int64_t)0) + at.c, at.n);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
-        if (DROP) drop8<KIND>(p.mask, key, r, at.c, y);
-        Piece<O, 8> o;
+        for (uint32_t u = 0; u < U; ++u) {
+          const uint32_t r = me.row + u * per_turn;
+          if (r >= rows) break;
+          Piece<float, 8> y;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = there[u] ? (O)y[j] : (O)0.f;
-        store8<O, KIND>((O*)p.out.data + to[u] + at.c, at.n, o);
+          for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
+          if (DROP) drop8<KIND>(p.mask, key, first + r, at.c, y);
+          Piece<O, 8> o;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = w[u].from >= 0 ? (O)y[j] : (O)0.f;
+          store8<O, KIND>((O*)p.out.data + w[u].to + at.c, at.n, o);
+        }
       }
-    }
   }
 }
 
