@@ -94,52 +94,59 @@ struct DropParams {
   Mask mask;
 };
 
-// Y[r] = residual[r] + factor * mask * X[r]; padding zeros, not read.
+// Y[r] = residual[r] + factor * mask * X[r]; padding zeros, not read.  Rows' places as in the lookup.
 template <typename T, bool ADD, Kind KIND>
 __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
-  constexpr int U = 2;
+  constexpr uint32_t U = 2;
+  struct alignas(16) Way { int64_t from, to; };      // from < 0: padding
+  __shared__ Way way[256 * U];
+  __shared__ int64_t add_from[ADD ? 256 * U : 1];
   const uint32_t per_turn = p.deal.per_turn, per_group = per_turn * U;
   const Seat me = seat(p.deal);
-  if (!me.taken) return;
   const Key key = load_key(p.mask);
-  for (uint32_t first = blockIdx.x * per_group + me.row; first < p.n; first += gridDim.x * per_group) {
-    uint32_t b[U], l[U];
-    bool there[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t r = min(first + u * per_turn, p.n - 1);
-      b[u] = p.by_L(r);
-      l[u] = r - b[u] * p.L;
-      there[u] = first + u * per_turn < p.n && (!p.lens || (int)l[u] < p.lens[b[u]]);
+  for (uint32_t first = blockIdx.x * per_group; first < p.n; first += gridDim.x * per_group) {
+    const uint32_t rows = min(per_group, p.n - first);
+    if (first != blockIdx.x * per_group) __syncthreads();
+    for (uint32_t i = threadIdx.x; i < rows; i += 256) {
+      const uint32_t b = p.by_L(first + i), l = first + i - b * p.L;
+      const bool there = !p.lens || (int)l < p.lens[b];
+      way[i] = {there ? (int64_t)b * p.x.user + (int64_t)l * p.x.row : -1, (int64_t)b * p.out.user + (int64_t)l * p.out.row};
+      if (ADD) add_from[i] = (int64_t)b * p.residual.user + (int64_t)l * p.residual.row;
     }
-    for (uint32_t piece = me.lane; (int)piece * 8 < p.d; piece += p.deal.lanes) {
-      const Part at = part_of<KIND>(piece, p.d);
-      Piece<T, 8> x[U], add[U];
+    __syncthreads();
+    if (me.taken)
+      for (uint32_t piece = me.lane; (int)piece * 8 < p.d; piece += p.deal.lanes) {
+        const Part at = part_of<KIND>(piece, p.d);
+        Way w[U];
+        Piece<T, 8> x[U], add[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (there[u]) {
-          x[u] = load8<T, KIND>((const T*)p.x.data + (int64_t)b[u] * p.x.user + (int64_t)l[u] * p.x.row + at.c, at.n);
-          if (ADD) add[u] = load8<T, KIND>((const T*)p.residual.data + (int64_t)b[u] * p.residual.user + (int64_t)l[u] * p.residual.row + at.c, at.n);
+        for (uint32_t u = 0; u < U; ++u) {
+          const uint32_t i = min(me.row + u * per_turn, rows - 1);
+          w[u] = way[i];
+          if (w[u].from >= 0) {
+            x[u] = load8<T, KIND>((const T*)p.x.data + w[u].from + at.c, at.n);
+            if (ADD) add[u] = load8<T, KIND>((const T*)p.residual.data + add_from[i] + at.c, at.n);
+          }
         }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t r = first + u * per_turn;
-        if (r >= p.n) continue;
-        Piece<float, 8> y = 0.f;
-        if (there[u]) {
+        for (uint32_t u = 0; u < U; ++u) {
+          const uint32_t r = me.row + u * per_turn;
+          if (r >= rows) break;
+          Piece<float, 8> y = 0.f;
+          if (w[u].from >= 0) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
-          drop8<KIND>(p.mask, key, r, at.c, y);
-          if (ADD)
+            for (int j = 0; j < 8; ++j) y[j] = (float)x[u][j] * p.factor;
+            drop8<KIND>(p.mask, key, first + r, at.c, y);
+            if (ADD)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] += (float)add[u][j];
+              for (int j = 0; j < 8; ++j) y[j] += (float)add[u][j];
+          }
+          Piece<T, 8> o;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = (T)y[j];
+          store8<T, KIND>((T*)p.out.data + w[u].to + at.c, at.n, o);
         }
-        Piece<T, 8> o;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = (T)y[j];
-        store8<T, KIND>((T*)p.out.data + (int64_t)b[u] * p.out.user + (int64_t)l[u] * p.out.row + at.c, at.n, o);
       }
-    }
   }
 }
 
