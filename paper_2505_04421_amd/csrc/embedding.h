@@ -22,6 +22,19 @@ inline Divider divider(uint32_t by) {
   return {(uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by), shift};
 }
 
+// The lanes of a workgroup of 256 that hold a row, a piece each: as many as it has pieces (a wider row: all of them, in turns), so that no power of two
+// has to be filled; what is left over of a workgroup idles.  A lane's piece is the same in all its rows.
+struct Deal { Divider by_lanes; uint32_t lanes, per_turn; };
+struct Seat { uint32_t lane, row; bool taken; };
+__device__ __forceinline__ Seat seat(const Deal& d) {
+  const uint32_t row = d.by_lanes(threadIdx.x);
+  return {threadIdx.x - row * d.lanes, row, row < d.per_turn};
+}
+inline Deal deal(uint32_t pieces) {
+  const uint32_t lanes = std::min(pieces, 256u);
+  return {divider(lanes), lanes, 256 / lanes};
+}
+
 // The 2^k lanes, at most `most` = 2^m, that hold a row in pieces of 8 values
 inline int lanes_shift(int pieces, int m) {
   int k = 0;

@@ -6,15 +6,6 @@ namespace emb {
 
 struct Ids { const char* data; int64_t user, row; const int32_t* lens; uint32_t table_rows; int wide; };
 
-// The lanes of a workgroup that hold a row, 8 values each: as many as it has pieces (a wider row: all of them, in turns), so that no power of two
-// has to be filled; what is left over of a workgroup idles.  A lane's piece is the same in all its rows.
-struct Deal { Divider by_lanes; uint32_t lanes, per_turn; };
-struct Seat { uint32_t lane, row; bool taken; };
-__device__ __forceinline__ Seat seat(const Deal& d) {
-  const uint32_t row = d.by_lanes(threadIdx.x);
-  return {threadIdx.x - row * d.lanes, row, row < d.per_turn};
-}
-
 struct LookupParams {
   const char* table;
   int64_t stride;
@@ -151,10 +142,6 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
 }
 
 // ------------------------------------------------------------------------------------ host
-static Deal deal(int d) {
-  const uint32_t lanes = std::min((uint32_t)(d + 7) / 8, 256u);
-  return {divider(lanes), lanes, 256 / lanes};
-}
 static unsigned groups(uint32_t n, const Deal& deal, uint32_t turns) {
   return std::min((n + deal.per_turn * turns - 1) / (deal.per_turn * turns), 1u << 22);      // (a grid counts threads in 32 bits)
 }
@@ -206,7 +193,7 @@ int longer_embedding(const longer_table* table, const longer_ids* ids, const int
   if (rc) return rc;
   const emb::LookupParams p = {(const char*)table->data, table->row_stride,
                                {(const char*)ids->data, B > 1 ? ids->user_stride : 0, L > 1 ? ids->row_stride : 0, lens, (uint32_t)table->rows, ids->type == LONGER_I64},
-                               emb::rows_of(e, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, emb::deal(d), (float)factor, emb::mask_of(drop)};
+                               emb::rows_of(e, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, emb::deal((d + 7) / 8), (float)factor, emb::mask_of(drop)};
   hipStream_t st = (hipStream_t)stream;
   if (table->dtype == LONGER_F32) e->dtype == LONGER_F32 ? emb::lookup<float, float>(p, st) : emb::lookup<float, __bf16>(p, st);
   else e->dtype == LONGER_F32 ? emb::lookup<__bf16, float>(p, st) : emb::lookup<__bf16, __bf16>(p, st);
@@ -228,7 +215,7 @@ int longer_dropout(const longer_rows* x, const longer_rows* residual, const int3
   if (!rc) rc = emb::check_mask(drop);
   if (rc) return rc;
   const emb::DropParams p = {emb::rows_of(x, B, L), residual ? emb::rows_of(residual, B, L) : emb::Rows{}, emb::rows_of(y, B, L), lens, emb::divider(L), (uint32_t)B * L,
-                             (uint32_t)L, d, emb::deal(d), emb::kind_of(d, x->data == y->data || (residual && residual->data == y->data)), (float)emb::kept(drop), emb::mask_of(drop)};
+                             (uint32_t)L, d, emb::deal((d + 7) / 8), emb::kind_of(d, x->data == y->data || (residual && residual->data == y->data)), (float)emb::kept(drop), emb::mask_of(drop)};
   if (x->dtype == LONGER_F32) emb::dropout<float>(p, (hipStream_t)stream);
   else emb::dropout<__bf16>(p, (hipStream_t)stream);
   return launched("dropout");

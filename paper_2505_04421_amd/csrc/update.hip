@@ -260,7 +260,7 @@ __global__ __launch_bounds__(kStepPiece / 4) void step_kernel(StepArgs a) {
   else step_piece<float>(a, buffers, at, kind, n, c, decay);
 }
 
-// The rows of a table that a batch names: row i of g is the gradient of row rows[i].  2^shift lanes hold a row, four values each.
+// The rows of a table that a batch names: row i of g is the gradient of row rows[i].  A lane holds four values of a row.
 // Bound by memory: 400 thousand rows of 128 in 292 us, 5.3 TB/s, p, m, v and w past the caches (305 with ordinary accesses), g, which the gradient's pass
 // has left there, not.  The grid is as large as
 // pays where the count, which is on the GPU, turns out small (2048 / 16384 / 65536 workgroups: 140 thousand rows 113 / 105 / 114).
@@ -271,29 +271,40 @@ struct RowsArgs {
   const int32_t *rows, *counts;
   const float* norm;
   uint32_t most, table_rows;                          // rows of g at most, rows of the table
-  int d, shift;
+  int d;
+  emb::Deal deal;
   float decay;                                        // lr * decay
   How how;
 };
 
-template <typename W, bool COPY>
+template <bool PAST>
+__device__ __forceinline__ Four<float> load_four(const float* p) { return PAST ? __builtin_nontemporal_load((const Four<float>*)p) : *(const Four<float>*)p; }
+template <bool PAST, typename T>
+__device__ __forceinline__ void store_four(T* p, Four<T> v) {
+  if (PAST) __builtin_nontemporal_store(v, (Four<T>*)p);
+  else *(Four<T>*)p = v;
+}
+
+template <typename W, bool COPY, bool PAST>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
   float c = 1.f;
   if (a.norm) {
     if (!isfinite(a.norm[0])) return;
     c = a.norm[1];
   }
-  const uint32_t count = min((uint32_t)max(a.counts[0], 0), a.most), lanes = 1u << a.shift, step = gridDim.x * (256 >> a.shift);
-  for (uint32_t i = blockIdx.x * (256 >> a.shift) + (threadIdx.x >> a.shift); i < count; i += step) {
+  const uint32_t count = min((uint32_t)max(a.counts[0], 0), a.most);
+  const emb::Seat me = emb::seat(a.deal);
+  if (!me.taken) return;
+  for (uint32_t i = blockIdx.x * a.deal.per_turn + me.row; i < count; i += gridDim.x * a.deal.per_turn) {
     const uint32_t row = (uint32_t)a.rows[i];
     if (row >= a.table_rows) continue;
     const size_t at = (size_t)row * a.d;
     const float* gs = a.g + (size_t)i * a.d;
     W* ws = (W*)a.w;
-    for (int k = (threadIdx.x & (lanes - 1)) * 4; k < a.d; k += lanes * 4) {
+    for (int k = me.lane * 4; k < a.d; k += a.deal.lanes * 4) {
       if (k + 4 <= a.d) {
         const Four<float> g = *(const Four<float>*)(gs + k);
-        Four<float> m = __builtin_nontemporal_load((const Four<float>*)(a.m + at + k)), v = __builtin_nontemporal_load((const Four<float>*)(a.v + at + k)), p = __builtin_nontemporal_load((const Four<float>*)(a.p + at + k));
+        Four<float> m = load_four<PAST>(a.m + at + k), v = load_four<PAST>(a.v + at + k), p = load_four<PAST>(a.p + at + k);
         Four<W> w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -304,10 +315,10 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
           v[j] = vj;
           w[j] = (W)pj;
         }
-        __builtin_nontemporal_store(m, (Four<float>*)(a.m + at + k));
-        __builtin_nontemporal_store(v, (Four<float>*)(a.v + at + k));
-        __builtin_nontemporal_store(p, (Four<float>*)(a.p + at + k));
-        if (COPY) __builtin_nontemporal_store(w, (Four<W>*)(ws + at + k));
+        store_four<PAST>(a.m + at + k, m);
+        store_four<PAST>(a.v + at + k, v);
+        store_four<PAST>(a.p + at + k, p);
+        if (COPY) store_four<PAST>(ws + at + k, w);
       } else {
         for (int j = k; j < a.d; ++j) {
           float p = a.p[at + j], m = a.m[at + j], v = a.v[at + j];
@@ -566,13 +577,17 @@ int longer_adamw_rows(const longer_adamw_table* t, const longer_order* order, in
   if (!(t->decay >= 0.) || !(how->lr * t->decay <= FLT_MAX)) return api_error(LONGER_ERR_ARG, "decay=%g: not negative, lr decay an fp32 number", t->decay);
   if ((uintptr_t)norm & 3) return api_error(LONGER_ERR_ARG, "norm is not aligned");
   const uint32_t most = (uint32_t)std::min<int64_t>((int64_t)B * L, t->rows);
-  const upd::RowsArgs a = {t->p, t->m, t->v, t->w, g, order->rows, order->counts, norm, most, (uint32_t)t->rows, t->d, emb::lanes_shift((t->d + 3) / 4, 8),
+  const upd::RowsArgs a = {t->p, t->m, t->v, t->w, g, order->rows, order->counts, norm, most, (uint32_t)t->rows, t->d, emb::deal((t->d + 3) / 4),
                            (float)(how->lr * t->decay), h};
-  const unsigned per_group = 256u >> a.shift, groups = std::min((most + per_group - 1) / per_group, 16384u);
+  const unsigned groups = std::min((most + a.deal.per_turn - 1) / a.deal.per_turn, 16384u);
   hipStream_t st = (hipStream_t)stream;
-  if (!t->w) upd::rows_kernel<float, false><<<groups, 256, 0, st>>>(a);
-  else if (t->w_dtype == LONGER_BF16) upd::rows_kernel<__bf16, true><<<groups, 256, 0, st>>>(a);
-  else upd::rows_kernel<float, true><<<groups, 256, 0, st>>>(a);
+  // Whole lines of 128 bytes go past the caches; rows of other widths through them, where the lines that two rows share may meet (140 thousand rows of
+  // 33 / 40 / 100 / 129 values, 16000 of 4099: 97 / 64 / 127 / 170 / 311 us past, 53 / 42 / 135 / 166 / 296 through).
+  const bool past = t->d % 32 == 0 && !(((uintptr_t)t->p | (uintptr_t)t->m | (uintptr_t)t->v) & 127);
+  auto go = [&](auto kernel) { kernel<<<groups, 256, 0, st>>>(a); };
+  if (!t->w) past ? go(upd::rows_kernel<float, false, true>) : go(upd::rows_kernel<float, false, false>);
+  else if (t->w_dtype == LONGER_BF16) past ? go(upd::rows_kernel<__bf16, true, true>) : go(upd::rows_kernel<__bf16, true, false>);
+  else past ? go(upd::rows_kernel<float, true, true>) : go(upd::rows_kernel<float, true, false>);
   return launched("AdamW update of rows");
 }
 
