@@ -51,12 +51,12 @@ template <typename T, int V> using Piece = typename Piece_<T, V>::type;
 // taken value by value.  Accesses are aligned to the element only, which the memory path takes at any address.
 enum Kind { WHOLE, BACK, VALUES };                   // rows of whole pieces; the last piece is moved back; the last piece is taken value by value
 struct Part { int c, n, twice; };                    // n: values of the row from c on, 8 or more: a whole piece
-template <Kind KIND>
+template <Kind KIND, int V = 8>
 __device__ __forceinline__ Part part_of(uint32_t piece, int d) {
-  const int c = piece * 8;
-  if (KIND == WHOLE) return {c, 8, 0};
+  const int c = piece * V;
+  if (KIND == WHOLE) return {c, V, 0};
   if (KIND == VALUES) return {c, d - c, 0};
-  return {min(c, d - 8), 8, max(c - (d - 8), 0)};
+  return {min(c, d - V), V, max(c - (d - V), 0)};
 }
 template <typename Go>
 inline void with_kind(Kind kind, Go go) {
@@ -64,25 +64,25 @@ inline void with_kind(Kind kind, Go go) {
   else if (kind == BACK) go(std::integral_constant<Kind, BACK>());
   else go(std::integral_constant<Kind, VALUES>());
 }
-inline Kind kind_of(int d, bool in_place = false) { return d % 8 == 0 ? WHOLE : d > 8 && !in_place ? BACK : VALUES; }
+inline Kind kind_of(int d, int V = 8, bool in_place = false) { return d % V == 0 ? WHOLE : d > V && !in_place ? BACK : VALUES; }
 
-template <typename T, Kind KIND>
-__device__ __forceinline__ Piece<T, 8> load8(const T* p, int n) {
-  if (KIND != VALUES || n >= 8) return *(const Piece<T, 8>*)p;
-  Piece<T, 8> x;
+template <typename T, Kind KIND, int V = 8>
+__device__ __forceinline__ Piece<T, V> load_piece(const T* p, int n) {
+  if (KIND != VALUES || n >= V) return *(const Piece<T, V>*)p;
+  Piece<T, V> x;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = j < n ? p[j] : (T)0.f;
+  for (int j = 0; j < V; ++j) x[j] = j < n ? p[j] : (T)0.f;
   return x;
 }
 // written once and read by another kernel: past the caches
-template <typename T, Kind KIND>
-__device__ __forceinline__ void store8(T* p, int n, const Piece<T, 8>& x) {
-  if (KIND != VALUES || n >= 8) {
-    __builtin_nontemporal_store(x, (Piece<T, 8>*)p);
+template <typename T, Kind KIND, int V = 8>
+__device__ __forceinline__ void store_piece(T* p, int n, const Piece<T, V>& x) {
+  if (KIND != VALUES || n >= V) {
+    __builtin_nontemporal_store(x, (Piece<T, V>*)p);
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 7; ++j)
+  for (int j = 0; j < V - 1; ++j)
     if (j < n) p[j] = x[j];
 }
 
@@ -118,25 +118,30 @@ __device__ __forceinline__ void words(const Mask& m, const Key& key, uint32_t ro
   }
 }
 
-// x[j] where value c + j of the row is kept, zero (whatever x[j] is) where it is not; a piece off the multiples of 8 lies in two blocks
-template <Kind KIND, typename V>
-__device__ __forceinline__ void drop8(const Mask& m, const Key& key, uint32_t row, int c, V& x) {
+// x[j] where value c + j of the row is kept, zero (whatever x[j] is) where it is not, for V values from c on: of the words of c's block the half-words
+// from c mod 8 on, and of the next block's what they lack (a piece that was moved back).
+template <Kind KIND, int V, typename X>
+__device__ __forceinline__ void drop_piece(const Mask& m, const Key& key, uint32_t row, int c, X& x) {
   uint32_t w[4];
   words(m, key, row, (uint32_t)c / 8, w);
-  if (KIND == BACK && (c & 7)) {
-    uint32_t v[4];
-    words(m, key, row, (uint32_t)c / 8 + 1, v);
-    for (int i = c & 7; i; --i) {                    // (at most 7 half-words on)
+  if (V == 4 && (c & 4)) {
+    w[0] = w[2];
+    w[1] = w[3];
+  }
+  if (KIND == BACK && c % V) {
+    uint32_t v[4] = {w[2], w[3], 0, 0};              // what follows the first V half-words
+    if (V == 8 || (c & 4)) words(m, key, row, (uint32_t)c / 8 + 1, v);
+    for (int i = c % V; i; --i) {
 #pragma unroll
-      for (int k = 0; k < 3; ++k) w[k] = __builtin_amdgcn_alignbit(w[k + 1], w[k], 16);
-      w[3] = __builtin_amdgcn_alignbit(v[0], w[3], 16);
+      for (int k = 0; k < V / 2 - 1; ++k) w[k] = __builtin_amdgcn_alignbit(w[k + 1], w[k], 16);
+      w[V / 2 - 1] = __builtin_amdgcn_alignbit(v[0], w[V / 2 - 1], 16);
 #pragma unroll
       for (int k = 0; k < 3; ++k) v[k] = __builtin_amdgcn_alignbit(v[k + 1], v[k], 16);
       v[3] >>= 16;
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = (w[j / 2] >> 16 * (j & 1) & 0xffff) >= m.drop ? x[j] : 0.f;
+  for (int j = 0; j < V; ++j) x[j] = (w[j / 2] >> 16 * (j & 1) & 0xffff) >= m.drop ? x[j] : 0.f;
 }
 
 // ------------------------------------------------------------------------------------ host

@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t i = min(at + u, end - 1);
-        to.x[u] = load8<T, KIND>((const T*)p.de.data + from[i] + c, width);
+        to.x[u] = load_piece<T, KIND>((const T*)p.de.data + from[i] + c, width);
         to.run[u] = runs[i];
         if (DROP) to.token[u] = tokens[i];
       }
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
         Piece<float, 8> y;
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = (float)in.x[u][j];
-        if (DROP) drop8<KIND>(p.mask, key, in.token[u], c, y);
+        if (DROP) drop_piece<KIND, 8>(p.mask, key, in.token[u], c, y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += y[j];
       }
@@ -299,7 +299,7 @@ __device__ __forceinline__ bool add_leads(const GradParams& p, float (&acc)[8], 
   for (uint32_t u = 0; u < U; ++u) {
     const uint32_t i = min(h + u * by, p.blocks - 1);
     lead[u] = h + u * by < p.blocks ? p.borders[i].lead : kNone;
-    x[u] = load8<float, KIND>(p.part + (size_t)i * 2 * p.d + c, width);
+    x[u] = load_piece<float, KIND>(p.part + (size_t)i * 2 * p.d + c, width);
   }
   bool more = true;
 #pragma unroll
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
   __syncthreads();
   if (g < p.blocks) {
     const Border own = p.borders[g];
-    const Piece<float, 8> x = load8<float, KIND>(p.part + g * step + p.d + c, width);
+    const Piece<float, 8> x = load_piece<float, KIND>(p.part + g * step + p.d + c, width);
     float acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = x[j];
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
     float acc[8] = {};
     for (uint32_t h = a + 1 + group; add_leads<KIND, 8>(p, acc, h, groups, own.tail, c, width); h += 8 * groups) {}
     if (group == 0) {
-      const Piece<float, 8> x = load8<float, KIND>(p.part + a * step + p.d + c, width);
+      const Piece<float, 8> x = load_piece<float, KIND>(p.part + a * step + p.d + c, width);
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += x[j];
     }
