@@ -400,7 +400,7 @@ int longer_adamw_step(const longer_adamw_tensor* tensors, int count, const longe
  * A dropout mask is never stored: it follows from a key, a site and a value's place.  key: device, [0] a seed, [1] the number
  * of the step, both of 64 bits and read on the GPU, so that a captured step draws a new mask wherever the caller has counted the
  * step number on.  Value c of row r = b L + l of a [B, L, d] call is kept where h >= t, t = round(65536 p), and then counts 65536 /
- * (65536 - t) times (p is taken to the next multiple of 2^-16); h is half-word c mod 8 (0: the low half of word 0) of the four words that
+ * (65536 - t) times (p is taken to the nearest multiple of 2^-16, halves up); h is half-word c mod 8 (0: the low half of word 0) of the four words that
  * Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, 2011) makes of the counter
  * (c div 8 + 65536 site, r, low word of the step, high word of the step) under the key (low word of the seed, high word).  site tells apart the places
  * of one step where a mask is drawn.  0 <= p, t <= 65535; 0 <= site <= 65535.  A dropped value is an exact zero, also of an infinity or NaN. */
@@ -447,7 +447,7 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
  *   dense == 1: grads_out [out_rows][d] holds every row of the table, zeros where no token names it (ids from out_rows on are dropped).
  * norms_out [out_rows] fp32, or NULL: the norm of each row of grads_out, zeros behind the last one: in a list of longer_grad_norm it
  * stands for the table's gradient, of which nothing is read again.
- * Sums in fp32 in a fixed order: the same call gives the same bits.  A norm is within 8 half steps of fp32 of its row's, whatever its size.
+ * Sums in fp32 in a fixed order: the same call gives the same bits.  A norm is its row's, from squares in 64 bits, rounded once.
  * ws: device, 256-byte aligned, at least longer_embedding_backward_workspace_bytes(B, L, d) bytes (0 = unsupported). */
 size_t longer_embedding_backward_workspace_bytes(int B, int L, int d);
 int longer_embedding_backward(const longer_order* order, const longer_rows* de, int B, int L, int d, float scale,

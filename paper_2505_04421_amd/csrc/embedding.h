@@ -89,7 +89,7 @@ __device__ __forceinline__ void store_piece(T* p, int n, const Piece<T, V>& x) {
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, 2011): ten rounds of two 32 x 32 -> 64 bit
 // products on a counter of four words under a key of two.  Half a word decides about one value: 8 values, 16 bytes of bf16, to a
 // call, and a share that is a multiple of 2^-16.  A wave's call takes 187 cycles of its SIMD with the words joined in one instruction
-// (275 with two exclusive ors): 65 million values in 10 us of the whole chip, of a lookup's 33 in bf16.
+// (275 with two exclusive ors): 65 million values in 10 us of the whole chip, of a lookup's 29 in bf16.
 struct Mask { const uint64_t* key; uint32_t site, drop; };      // site: in place; drop: half-words below it drop their value (0: there is no mask)
 struct Key { uint32_t k0, k1, c2, c3; };
 

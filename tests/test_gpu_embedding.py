@@ -3,9 +3,8 @@ of one value to 16384, one token to hundreds of thousands, any strides, both id 
 
 Tolerances.  u = 2^-24, half a step of fp32; half a step of bf16 is 2^-8 of the value.  A looked-up value is a product with the factor,
 itself rounded: 2 u, and the output's rounding.  Dropout adds one sum.  A gradient is a sum of n terms in fp32, in any order at most n u of
-the terms' magnitudes, and the factor's two roundings.  A norm is off by the norm of what its row is off, by 7 u for the sum of its squares
-(a fused step for each of a lane's 8, 6 joins of lanes: 14 u of the sum, half of that of the root; chunks of 512 columns join in 64 bits) and by its own
-rounding: 8 u."""
+the terms' magnitudes, and the factor's two roundings.  A norm is off by the norm of what its row is off, and by its own
+rounding: u (1.01 u with the squares' sum and root in 64 bits)."""
 import numpy as np
 import pytest
 import torch
@@ -252,7 +251,7 @@ def test_gradient(shape, dtype, skew):
         distinct, g, mag, count = gradient(ids, lens, R, np64(de), scale, f(np.arange(B * L), d) if p else None)
         tol = mag * (count[:, None] + 3) * U + TINY
         norm = np.sqrt((g * g).sum(1))
-        norm_tol = np.sqrt((tol * tol).sum(1)) + 8 * U * norm
+        norm_tol = np.sqrt((tol * tol).sum(1)) + 1.01 * U * norm
         for dense in (False, True):
             grads, norms, ws = backward(o, de, scale, drop, dense, R)
             got, gn = np64(grads), np64(norms)
@@ -314,7 +313,7 @@ def test_gradient_that_is_not_finite_and_one_beyond_the_norms_square():
     grads, norms, _ = backward(o, de, 1.0, None, False, 4)
     assert torch.isnan(grads[0]).sum() == 1 and bool(torch.isnan(norms[0]))
     assert float(grads[1, 4]) == float("inf") and float(norms[1]) == float("inf")
-    assert abs(float(norms[3]) / (1e30 * np.sqrt(40)) - 1) <= 8 * U and abs(float(norms[2]) / np.sqrt(40) - 1) <= 8 * U
+    assert abs(float(norms[3]) / (1e30 * np.sqrt(40)) - 1) <= 1.01 * U and abs(float(norms[2]) / np.sqrt(40) - 1) <= 1.01 * U
 
 
 def test_gradient_against_differences():
