@@ -111,17 +111,17 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t* lds, uint32
 }
 
 // ------------------------------------------------------------------------------------ few tokens: one workgroup
-constexpr int kFewThreads = 1024, kFewItems = 8, kFew = kFewThreads * kFewItems, kFewWaves = kFewThreads / 64;
+constexpr int kFewThreads = 1024, kFewItems = 4, kFew = kFewThreads * kFewItems, kFewWaves = kFewThreads / 64;
 
-// A wave takes 64 * items neighbours; rounds of up to kMostBits bits, all in LDS.  (6144 tokens of 1000 rows: 11.4 us, 256
-// tokens 5.6: bound by the one compute unit that they are on)
+// A wave takes 64 * items neighbours; rounds of up to kMostBits bits, all in LDS.  Bound by the one compute unit that they are on: 256 / 4096 tokens of 1000
+// rows in 6.7 / 9.2 us (the launches for many tokens: 9.3 / 9.7), of 1000003 rows 8.4 / 13.8 (15.3 / 17.5); 6144 tokens 11.5 / 18.0 (9.7 / 17.7).
 __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int per_round, longer_order out) {
   __shared__ alignas(16) uint32_t keys[kFew], words[kFewWaves << (kMostBits - 1)], base[1 << kMostBits];
   __shared__ uint32_t lds[kFewWaves];
   __shared__ uint16_t tokens[kFew];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int items = (a.n + kFewThreads - 1) / kFewThreads;
-  uint32_t n = a.n, key[kFewItems], token[kFewItems];        // (a token and, above it, its place: both below 2^13)
+  uint32_t n = a.n, key[kFewItems], token[kFewItems];
 #pragma unroll
   for (int i = 0; i < kFewItems; ++i) {
     const uint32_t k = (wave * items + i) * 64 + lane;
@@ -141,21 +141,14 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
     }
     for (uint32_t i = threadIdx.x; i < kFewWaves * digits / 2; i += kFewThreads) words[i] = 0;
     __syncthreads();
+    uint32_t digit[kFewItems], at[kFewItems];
+    bool there[kFewItems];
 #pragma unroll
-    for (int h = 0; h < kFewItems; h += 4) {
-      if (h >= items) break;
-      uint32_t digit[4], at[4];
-      bool there[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        there[i] = key[h + i] != kNone;
-        digit[i] = key[h + i] >> shift & (digits - 1);
-      }
-      rank<4>(digit, there, items - h, round, words + wave * (digits / 2), at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (h + i < items) token[h + i] |= at[i] << 16;
+    for (int i = 0; i < kFewItems; ++i) {
+      there[i] = key[i] != kNone;
+      digit[i] = key[i] >> shift & (digits - 1);
     }
+    rank<kFewItems>(digit, there, items, round, words + wave * (digits / 2), at);
     __syncthreads();
     // where each digit begins, and in it each wave
     const uint32_t four = threadIdx.x;
@@ -166,7 +159,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 #pragma unroll
     for (int i = 0; i < kFewItems; ++i)
       if (i < items && key[i] != kNone) {
-        const uint32_t digit = key[i] >> shift & (digits - 1), to = base[digit] + ((const uint16_t*)words)[wave * digits + digit] + (token[i] >> 16);
+        const uint32_t to = base[digit[i]] + ((const uint16_t*)words)[wave * digits + digit[i]] + at[i];
         keys[to] = key[i];
         tokens[to] = (uint16_t)token[i];
       }
@@ -219,7 +212,10 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 // number of digits before it whose count is not zero.  Two rounds: the first one's move leaves a byte at each id that it meets, the second
 // one's count makes of them, for every 32 ids, a mask and how many ids there are before it in its 2048, and the second move looks its ids up.
 // Larger tables take three rounds and two launches that number the runs of the sorted ids.
-constexpr int kThreads = 512, kItems = 4, kTile = kThreads * kItems, kWaves = kThreads / 64, kMostGroups = 512;
+//
+// A thread has 4 items of a tile; 2 where that leaves no compute unit a second workgroup, 1 in the smallest (4 / 2 / 1, 1000003 rows: 512000 tokens 40 / 43 / - us,
+// 256000 35.6 / 31.5 / 36.6, 64000 28.6 / 26.5 / 25.7, 16384 25.3 / 20.1 / 19.8, 6144 - / 19.7 / 17.7).
+constexpr int kThreads = 512, kItems = 4, kWaves = kThreads / 64, kMostGroups = 512;
 constexpr int kSumAlone = 64;                        // groups whose counts each workgroup adds up itself, for want of anything to do
 constexpr int kMaskRows = 32, kSegment = 2048;       // ids of a mask, and of a segment: a wave's
 
@@ -247,7 +243,9 @@ __device__ __forceinline__ uint32_t group_number(uint32_t groups) {
 
 // a workgroup's stretch of n items: whole tiles, as even as they can be dealt (behind the last group: none)
 struct Stretch { uint32_t begin, end; };
+template <int ITEMS>
 __device__ __forceinline__ Stretch stretch(uint32_t n, uint32_t group, uint32_t groups) {
+  constexpr uint32_t kTile = kThreads * ITEMS;
   const uint32_t tiles = (n + kTile - 1) / kTile, per = (tiles + groups - 1) / groups;
   const uint32_t begin = min((uint64_t)group * per * kTile, (uint64_t)n);
   return {begin, (uint32_t)min((uint64_t)begin + (uint64_t)per * kTile, (uint64_t)n)};
@@ -256,23 +254,23 @@ __device__ __forceinline__ Stretch stretch(uint32_t n, uint32_t group, uint32_t 
 // four bytes that are 0 or 1 as four bits
 __device__ __forceinline__ uint32_t four_bits(uint32_t bytes) { return bytes * 0x01020408u >> 24 & 15; }
 
-template <bool FIRST>
+template <bool FIRST, int ITEMS>
 __global__ __launch_bounds__(kThreads) void count_kernel(Round r) {
   __shared__ uint32_t count[1 << kMostBits];
   const uint32_t digits = 1u << r.bits;
   for (uint32_t i = threadIdx.x; i < digits; i += kThreads) count[i] = 0;
   __syncthreads();
   const uint32_t group = group_number(r.groups);
-  const Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group, r.groups);
-  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
-    uint32_t key[kItems];
+  const Stretch s = stretch<ITEMS>(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group, r.groups);
+  for (uint32_t tile = s.begin; tile < s.end; tile += kThreads * ITEMS) {
+    uint32_t key[ITEMS];
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
       const uint32_t i = tile + k * kThreads + threadIdx.x;
       key[k] = i >= s.end ? kNone : FIRST ? id_of(r.ids, i) : (uint32_t)r.in[i];
     }
 #pragma unroll
-    for (int k = 0; k < kItems; ++k)
+    for (int k = 0; k < ITEMS; ++k)
       if (key[k] != kNone) atomicAdd(&count[key[k] >> r.shift & (digits - 1)], 1u);
   }
   if (r.seen) {
@@ -323,19 +321,19 @@ __global__ __launch_bounds__(1024) void sum_kernel(uint32_t* counts, uint32_t* t
 }
 
 // LAST: 0 items go on to another round, 1 to the order with their runs, 2 to the order and the sorted ids
-template <bool FIRST, int LAST>
+template <bool FIRST, int LAST, int ITEMS>
 __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
   static_assert((1 << kMostBits) <= 4 * kThreads, "a thread has four digits");
   __shared__ alignas(16) uint32_t words[kWaves << (kMostBits - 1)], base[1 << kMostBits], runs[1 << kMostBits];
   __shared__ uint32_t lds[kWaves];
   const uint32_t digits = 1u << r.bits, group = group_number(r.groups), four = 4 * threadIdx.x;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  uint32_t key[kItems], token[kItems], digit[kItems], at[kItems];
-  bool there[kItems];
+  uint32_t key[ITEMS], token[ITEMS], digit[ITEMS], at[ITEMS];
+  bool there[ITEMS];
   auto load = [&](uint32_t tile, uint32_t end) {
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const uint32_t k = tile + (wave * kItems + i) * 64 + lane;
+    for (int i = 0; i < ITEMS; ++i) {
+      const uint32_t k = tile + (wave * ITEMS + i) * 64 + lane;
       key[i] = kNone;
       if (k < end) {
         const uint64_t v = FIRST ? 0 : r.in[k];
@@ -344,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
       }
     }
   };
-  Stretch s = stretch(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group, r.groups);
+  Stretch s = stretch<ITEMS>(FIRST ? r.ids.n : (uint32_t)r.order.counts[1], group, r.groups);
   load(s.begin, s.end);                              // (under way while the digits' places are found)
   // where each digit begins, and in it this workgroup
   uint32_t n, named = 0;
@@ -402,22 +400,22 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
     if (FIRST) r.order.counts[1] = (int)n;
     if (LAST == 1) r.order.counts[0] = (int)named;
   }
-  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
+  for (uint32_t tile = s.begin; tile < s.end; tile += kThreads * ITEMS) {
     if (tile != s.begin) load(tile, s.end);
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
       there[i] = key[i] != kNone;
       digit[i] = key[i] >> r.shift & (digits - 1);
     }
     for (uint32_t i = threadIdx.x; i < kWaves * digits / 2; i += kThreads) words[i] = 0;
     __syncthreads();
-    rank<kItems>(digit, there, kItems, r.bits, words + wave * (digits / 2), at);
+    rank<ITEMS>(digit, there, ITEMS, r.bits, words + wave * (digits / 2), at);
     __syncthreads();
     // where each wave begins in a digit
     const u32x4 sums = four < digits ? waves_before<kWaves>(words, digits, four / 4) : u32x4{};
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
+    for (int i = 0; i < ITEMS; ++i)
       if (there[i]) {
         const uint32_t to = base[digit[i]] + ((const uint16_t*)words)[wave * digits + digit[i]] + at[i];
         if (LAST == 0) {
@@ -443,7 +441,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Round r) {
 // how many runs begin in each workgroup's stretch of the sorted ids
 __global__ __launch_bounds__(kThreads) void heads_kernel(const uint32_t* keys, const int32_t* n, uint32_t* heads) {
   __shared__ uint32_t lds[kWaves];
-  const Stretch s = stretch((uint32_t)*n, blockIdx.x, gridDim.x);
+  const Stretch s = stretch<kItems>((uint32_t)*n, blockIdx.x, gridDim.x);
   uint32_t mine = 0, all;
   for (uint32_t k = s.begin + threadIdx.x; k < s.end; k += kThreads) mine += k == 0 || keys[k] != keys[k - 1];
   group_scan<kThreads>(mine, lds, &all);
@@ -455,8 +453,8 @@ __global__ __launch_bounds__(kThreads) void runs_kernel(const uint32_t* keys, co
   __shared__ uint32_t lds[kWaves];
   uint32_t run, all;
   group_scan<kThreads>(threadIdx.x < blockIdx.x ? heads[threadIdx.x] : 0, lds, &run);
-  const Stretch s = stretch((uint32_t)out.counts[1], blockIdx.x, gridDim.x);
-  for (uint32_t tile = s.begin; tile < s.end; tile += kTile) {
+  const Stretch s = stretch<kItems>((uint32_t)out.counts[1], blockIdx.x, gridDim.x);
+  for (uint32_t tile = s.begin; tile < s.end; tile += kThreads * kItems) {
     const uint32_t first = tile + threadIdx.x * kItems;
     uint32_t key[kItems], before = first && first < s.end ? keys[first - 1] : kNone, mine = 0;
     bool head[kItems];
@@ -487,7 +485,7 @@ static int bits_of(int64_t rows) {
 }
 
 struct Plan {
-  int bits, rounds, per_round, groups;
+  int bits, rounds, per_round, items_each, groups;
   size_t items, keys, counts, totals, seen, masks, segments, heads, bytes;      // places in the workspace: items of two rounds, at its front
 };
 
@@ -501,7 +499,8 @@ static Plan plan(int B, int L, int64_t rows) {
     p.bytes = 256;
     return p;
   }
-  p.groups = (int)std::min<size_t>((n + kTile - 1) / kTile, kMostGroups);
+  p.items_each = n <= 16384 ? 1 : n <= 256 * 2 * kThreads ? 2 : kItems;
+  p.groups = (int)std::min<size_t>((n + kThreads * p.items_each - 1) / (kThreads * p.items_each), kMostGroups);
   size_t at = 0;
   auto place = [&](size_t bytes) {
     const size_t here = at;
@@ -558,25 +557,31 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
                   0, p.per_round, p.bits, (uint32_t)p.groups, p.groups > srt::kSumAlone};
   // (a wave for each segment of the ids that may have been seen: 9000 tokens of 1000003 rows 37 us with the items' 5 workgroups alone)
   const int grid = p.rounds == 2 ? std::max(p.groups, (1 << p.bits >> 11) / srt::kWaves) : p.groups;
-  for (int i = 0; i < p.rounds; ++i) {
-    r.in = i ? items[(i - 1) & 1] : nullptr;
-    r.out = items[i & 1];
-    r.shift = i * p.per_round;
-    r.bits = p.per_round;                            // (the last round's digits may pass the ids' bits)
-    const uint32_t digits = 1u << r.bits;
-    if (i == 0) srt::count_kernel<true><<<grid, srt::kThreads, 0, st>>>(r);
-    else srt::count_kernel<false><<<grid, srt::kThreads, 0, st>>>(r);
-    if (r.summed) {
-      auto sum = p.groups > 256 ? srt::sum_kernel<srt::kMostGroups / 32> : srt::sum_kernel<8>;
-      sum<<<(digits + 31) / 32, 1024, 0, st>>>(r.counts, r.totals, p.groups, digits);
+  auto sort = [&](auto items_each) {
+    constexpr int ITEMS = decltype(items_each)::value;
+    for (int i = 0; i < p.rounds; ++i) {
+      r.in = i ? items[(i - 1) & 1] : nullptr;
+      r.out = items[i & 1];
+      r.shift = i * p.per_round;
+      r.bits = p.per_round;                          // (the last round's digits may pass the ids' bits)
+      const uint32_t digits = 1u << r.bits;
+      if (i == 0) srt::count_kernel<true, ITEMS><<<grid, srt::kThreads, 0, st>>>(r);
+      else srt::count_kernel<false, ITEMS><<<grid, srt::kThreads, 0, st>>>(r);
+      if (r.summed) {
+        auto sum = p.groups > 256 ? srt::sum_kernel<srt::kMostGroups / 32> : srt::sum_kernel<8>;
+        sum<<<(digits + 31) / 32, 1024, 0, st>>>(r.counts, r.totals, p.groups, digits);
+      }
+      const int last = i + 1 < p.rounds ? 0 : p.rounds <= 2 ? 1 : 2;
+      if (i == 0 && last) srt::move_kernel<true, 1, ITEMS><<<p.groups, srt::kThreads, 0, st>>>(r);
+      else if (i == 0) srt::move_kernel<true, 0, ITEMS><<<p.groups, srt::kThreads, 0, st>>>(r);
+      else if (last == 0) srt::move_kernel<false, 0, ITEMS><<<p.groups, srt::kThreads, 0, st>>>(r);
+      else if (last == 1) srt::move_kernel<false, 1, ITEMS><<<grid, srt::kThreads, 0, st>>>(r);
+      else srt::move_kernel<false, 2, ITEMS><<<p.groups, srt::kThreads, 0, st>>>(r);
     }
-    const int last = i + 1 < p.rounds ? 0 : p.rounds <= 2 ? 1 : 2;
-    if (i == 0 && last) srt::move_kernel<true, 1><<<p.groups, srt::kThreads, 0, st>>>(r);
-    else if (i == 0) srt::move_kernel<true, 0><<<p.groups, srt::kThreads, 0, st>>>(r);
-    else if (last == 0) srt::move_kernel<false, 0><<<p.groups, srt::kThreads, 0, st>>>(r);
-    else if (last == 1) srt::move_kernel<false, 1><<<grid, srt::kThreads, 0, st>>>(r);
-    else srt::move_kernel<false, 2><<<p.groups, srt::kThreads, 0, st>>>(r);
-  }
+  };
+  if (p.items_each == 1) sort(std::integral_constant<int, 1>());
+  else if (p.items_each == 2) sort(std::integral_constant<int, 2>());
+  else sort(std::integral_constant<int, srt::kItems>());
   if (p.rounds > 2) {
     uint32_t* heads = (uint32_t*)(w + p.heads);
     srt::heads_kernel<<<p.groups, srt::kThreads, 0, st>>>(keys, order->counts + 1, heads);

@@ -192,7 +192,8 @@ def sort(ids, kind, fields, glens, rows):
 
 
 SORTS = [(1, 1, 1), (1, 1, 900), (1, 2, 2), (3, 21, 5), (1, 64, 1), (5, 13, 64), (1, 65, 300), (64, 96, 1000), (1, 8191, 257), (8, 1024, 65536), (1, 8193, 1), (1, 8193, 3),
-         (9, 911, 2048), (3, 4096, 2049), (6, 2049, 70000), (2, 10241, 1 << 22), (64, 2000, (1 << 22) + 1), (31, 3333, (1 << 31) - 1), (256, 2000, 1_000_003), (1, 1_100_001, 2_000_000)]
+         (9, 911, 2048), (3, 4096, 2049), (6, 2049, 70000), (2, 10241, 1 << 22), (64, 2000, (1 << 22) + 1), (31, 3333, (1 << 31) - 1), (256, 2000, 1_000_003), (1, 1_100_001, 2_000_000),
+         (1, 4096, 1000), (1, 4097, 1000), (17, 241, 1_000_003), (1, 16384, 2048), (5, 3277, 90000), (2, 8191, 5_000_000), (2, 131072, 300), (1, 262145, 3000), (4, 65536, 1 << 23)]
 
 
 @pytest.mark.parametrize("skew", ["even", "popular", "one"])
