@@ -118,26 +118,44 @@ __device__ __forceinline__ void words(const Mask& m, const Key& key, uint32_t ro
   }
 }
 
-// x[j] where value c + j of the row is kept, zero (whatever x[j] is) where it is not, for V values from c on: of the words of c's block the half-words
-// from c mod 8 on, and of the next block's what they lack (a piece that was moved back).
+// x[j] where the value is kept, zero (whatever x[j] is) where it is not, for the V values of a lane's piece.  A last piece that was moved back begins in the
+// words of the piece before it, which the lane before has (512000 rows of 100 in bf16 looked up: 34 us, 39 with a second call of the generator for them);
+// only where that lane is of another wave or turn they are drawn again.
 template <Kind KIND, int V, typename X>
-__device__ __forceinline__ void drop_piece(const Mask& m, const Key& key, uint32_t row, int c, X& x) {
+__device__ __forceinline__ void drop_piece(const Mask& m, const Key& key, uint32_t row, uint32_t piece, bool first, int d, X& x) {
+  constexpr int W = V / 2;
   uint32_t w[4];
-  words(m, key, row, (uint32_t)c / 8, w);
-  if (V == 4 && (c & 4)) {
-    w[0] = w[2];
-    w[1] = w[3];
-  }
-  if (KIND == BACK && c % V) {
-    uint32_t v[4] = {w[2], w[3], 0, 0};              // what follows the first V half-words
-    if (V == 8 || (c & 4)) words(m, key, row, (uint32_t)c / 8 + 1, v);
-    for (int i = c % V; i; --i) {
+  auto draw = [&](uint32_t i) {                      // the W words of piece i
+    words(m, key, row, i * V / 8, w);
+    if (V == 4 && (i & 1)) {
+      w[0] = w[2];
+      w[1] = w[3];
+    }
+  };
+  draw(piece);
+  if (KIND == BACK) {
+    const bool last = (int)(piece + 1) * V > d;
+    const uint32_t by = (uint32_t)d % V;             // half-words to pass over
+    uint32_t v[2 * W];
 #pragma unroll
-      for (int k = 0; k < V / 2 - 1; ++k) w[k] = __builtin_amdgcn_alignbit(w[k + 1], w[k], 16);
-      w[V / 2 - 1] = __builtin_amdgcn_alignbit(v[0], w[V / 2 - 1], 16);
+    for (int k = 0; k < W; ++k) {
+      v[W + k] = w[k];
+      v[k] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[k], 0x138, 0xF, 0xF, true);       // the lane before
+    }
+    if (last && (first || (threadIdx.x & 63) == 0)) {
+      draw(piece - 1);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) v[k] = __builtin_amdgcn_alignbit(v[k + 1], v[k], 16);
-      v[3] >>= 16;
+      for (int k = 0; k < W; ++k) v[k] = w[k];
+    }
+#pragma unroll
+    for (int step = W / 2; step; step /= 2)
+      if (by & 2 * step)
+#pragma unroll
+        for (int k = 0; k + step < 2 * W; ++k) v[k] = v[k + step];
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      if (by & 1) v[k] = __builtin_amdgcn_alignbit(v[k + 1], v[k], 16);
+      w[k] = last ? v[k] : w[k];
     }
   }
 #pragma unroll

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p) {
           Piece<float, V> y;
 #pragma unroll
           for (int j = 0; j < V; ++j) y[j] = (float)x[u][j] * p.factor;
-          if (DROP) drop_piece<KIND, V>(p.mask, key, first + r, at.c, y);
+          if (DROP) drop_piece<KIND, V>(p.mask, key, first + r, piece, me.lane == 0, p.d, y);
           Piece<O, V> o;
 #pragma unroll
           for (int j = 0; j < V; ++j) o[j] = w[u].from >= 0 ? (O)y[j] : (O)0.f;
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropParams p) {
           if (w[u].from >= 0) {
 #pragma unroll
             for (int j = 0; j < V; ++j) y[j] = (float)x[u][j] * p.factor;
-            drop_piece<KIND, V>(p.mask, key, first + r, at.c, y);
+            drop_piece<KIND, V>(p.mask, key, first + r, piece, me.lane == 0, p.d, y);
             if (ADD)
 #pragma unroll
               for (int j = 0; j < V; ++j) y[j] += (float)add[u][j];

@@ -52,12 +52,12 @@ __device__ __forceinline__ void store_sums(float* to, int n, const float (&a)[V]
       if (j < n) to[j] = v[j];
 }
 
-struct Lane { Part at; int lane, chunk; };           // a lane's columns (n <= 0: it has none)
+struct Lane { Part at; uint32_t piece; int lane, chunk; };           // a lane's columns (n <= 0: it has none)
 template <Kind KIND, int V>
 __device__ __forceinline__ Lane lane_of(const GradParams& p) {
   const int lane = threadIdx.x & ((1 << p.shift) - 1), chunk = blockIdx.y, c = (chunk * 64 + lane) * V;
-  if (c >= p.d) return {{0, 0, 0}, lane, chunk};
-  return {part_of<KIND, V>((uint32_t)c / V, p.d), lane, chunk};
+  if (c >= p.d) return {{0, 0, 0}, 0, lane, chunk};
+  return {part_of<KIND, V>((uint32_t)c / V, p.d), (uint32_t)c / V, lane, chunk};
 }
 
 template <int CTRL> __device__ __forceinline__ float from_lane(float v) {
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
         Piece<float, V> y;
 #pragma unroll
         for (int j = 0; j < V; ++j) y[j] = (float)in.x[u][j];
-        if (DROP) drop_piece<KIND, V>(p.mask, key, in.token[u], c, y);
+        if (DROP) drop_piece<KIND, V>(p.mask, key, in.token[u], me.piece, me.lane == 0, p.d, y);
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] += y[j];
       }
