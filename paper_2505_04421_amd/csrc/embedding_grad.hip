@@ -281,8 +281,6 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   }
 }
 
-constexpr int kJoinThreads = 512;
-
 // The sums of stretches h, h + by, ..., U of them under way at once, while they go on with the run; says whether the last one did.  (A
 // stretch that does not has left nothing to read: what is there is not used.)
 template <Kind KIND, int V, uint32_t U>
@@ -306,16 +304,17 @@ __device__ __forceinline__ bool add_leads(const GradParams& p, float (&acc)[V], 
 }
 
 // The runs that cross workgroups' stretches, each by the group of the stretch that it begins in, and by the whole workgroup where it
-// goes on for more than ALONE: group k takes every groups-th of its sums, which then meet in two steps.  Bound by its loads' latency (8 values a lane: 512000
-// tokens of 128 in 10.6 us with ALONE 4, 11.8 with 8; 230 thousand tokens of one item in 11.4 us with 8 sums of a group under way, 14.2 with 4).
-template <Kind KIND, int V>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(GradParams p) {
+// goes on for more than ALONE: group k takes every groups-th of its sums, which then meet in two steps.  Bound by its loads' latency (512000
+// tokens of 128, 8 values a lane: 10.6 us with ALONE 4, 11.8 with 8; 230 thousand tokens of one item: 11.4 us with 8 sums of a group under way, 14.2 with 4), and
+// where one item has most tokens by what one compute unit can read (2 MB in 26 us).
+template <Kind KIND, int V, int THREADS>
+__global__ __launch_bounds__(THREADS) void join_kernel(GradParams p) {
   constexpr uint32_t ALONE = 4;
-  __shared__ float lds[kJoinThreads * V];
-  __shared__ uint32_t list[kJoinThreads], listed;
+  __shared__ float lds[THREADS * V];
+  __shared__ uint32_t list[THREADS], listed;
   const Lane me = lane_of<KIND, V>(p);
   const int c = me.at.c, width = max(me.at.n, 0);
-  const uint32_t group = threadIdx.x >> p.shift, groups = kJoinThreads >> p.shift, g = blockIdx.x * groups + group;
+  const uint32_t group = threadIdx.x >> p.shift, groups = THREADS >> p.shift, g = blockIdx.x * groups + group;
   const size_t step = (size_t)2 * p.d;
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
@@ -423,14 +422,15 @@ static void grad(const GradParams& p, dim3 grid, hipStream_t st) {
   with_kind(kind_of(p.d, kValues), go);
 }
 
-// (V: values of a lane.  4 where a wave holds a row so, which is one chunk either way: 512000 tokens of 128 in 7.9 us for 10.5, of which one item has
-// most in 13.2 for 11.6)
-template <int V>
+// V: values of a lane.  4 where a wave holds a row so, which is one chunk either way (512000 tokens of 128, few / most of one item: 7.8 / 26.6 us, 10.6 / 27.2
+// with 8).  Groups: as many as 512 threads have, 128 threads' where these are at least 8, so that fewer of a batch's popular items meet in one workgroup, one
+// behind the other (512000 tokens of 32, popular / most of one item: 6.9 / 10.0 us, 13.4 / 5.5 with 512 threads; of 64: 5.9, 11.3).
+template <int V, int THREADS>
 static void join(GradParams p, hipStream_t st) {
   p.shift = lanes_shift(std::min((p.d + V - 1) / V, 64), 6);
-  const uint32_t groups = (uint32_t)kJoinThreads >> p.shift;
+  const uint32_t groups = (uint32_t)THREADS >> p.shift;
   const dim3 grid((p.blocks + groups - 1) / groups, p.chunks);
-  with_kind(kind_of(p.d, V), [&](auto kind) { join_kernel<decltype(kind)::value, V><<<grid, kJoinThreads, 0, st>>>(p); });
+  with_kind(kind_of(p.d, V), [&](auto kind) { join_kernel<decltype(kind)::value, V, THREADS><<<grid, THREADS, 0, st>>>(p); });
 }
 
 }  // namespace emb
@@ -472,7 +472,7 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   const dim3 grid(g.blocks + (dense ? (p.out_rows + p.zero_rows - 1) / p.zero_rows : 0), g.chunks);
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
   else emb::grad<__bf16>(p, grid, st);
-  if (g.blocks > 1) d <= 256 ? emb::join<4>(p, st) : emb::join<emb::kValues>(p, st);
+  if (g.blocks > 1) d <= 64 ? emb::join<4, 128>(p, st) : d <= 256 ? emb::join<4, 512>(p, st) : emb::join<emb::kValues, 512>(p, st);
   if (norms_out && g.chunks > 1) emb::norm_kernel<<<std::min((p.n + 255) / 256, 2048u), 256, 0, st>>>(p);
   return launched("embedding gradient");
 }
