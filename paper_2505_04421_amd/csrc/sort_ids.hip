@@ -114,7 +114,7 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t* lds, uint32
 constexpr int kFewThreads = 1024, kFewItems = 4, kFew = kFewThreads * kFewItems, kFewWaves = kFewThreads / 64;
 
 // A wave takes 64 * items neighbours; rounds of up to kMostBits bits, all in LDS.  Bound by the one compute unit that they are on: 256 / 4096 tokens of 1000
-// rows in 6.7 / 9.2 us (the launches for many tokens: 9.3 / 9.7), of 1000003 rows 8.4 / 13.8 (15.3 / 17.5); 6144 tokens 11.5 / 18.0 (9.7 / 17.7).
+// rows in 6.7 / 8.6 us (the launches for many tokens: 9.3 / 9.7), of 1000003 rows 7.4 / 12.9 (15.3 / 17.5); 6144 tokens 11.5 / 18.0 (9.7 / 17.7).
 __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int per_round, longer_order out) {
   __shared__ alignas(16) uint32_t keys[kFew], words[kFewWaves << (kMostBits - 1)], base[1 << kMostBits];
   __shared__ uint32_t lds[kFewWaves];
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Ids a, int bits, int p
 // A round of the sort takes one digit, in three launches: every workgroup counts the digits of its stretch of the items, the counts are summed
 // over the workgroups before it, and it moves its items.  The first round reads the ids themselves and drops the tokens that name no
 // row; between rounds an item is a word of eight bytes, id below and token above.  (The sums inside the move, each workgroup reading
-// all counts: 30 us a round for 24.)  512000 tokens of 1000003 rows take 38 us, of which each launch's own time is a third: count 4.5, sums 5, move 13
+// all counts: 30 us a round for 24.)  512000 tokens of 1000003 rows take 40 us, of which each launch's own time is a third: count 5, sums 5, move 12
 // and 10, bound by latency and the scattered stores; 14 MB have to move.
 //
 // The runs' numbers need no pass over the sorted ids where the table has at most 2^22 rows.  One round (up to 2^11 rows): a digit is an id, and its run the
@@ -231,7 +231,7 @@ struct Round {
   longer_order order;
   int shift, bits, id_bits;
   uint32_t groups;                                   // workgroups with items; those behind them help with the ids that were seen
-  int summed;                                     // summed: counts and totals are sums; else each workgroup adds up the counts itself
+  int summed;                                        // summed: counts and totals are sums; else each workgroup adds up the counts itself
 };
 
 // Workgroups go to the eight chiplets in turn, each with a second-level cache of its own.  Neighbouring stretches, whose items land side by side,
@@ -555,7 +555,7 @@ int longer_sort_ids(const longer_ids* ids, const int32_t* lens, int B, int L, in
   uint32_t* keys = (uint32_t*)(w + p.keys);
   srt::Round r = {a, nullptr, items[0], (uint32_t*)(w + p.counts), (uint32_t*)(w + p.totals), p.rounds == 2 ? (uint8_t*)(w + p.seen) : nullptr, (uint64_t*)(w + p.masks), (uint32_t*)(w + p.segments), keys, *order,
                   0, p.per_round, p.bits, (uint32_t)p.groups, p.groups > srt::kSumAlone};
-  // (a wave for each segment of the ids that may have been seen: 9000 tokens of 1000003 rows 37 us with the items' 5 workgroups alone)
+  // (a wave for each segment of the ids that may have been seen: 9000 tokens of 1000003 rows 37 us with the items' workgroups alone)
   const int grid = p.rounds == 2 ? std::max(p.groups, (1 << p.bits >> 11) / srt::kWaves) : p.groups;
   auto sort = [&](auto items_each) {
     constexpr int ITEMS = decltype(items_each)::value;
