@@ -82,27 +82,34 @@ __device__ __forceinline__ V group_sum(V v, int shift) {
   return v;
 }
 
-// A run's sums are complete: its row, and its norm's squares, which are added up in 64 bits so that a row of any size has its norm, rounded once
-// (in fp32 where that is safe: 74 us for 512000 tokens of 128 either way).  All lanes of the group are here.
+// A run's sums are complete: its row goes out, and the squares of its values, which are added up in 64 bits so that a row of any size has its norm, rounded
+// once, are returned.  All lanes of the group are here.
 template <Kind KIND, int V>
-__device__ __forceinline__ void finish(const GradParams& p, uint32_t run, uint32_t row, const Lane& me, const float (&acc)[V]) {
-  if (row >= p.out_rows) return;
+__device__ __forceinline__ double put_row(const GradParams& p, uint32_t row, const Lane& me, const float (&acc)[V]) {
   float g[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) g[j] = p.factor * acc[j];
-  if (me.at.n > 0) store_sums<KIND, V>(p.grads + (size_t)row * p.d + me.at.c, me.at.n, g);
-  if (!p.norms) return;
+  if (row < p.out_rows && me.at.n > 0) store_sums<KIND, V>(p.grads + (size_t)row * p.d + me.at.c, me.at.n, g);
   double squares = 0.;
+  if (!p.norms) return squares;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const double x = KIND == WHOLE ? (me.at.n ? g[j] : 0.f) : j >= me.at.twice && j < me.at.n ? g[j] : 0.f;
     squares = fma(x, x, squares);
   }
-  squares = group_sum(squares, p.shift);
-  if (me.lane == 0) {
-    if (p.chunks > 1) p.squares[(size_t)run * p.chunks + me.chunk] = squares;
-    else p.norms[row] = (float)sqrt(squares);
-  }
+  return group_sum(squares, p.shift);
+}
+
+__device__ __forceinline__ void put_norm(const GradParams& p, uint32_t run, uint32_t row, int chunk, double squares) {
+  if (row >= p.out_rows) return;
+  if (p.chunks > 1) p.squares[(size_t)run * p.chunks + chunk] = squares;
+  else p.norms[row] = (float)sqrt(squares);
+}
+
+template <Kind KIND, int V>
+__device__ __forceinline__ void finish(const GradParams& p, uint32_t run, uint32_t row, const Lane& me, const float (&acc)[V]) {
+  const double squares = put_row<KIND, V>(p, row, me, acc);
+  if (p.norms && me.lane == 0) put_norm(p, run, row, me.chunk, squares);
 }
 
 // The first of `count` ascending numbers that is not below `from`: 64 places at a time.
@@ -211,6 +218,11 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
         if (DROP) to.token[u] = tokens[i];
       }
     };
+    // a run that began here is complete with token i, whose place in dE nobody asks for any more: its norm's squares wait there
+    auto done = [&](uint32_t i) {
+      const double squares = put_row<KIND, V>(p, rows[i], me, acc);
+      if (p.norms && me.lane == 0) from[i] = __builtin_bit_cast(int64_t, squares);
+    };
     auto take = [&](const Batch& in, uint32_t at) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -220,7 +232,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
 #pragma unroll
             for (int j = 0; j < V; ++j) lead[threadIdx.x * V + j] = acc[j];
           } else {
-            finish<KIND, V>(p, run, rows[at + u - 1], me, acc);
+            done(at + u - 1);
           }
           run = in.run[u];
           earlier = false;
@@ -251,10 +263,15 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
       for (int j = 0; j < V; ++j) lead[threadIdx.x * V + j] = acc[j];
       if (me.lane == 0) flags[group] = kLead | (on ? kOn : 0);
     } else if (!on) {
-      finish<KIND, V>(p, run, rows[end - 1], me, acc);
+      done(end - 1);
     }
   }
   __syncthreads();
+  // the norms of the runs that began and ended in one range, a thread each (by a group at each run's end: 512000 tokens of 129 in 102 us for 89, of 128 75 for 74,
+  // of 33 38 for 34)
+  if (p.norms)
+    for (uint32_t i = threadIdx.x; i < count; i += kThreads)
+      if (runs[i] != runs[i + 1] && runs[i] != runs[(int)(i & ~(p.range - 1)) - 1]) put_norm(p, runs[i], rows[i], me.chunk, __builtin_bit_cast(double, from[i]));
   // a run that goes on: the group where it begins (or the workgroup's first, where it began before) adds up the sums of those behind
   const bool owner = begin < end && on && !earlier, before = group == 0 && flags[0] & kLead;
   if (!owner && !before) return;
