@@ -301,7 +301,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
     const size_t at = (size_t)row * a.d;
     const float* gs = a.g + (size_t)i * a.d;
     W* ws = (W*)a.w;
-    for (int k = me.lane * 4; k < a.d; k += a.deal.lanes * 4) {
+    for (int k = (blockIdx.y * a.deal.lanes + me.lane) * 4; k < a.d; k += gridDim.y * a.deal.lanes * 4) {
       if (k + 4 <= a.d) {
         const Four<float> g = *(const Four<float>*)(gs + k);
         Four<float> m = load_four<PAST>(a.m + at + k), v = load_four<PAST>(a.v + at + k), p = load_four<PAST>(a.p + at + k);
@@ -580,11 +580,13 @@ int longer_adamw_rows(const longer_adamw_table* t, const longer_order* order, in
   const upd::RowsArgs a = {t->p, t->m, t->v, t->w, g, order->rows, order->counts, norm, most, (uint32_t)t->rows, t->d, emb::deal((t->d + 3) / 4),
                            (float)(how->lr * t->decay), h};
   const unsigned groups = std::min((most + a.deal.per_turn - 1) / a.deal.per_turn, 16384u);
+  // Few rows of several turns: a workgroup for each turn (300 rows of 8192 in 9.2 us for 12.3, 4606 of 3486 in 38 for 41; 16000 of 4096 in 263 for 255).
+  const unsigned parts = most <= 8192 ? (t->d + 1023) / 1024 : 1;
   hipStream_t st = (hipStream_t)stream;
   // Whole lines of 128 bytes go past the caches; rows of other widths through them, where the lines that two rows share may meet (140 thousand rows of
   // 33 / 40 / 100 / 129 values, 16000 of 4099: 97 / 64 / 127 / 170 / 311 us past, 53 / 42 / 135 / 166 / 296 through).
   const bool past = t->d % 32 == 0 && !(((uintptr_t)t->p | (uintptr_t)t->m | (uintptr_t)t->v) & 127);
-  auto go = [&](auto kernel) { kernel<<<groups, 256, 0, st>>>(a); };
+  auto go = [&](auto kernel) { kernel<<<dim3(groups, parts), 256, 0, st>>>(a); };
   if (!t->w) past ? go(upd::rows_kernel<float, false, true>) : go(upd::rows_kernel<float, false, false>);
   else if (t->w_dtype == LONGER_BF16) past ? go(upd::rows_kernel<__bf16, true, true>) : go(upd::rows_kernel<__bf16, true, false>);
   else past ? go(upd::rows_kernel<float, true, true>) : go(upd::rows_kernel<float, true, false>);

@@ -339,7 +339,7 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.parametrize("weights", ["none", "f32", "bf16"])
-@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (3, 5, 7, 11), (64, 96, 32, 1000), (2, 700, 130, 90), (1, 40, 2049, 70), (20, 1000, 64, 30000), (1, 3, 16384, 4)])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (3, 5, 7, 11), (64, 96, 32, 1000), (2, 700, 130, 90), (1, 40, 2049, 70), (20, 1000, 64, 30000), (1, 3, 16384, 4), (3, 3000, 1030, 8500), (2, 150, 3001, 500)])
 def test_rows_update(shape, weights):
     """The rows that a batch names: the bits of longer_adamw_step on the dense gradient; the others as they were."""
     B, L, d, R = shape
