@@ -20,7 +20,7 @@ struct alignas(16) Border { uint32_t lead, tail, row, unused; };
 
 struct GradParams {
   Rows de;
-  Divider by_L;
+  Divider by_L, by_d;
   uint32_t n, L;                                     // tokens of the batch
   int d, shift, chunks;
   uint32_t range, block;                             // tokens of a group and of a workgroup
@@ -140,19 +140,21 @@ __device__ __forceinline__ void zero_rows(const GradParams& p, uint32_t part, ui
     if (row >= a) named[row - a] = 1;
   }
   __syncthreads();
-  int shift = 0;                                     // lanes of a row, four values each
-  while (shift < kThreadBits && 4 << shift < p.d) ++shift;
-  const int lane = threadIdx.x & ((1 << shift) - 1);
-  for (uint32_t row = a + (threadIdx.x >> shift); row < b; row += kThreads >> shift) {
-    if (named[row - a]) continue;
-    float* to = p.grads + (size_t)row * p.d;
-    for (int c = 4 * lane; c < p.d; c += 4 << shift) {
-      if (c + 4 <= p.d) __builtin_nontemporal_store(Piece<float, 4>(0.f), (Piece<float, 4>*)(to + c));
-      else
-        for (int k = c; k < p.d; ++k) to[k] = 0.f;
-    }
-    if (p.norms && lane == 0) p.norms[row] = 0.f;
+  // the share's values in pieces of four, whatever row they are of (row by row: 1000438 rows of 33 in 56 us for 30, 145146 of 282 in 44 for 30)
+  const uint32_t values = (b - a) * p.d;
+  float* to = p.grads + (size_t)a * p.d;
+  for (uint32_t i = 4 * threadIdx.x; i < values; i += 4 * kThreads) {
+    const uint32_t first_row = p.by_d(i), last_row = p.d % 4 ? p.by_d(min(i + 4, values) - 1) : first_row;
+    uint32_t any = i + 4 > values;
+    for (uint32_t row = first_row; row <= last_row; ++row) any |= named[row];
+    if (!any) __builtin_nontemporal_store(Piece<float, 4>(0.f), (Piece<float, 4>*)(to + i));
+    else
+      for (uint32_t k = i; k < min(i + 4, values); ++k)
+        if (!named[p.by_d(k)]) to[k] = 0.f;
   }
+  if (p.norms)
+    for (uint32_t row = a + threadIdx.x; row < b; row += kThreads)
+      if (!named[row - a]) p.norms[row] = 0.f;
 }
 
 // LDS of a workgroup's tokens: where their rows of dE lie, their runs (with the neighbours' on both sides), the runs' rows, their numbers
@@ -482,9 +484,10 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   if (ws_bytes < g.bytes) return api_error(LONGER_ERR_WS, "workspace too small: %zu < %zu bytes", ws_bytes, g.bytes);
   hipStream_t st = (hipStream_t)stream;
   uint32_t zero_rows = std::max(4096u / (uint32_t)d, 1u);
+  if (d % 4) zero_rows = (zero_rows + 3) & ~3u;                       // (shares begin where pieces of 16 bytes do)
   while (out_rows / zero_rows >= 1 << 23) zero_rows *= 2;              // (a grid counts threads in 32 bits)
   zero_rows = std::min(zero_rows, emb::kMostZeroRows);
-  const emb::GradParams p = {emb::rows_of(de, B, L), emb::divider(L), (uint32_t)B * L, (uint32_t)L, d, g.shift, g.chunks, g.range, g.block, (float)factor,
+  const emb::GradParams p = {emb::rows_of(de, B, L), emb::divider(L), emb::divider(d), (uint32_t)B * L, (uint32_t)L, d, g.shift, g.chunks, g.range, g.block, (float)factor,
                              emb::mask_of(drop), *order, dense, (uint32_t)out_rows, g.blocks, zero_rows, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares)};
   const dim3 grid(g.blocks + (dense ? (p.out_rows + p.zero_rows - 1) / p.zero_rows : 0), g.chunks);
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
