@@ -176,27 +176,33 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   }
   const Lane me = lane_of<KIND, V>(p);
   const int c = me.at.c, width = me.at.n;
-  const uint32_t n = tokens_of(p), group = threadIdx.x >> p.shift, groups = kThreads >> p.shift;
+  const uint32_t group = threadIdx.x >> p.shift, groups = kThreads >> p.shift, first = blockIdx.x * p.block;
+  // (read before it is known how many of them the order holds; its arrays are as long as the batch)
+  const uint32_t at = min(first + threadIdx.x, p.n - 1);
+  const uint32_t token0 = (uint32_t)p.order.tokens[at], run0 = (uint32_t)p.order.runs[at];
+  const uint32_t run_before = (uint32_t)p.order.runs[max(first, 1u) - 1], run_behind = (uint32_t)p.order.runs[min(first + p.block, p.n - 1)];
+  const uint32_t n = tokens_of(p);
   if (p.norms && blockIdx.y == 0 && !p.dense)        // zeros behind the last row's norm
     for (uint64_t i = (uint64_t)runs_of(p) + blockIdx.x * kThreads + threadIdx.x; i < p.out_rows; i += (uint64_t)p.blocks * kThreads) p.norms[i] = 0.f;
-  if ((uint64_t)blockIdx.x * p.block >= n) {
+  if (first >= n) {
     if (blockIdx.y == 0 && threadIdx.x == 0) p.borders[blockIdx.x] = {kNone, kNone, 0, 0};
     return;
   }
-  const uint32_t first = blockIdx.x * p.block, count = min(p.block, n - first);
+  const uint32_t count = min(p.block, n - first);
   const Key key = DROP ? load_key(p.mask) : Key{};
   // (whatever the order holds, nothing outside the buffers is read or written: rows ascend, so that a run has no row below its number)
   const uint32_t most = min(p.n, p.out_rows);
   for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
-    const uint32_t token = (uint32_t)p.order.tokens[first + i], run = (uint32_t)p.order.runs[first + i], b = p.by_L(token), l = token - b * p.L;
+    const uint32_t token = i == threadIdx.x ? token0 : (uint32_t)p.order.tokens[first + i], run = i == threadIdx.x ? run0 : (uint32_t)p.order.runs[first + i];
+    const uint32_t b = p.by_L(token), l = token - b * p.L;
     from[i] = token < p.n ? (int64_t)b * p.de.user + (int64_t)l * p.de.row : 0;
     runs[i] = run;
     rows[i] = run >= most ? kNone : p.dense ? (uint32_t)p.order.rows[run] : run;
     if (DROP) tokens[i] = token;
   }
   if (threadIdx.x == 0) {
-    runs[-1] = first ? (uint32_t)p.order.runs[first - 1] : kNone;
-    runs[count] = first + count < n ? (uint32_t)p.order.runs[first + count] : kNone;
+    runs[-1] = first ? run_before : kNone;
+    runs[count] = first + count < n ? run_behind : kNone;
   }
   __syncthreads();
   if (blockIdx.y == 0 && threadIdx.x == 0) {
