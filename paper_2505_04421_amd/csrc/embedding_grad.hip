@@ -280,28 +280,53 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   if (p.norms)
     for (uint32_t i = threadIdx.x; i < count; i += kThreads)
       if (runs[i] != runs[i + 1] && runs[i] != runs[(int)(i & ~(p.range - 1)) - 1]) put_norm(p, runs[i], rows[i], me.chunk, __builtin_bit_cast(double, from[i]));
-  // a run that goes on: the group where it begins (or the workgroup's first, where it began before) adds up the sums of those behind
+  // Runs that go on: where a wave has eight groups or more, what each of them has of the run that began before it first becomes the sum over the groups from it
+  // on, as far as that run goes in the wave, doubling the distance at every step (163 thousand tokens of 537 rows of 16 / 32 / 64: 11 / 10 / 12 us, 19 / 14 / 13
+  // group after group; of 128 16.6, 16.4).
+  const int per_step = p.shift <= 3 ? 64 >> p.shift : 1;
+  if (per_step > 1) {
+    const uint32_t flag = begin < end ? flags[group] : 0;
+    bool more = flag & kOn;                          // whether the run goes on behind them
+    if (__any(more)) {
+      float x[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[j] = flag & kLead ? lead[threadIdx.x * V + j] : 0.f;
+      for (int by = 1; by < per_step; by *= 2) {
+        const bool there = (threadIdx.x & 63) + (by << p.shift) < 64;
+        const int behind = __shfl_down((int)more, by << p.shift);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float y = __shfl_down(x[j], by << p.shift);
+          x[j] += there && more ? y : 0.f;
+        }
+        more &= !there || behind;
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) lead[threadIdx.x * V + j] = x[j];
+      if (me.lane == 0) flags[group] = (flag & kLead) | (more ? kOn : 0);
+    }
+    __syncthreads();
+  }
+  // Then the group where a run begins (or the workgroup's first, where it began before) adds up those sums.
   const bool owner = begin < end && on && !earlier, before = group == 0 && flags[0] & kLead;
   if (!owner && !before) return;
   float* part = p.part + (size_t)blockIdx.x * 2 * p.d + c;
-  if (before) {
-    float sum[V];
-    bool more = true;
-    for (uint32_t h = 0; h < groups && more; ++h) {
-      more = flags[h] & kOn;
+  auto add_sums = [&](float (&sum)[V], uint32_t h) {
+    bool on = true;
+    for (; h < groups && on; h = (h / per_step + 1) * per_step) {
+      on = flags[h] & kOn;
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] = (h ? sum[j] : 0.f) + lead[((h << p.shift) + me.lane) * V + j];
+      for (int j = 0; j < V; ++j) sum[j] += lead[((h << p.shift) + me.lane) * V + j];
     }
+    return on;
+  };
+  if (before) {
+    float sum[V] = {};
+    add_sums(sum, 0);
     if (width > 0) store_sums<KIND, V>(part, width, sum);
   }
   if (owner) {
-    bool more = true;
-    for (uint32_t h = group + 1; h < groups && more; ++h) {
-      more = flags[h] & kOn;
-#pragma unroll
-      for (int j = 0; j < V; ++j) acc[j] += lead[((h << p.shift) + me.lane) * V + j];
-    }
-    if (!more) finish<KIND, V>(p, run, rows[end - 1], me, acc);
+    if (!add_sums(acc, group + 1)) finish<KIND, V>(p, run, rows[end - 1], me, acc);
     else if (width > 0) store_sums<KIND, V>(part + p.d, width, acc);
   }
 }
