@@ -33,6 +33,9 @@ struct GradParams {
   float* part;                                       // [workgroups][2][d]
   Border* borders;                                   // [workgroups]
   double* squares;                                   // [runs][chunks], where there is more than one chunk
+  int part_bits;                                     // 2^part_bits workgroups share the columns of a run of many stretches
+  uint32_t* arrivals;                                // [workgroups][chunks]: of them, how many are done with the run that begins there
+  double* part_squares;                              // [workgroups][chunks][parts]
 };
 
 __device__ __forceinline__ uint32_t tokens_of(const GradParams& p) { return min((uint32_t)max(p.order.counts[1], 0), p.n); }
@@ -52,12 +55,12 @@ __device__ __forceinline__ void store_sums(float* to, int n, const float (&a)[V]
       if (j < n) to[j] = v[j];
 }
 
-struct Lane { Part at; uint32_t piece; int lane, chunk; };           // a lane's columns (n <= 0: it has none)
+struct Lane { Part at; uint32_t piece; int lane, chunk, shift; };    // a lane's columns (n <= 0: it has none), of the 2^shift lanes of its group
 template <Kind KIND, int V>
-__device__ __forceinline__ Lane lane_of(const GradParams& p) {
-  const int lane = threadIdx.x & ((1 << p.shift) - 1), chunk = blockIdx.y, c = (chunk * 64 + lane) * V;
-  if (c >= p.d) return {{0, 0, 0}, 0, lane, chunk};
-  return {part_of<KIND, V>((uint32_t)c / V, p.d), (uint32_t)c / V, lane, chunk};
+__device__ __forceinline__ Lane lane_of(const GradParams& p, int shift, uint32_t part = 0) {
+  const int lane = threadIdx.x & ((1 << shift) - 1), chunk = blockIdx.y, c = (chunk * 64 + (part << shift) + lane) * V;
+  if (c >= p.d) return {{0, 0, 0}, 0, lane, chunk, shift};
+  return {part_of<KIND, V>((uint32_t)c / V, p.d), (uint32_t)c / V, lane, chunk, shift};
 }
 
 template <int CTRL> __device__ __forceinline__ float from_lane(float v) {
@@ -97,7 +100,7 @@ __device__ __forceinline__ double put_row(const GradParams& p, uint32_t row, con
     const double x = KIND == WHOLE ? (me.at.n ? g[j] : 0.f) : j >= me.at.twice && j < me.at.n ? g[j] : 0.f;
     squares = fma(x, x, squares);
   }
-  return group_sum(squares, p.shift);
+  return group_sum(squares, me.shift);
 }
 
 __device__ __forceinline__ void put_norm(const GradParams& p, uint32_t run, uint32_t row, int chunk, double squares) {
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
     if (blockIdx.y == 0) zero_rows(p, blockIdx.x - p.blocks, (uint8_t*)lead);
     return;
   }
-  const Lane me = lane_of<KIND, V>(p);
+  const Lane me = lane_of<KIND, V>(p, p.shift);
   const int c = me.at.c, width = me.at.n;
   const uint32_t group = threadIdx.x >> p.shift, groups = kThreads >> p.shift, first = blockIdx.x * p.block;
   // (read before it is known how many of them the order holds; its arrays are as long as the batch)
@@ -184,6 +187,7 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   const uint32_t n = tokens_of(p);
   if (p.norms && blockIdx.y == 0 && !p.dense)        // zeros behind the last row's norm
     for (uint64_t i = (uint64_t)runs_of(p) + blockIdx.x * kThreads + threadIdx.x; i < p.out_rows; i += (uint64_t)p.blocks * kThreads) p.norms[i] = 0.f;
+  if (p.part_bits && threadIdx.x == 0) p.arrivals[blockIdx.x * p.chunks + blockIdx.y] = 0;
   if (first >= n) {
     if (blockIdx.y == 0 && threadIdx.x == 0) p.borders[blockIdx.x] = {kNone, kNone, 0, 0};
     return;
@@ -331,6 +335,8 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   }
 }
 
+constexpr uint32_t kLong = 256;
+
 // The sums of stretches h, h + by, ..., U of them under way at once, while they go on with the run; says whether the last one did.  (A
 // stretch that does not has left nothing to read: what is there is not used.)
 template <Kind KIND, int V, uint32_t U>
@@ -354,39 +360,49 @@ __device__ __forceinline__ bool add_leads(const GradParams& p, float (&acc)[V], 
 }
 
 // The runs that cross workgroups' stretches, each by the group of the stretch that it begins in, and by the whole workgroup where it
-// goes on for more than ALONE: group k takes every groups-th of its sums, which then meet in two steps.  Bound by its loads' latency (512000
-// tokens of 128, 8 values a lane: 10.6 us with ALONE 4, 11.8 with 8; 230 thousand tokens of one item: 11.4 us with 8 sums of a group under way, 14.2 with 4), and
-// where one item has most tokens by what one compute unit can read (2 MB in 26 us).
+// goes on for more than ALONE.  Then group k takes every groups-th of its sums, which meet in two steps; of more than kLong, workgroups z = 0, 1, ... take a part
+// of its columns each, as one item may have most of the tokens, and one compute unit reads 2 MB in 26 us.  The last of them to be done adds up what the
+// others left for the norm, in the order of the parts: nobody waits.  Bound by its loads' latency (512000
+// tokens of 128, 8 values a lane: 10.6 us with ALONE 4, 11.8 with 8; 230 thousand tokens of one item: 11.4 us with 8 sums of a group under way, 14.2 with 4).
 template <Kind KIND, int V, int THREADS>
 __global__ __launch_bounds__(THREADS) void join_kernel(GradParams p) {
   constexpr uint32_t ALONE = 4;
   __shared__ float lds[THREADS * V];
+  constexpr uint32_t kShared = 1u << 31;             // of a list's entry: the run is shared among the workgroups z
   __shared__ uint32_t list[THREADS], listed;
-  const Lane me = lane_of<KIND, V>(p);
-  const int c = me.at.c, width = max(me.at.n, 0);
-  const uint32_t group = threadIdx.x >> p.shift, groups = THREADS >> p.shift, g = blockIdx.x * groups + group;
   const size_t step = (size_t)2 * p.d;
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
-  if (g < p.blocks) {
-    const Border own = p.borders[g];
-    const Piece<float, V> x = load_piece<float, KIND, V>(p.part + g * step + p.d + c, width);
-    float acc[V];
+  {
+    const Lane me = lane_of<KIND, V>(p, p.shift);
+    const int c = me.at.c, width = max(me.at.n, 0);
+    const uint32_t group = threadIdx.x >> p.shift, groups = THREADS >> p.shift, g = blockIdx.x * groups + group;
+    if (g < p.blocks) {
+      const Border own = p.borders[g];
+      const Piece<float, V> x = load_piece<float, KIND, V>(p.part + g * step + p.d + c, width);
+      float acc[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] = x[j];
-    const uint32_t after = g + ALONE + 1 < p.blocks ? p.borders[g + ALONE + 1].lead : kNone;
-    if (own.tail != kNone) {
-      if (after == own.tail) {
-        if (me.lane == 0) list[atomicAdd(&listed, 1u)] = g;          // (the order of the list is that of the work alone)
-      } else {
-        add_leads<KIND, V, ALONE>(p, acc, g + 1, 1, own.tail, c, width);
-        finish<KIND, V>(p, own.tail, own.row, me, acc);
+      for (int j = 0; j < V; ++j) acc[j] = x[j];
+      const uint32_t after = g + ALONE + 1 < p.blocks ? p.borders[g + ALONE + 1].lead : kNone;
+      const bool is_long = p.part_bits && (g + kLong < p.blocks ? p.borders[g + kLong].lead : kNone) == own.tail;
+      if (own.tail != kNone) {
+        if (after == own.tail) {
+          if (me.lane == 0 && (is_long || blockIdx.z == 0)) list[atomicAdd(&listed, 1u)] = is_long ? g | kShared : g;      // (the order of the list is that of the work alone)
+        } else if (blockIdx.z == 0) {
+          add_leads<KIND, V, ALONE>(p, acc, g + 1, 1, own.tail, c, width);
+          finish<KIND, V>(p, own.tail, own.row, me, acc);
+        }
       }
     }
   }
   __syncthreads();
   for (uint32_t i = 0; i < listed; ++i) {
-    const uint32_t a = list[i];
+    const bool shared = list[i] & kShared;
+    const uint32_t a = list[i] & ~kShared;
+    const int shift = shared ? p.shift - p.part_bits : p.shift;
+    const Lane me = lane_of<KIND, V>(p, shift, blockIdx.z);
+    const int c = me.at.c, width = max(me.at.n, 0);
+    const uint32_t group = threadIdx.x >> shift, groups = THREADS >> shift;
     const Border own = p.borders[a];
     float acc[V] = {};
     constexpr uint32_t MANY = 64 / V;
@@ -404,7 +420,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(GradParams p) {
 #pragma unroll 4
       for (uint32_t h = group + 8; h < groups; h += 8)
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += lds[((h << p.shift) + me.lane) * V + j];
+        for (int j = 0; j < V; ++j) acc[j] += lds[((h << shift) + me.lane) * V + j];
     }
     __syncthreads();
     if (group < 8)
@@ -414,8 +430,23 @@ __global__ __launch_bounds__(THREADS) void join_kernel(GradParams p) {
     if (group == 0) {
       for (uint32_t h = 1; h < 8; ++h)
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += lds[((h << p.shift) + me.lane) * V + j];
-      finish<KIND, V>(p, own.tail, own.row, me, acc);
+        for (int j = 0; j < V; ++j) acc[j] += lds[((h << shift) + me.lane) * V + j];
+      double squares = put_row<KIND, V>(p, own.row, me, acc);
+      if (p.norms && me.lane == 0) {
+        const uint32_t parts = 1u << p.part_bits;
+        bool last = true;
+        if (shared) {
+          const size_t at = (size_t)a * p.chunks + me.chunk;
+          double* all = p.part_squares + at * parts;
+          __hip_atomic_store(all + blockIdx.z, squares, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          last = __hip_atomic_fetch_add(p.arrivals + at, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+          if (last) {
+            squares = 0.;
+            for (uint32_t k = 0; k < parts; ++k) squares += __hip_atomic_load(all + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          }
+        }
+        if (last) put_norm(p, own.tail, own.row, me.chunk, squares);
+      }
     }
   }
 }
@@ -444,7 +475,10 @@ static uint32_t range_of(int64_t n, int shift, int chunks) {
   return s;
 }
 
-struct GradPlan { int shift, chunks; uint32_t range, block, blocks; size_t borders, squares, bytes; };
+// A run that goes on for more than kLong of a workgroup's stretches is shared among 2^kPartBits workgroups, where the rows are wide enough (512000 tokens of 128: most of
+// one item in 16 us for 26, popular in 8.3 for 7.8, also where 8 share it 17 and 13; shared from 128 on: 9.6; 23 thousand tokens of 512, most of one: 16 for 34).
+constexpr int kPartBits = 2;
+struct GradPlan { int shift, chunks, part_bits; uint32_t range, block, blocks; size_t borders, squares, arrivals, part_squares, bytes; };
 
 static GradPlan grad_plan(int B, int L, int d) {
   const int64_t n = (int64_t)B * L;
@@ -457,7 +491,10 @@ static GradPlan grad_plan(int B, int L, int d) {
   g.blocks = (uint32_t)((n + g.block - 1) / g.block);
   g.borders = align256((size_t)g.blocks * 2 * d * 4);
   g.squares = g.borders + align256((size_t)g.blocks * sizeof(Border));
-  g.bytes = g.squares + (g.chunks > 1 ? align256((size_t)n * g.chunks * 8) : 0);
+  g.arrivals = g.squares + (g.chunks > 1 ? align256((size_t)n * g.chunks * 8) : 0);
+  g.part_bits = d > 64 && g.blocks > kLong ? kPartBits : 0;
+  g.part_squares = g.arrivals + (g.part_bits ? align256((size_t)g.blocks * g.chunks * 4) : 0);
+  g.bytes = g.part_squares + (g.part_bits ? align256((size_t)g.blocks * g.chunks * 8 << g.part_bits) : 0);
   return g;
 }
 
@@ -479,7 +516,7 @@ template <int V, int THREADS>
 static void join(GradParams p, hipStream_t st) {
   p.shift = lanes_shift(std::min((p.d + V - 1) / V, 64), 6);
   const uint32_t groups = (uint32_t)THREADS >> p.shift;
-  const dim3 grid((p.blocks + groups - 1) / groups, p.chunks);
+  const dim3 grid((p.blocks + groups - 1) / groups, p.chunks, 1 << p.part_bits);
   with_kind(kind_of(p.d, V), [&](auto kind) { join_kernel<decltype(kind)::value, V, THREADS><<<grid, THREADS, 0, st>>>(p); });
 }
 
@@ -519,7 +556,7 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   while (out_rows / zero_rows >= 1 << 23) zero_rows *= 2;              // (a grid counts threads in 32 bits)
   zero_rows = std::min(zero_rows, emb::kMostZeroRows);
   const emb::GradParams p = {emb::rows_of(de, B, L), emb::divider(L), emb::divider(d), (uint32_t)B * L, (uint32_t)L, d, g.shift, g.chunks, g.range, g.block, (float)factor,
-                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, g.blocks, zero_rows, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares)};
+                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, g.blocks, zero_rows, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares), g.part_bits, (uint32_t*)((char*)ws + g.arrivals), (double*)((char*)ws + g.part_squares)};
   const dim3 grid(g.blocks + (dense ? (p.out_rows + p.zero_rows - 1) / p.zero_rows : 0), g.chunks);
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
   else emb::grad<__bf16>(p, grid, st);

@@ -229,7 +229,7 @@ def backward(o, de, scale, drop, dense, rows):
 
 
 GRADS = [(1, 1, 1, 1), (1, 1, 8, 900), (2, 3, 7, 5), (1, 9, 16, 1), (3, 21, 33, 5), (1, 64, 32, 20), (64, 96, 64, 1000), (3, 401, 513, 65), (2, 150, 1024, 9), (1, 70, 16384, 12), (4, 4096, 20, 70000),
-         (6, 2049, 128, 300), (40, 500, 130, 3000)]
+         (6, 2049, 128, 300), (40, 500, 130, 3000), (9, 700, 600, 50), (40, 800, 128, 1000), (60, 400, 65, 9), (150, 400, 16, 30)]
 
 
 @pytest.mark.parametrize("skew", ["even", "popular", "one"])
