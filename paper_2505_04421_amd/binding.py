@@ -754,6 +754,8 @@ class TokenOrder:
         for name, t in (("tokens", tokens), ("runs", runs), ("rows", rows), ("counts", counts)):
             if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda:
                 raise LongerError("%s must be a contiguous device tensor of int32" % name)
+            if t.get_device() != tokens.get_device():
+                raise LongerError("%s is not on the device of tokens" % name)
         if counts.numel() != 2 or runs.numel() != tokens.numel():
             raise LongerError("counts must hold two values, and runs as many as tokens")
         self.tokens, self.runs, self.rows, self.counts = tokens, runs, rows, counts
@@ -782,6 +784,8 @@ class AdamWRows:
                 continue
             if p.dim() != 2 or t.shape != p.shape or not t.is_contiguous() or not t.is_cuda or (name != "w" and t.dtype != torch.float32):
                 raise LongerError("%s must be a contiguous device tensor like p [rows, d]%s" % (name, "" if name == "w" else " of float32"))
+            if t.get_device() != p.get_device():
+                raise LongerError("%s is not on the device of p" % name)
         self.rows, self.d = p.shape
         self.struct = CAdamWTable(p.data_ptr(), m.data_ptr(), v.data_ptr(), _ptr(w), self.rows, self.d, 0 if w is None else _tensor_dtype(w), decay)
 
@@ -818,6 +822,8 @@ def longer_dropout(X, residual, lens, drop: DropoutMask, Y_out, stream=None):
     _require_gpu()
     if X.dim() != 3:
         raise LongerError("X must be a device tensor [B, L, d]")
+    if drop is None:
+        raise LongerError("drop must be a DropoutMask")
     B, L, d = shape = X.shape
     device = _here(X, residual, lens, drop.key, Y_out)
     x, y = _rows(X, shape, "X"), _rows(Y_out, shape, "Y_out")

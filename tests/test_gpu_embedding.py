@@ -556,7 +556,7 @@ def test_python_calls_refuse():
            lambda: lg.longer_embedding(t, ids.float(), None, 1.0, None, E), lambda: lg.longer_embedding(t, ids[0], None, 1.0, None, E),
            lambda: lg.longer_embedding(t.half(), ids, None, 1.0, None, E), lambda: lg.longer_embedding(t[:, ::2], ids, None, 1.0, None, E[..., :4]),
            lambda: lg.longer_embedding(t, ids, None, 1.0, None, E[..., :4]), lambda: lg.longer_embedding(t, ids, ids[0], 1.0, None, E),
-           lambda: lg.longer_embedding(t.cpu(), ids, None, 1.0, None, E), lambda: lg.longer_dropout(E, E[:1], None, drop, E), lambda: lg.longer_dropout(E, None, None, drop, E.bfloat16()),
+           lambda: lg.longer_embedding(t.cpu(), ids, None, 1.0, None, E), lambda: lg.longer_dropout(E, E[:1], None, drop, E), lambda: lg.longer_dropout(E, None, None, None, E), lambda: lg.longer_dropout(E, None, None, drop, E.bfloat16()),
            lambda: lg.longer_sort_ids(ids.expand(2, 3).repeat(1, 9), None, 9, o, ws), lambda: lg.longer_sort_ids(ids, None, 0, o, ws),
            lambda: lg.longer_embedding_backward(o, E, 1.0, None, False, t[:5], None, ws), lambda: lg.longer_embedding_backward(o, E, 1.0, None, True, t, t[0], ws),
            lambda: lg.longer_embedding_backward(o, E, 1.0, None, True, t.bfloat16(), None, ws), lambda: lg.longer_embedding_backward(o, E, 1.0, None, True, t[:, :4], None, ws),
