@@ -430,11 +430,11 @@ def test_rows_beyond_2_to_the_31_values():
     assert np.array_equal(np64(E.reshape(-1, d)[i]), rows)
 
 
-def step_of(B, L, d, R, seed):
+def step_of(B, L, d, R, seed, skew="popular"):
     """The run of the operators as a training step has it, on buffers that stay: returns the step and what it writes."""
     r = np.random.default_rng(seed)
     table = (torch.from_numpy(r.standard_normal((R, d))) * 0.05).float().to(DEV)
-    ids, lens = on_gpu(draw_ids(r, B, L, R, "popular"), torch.int32), lengths(r, B, L, "ragged")[1]
+    ids, lens = on_gpu(draw_ids(r, B, L, R, skew), torch.int32), lengths(r, B, L, "ragged")[1]
     key = torch.tensor([12345, 0], dtype=torch.int64, device=DEV)
     drop_e, drop_h = lg.DropoutMask(0.1, key, 0), lg.DropoutMask(0.2, key, 1)
     state = [table, torch.zeros_like(table), torch.zeros_like(table), table.to(torch.bfloat16)]
@@ -489,11 +489,11 @@ def test_a_step_against_autograd():
     assert bool(((out["p"].double()[named_rows] - want).abs() <= 1e-7)[big].all())
 
 
-@pytest.mark.parametrize("shape", [(6, 50, 48, 70), (40, 700, 64, 5000)])
-def test_a_step_on_another_stream_and_in_a_graph(shape):
+@pytest.mark.parametrize("shape,skew", [((6, 50, 48, 70), "popular"), ((40, 700, 64, 5000), "popular"), ((150, 400, 70, 60), "one")])
+def test_a_step_on_another_stream_and_in_a_graph(shape, skew):
     """Steps, each with the next step's masks: eager, on another stream, and replayed from a graph with eager work between the replays; two
     graphs of two models in turn."""
-    runs = [step_of(*shape, seed) for seed in (1, 2)]
+    runs = [step_of(*shape, seed, skew) for seed in (1, 2)]
     for run in runs:                                                                      # (what no call has written compares as well)
         for k in ("E", "H", "norms", "norm"):
             run[3][k].zero_()
