@@ -747,7 +747,8 @@ class DropoutMask:
 
 class TokenOrder:
     """A batch's tokens by item, as longer_sort_ids leaves them: int32 device tensors tokens and runs [B L], rows [min(B L, table's rows)]
-    and counts [2] (distinct items, valid tokens); larger ones may be given."""
+    and counts [2] (distinct items, valid tokens); larger ones may be given: what a gradient and an update have to hold follows from the
+    batch and the table that longer_sort_ids had last (where it had none: from the arrays' sizes)."""
 
     def __init__(self, tokens, runs, rows, counts):
         import torch
@@ -759,6 +760,7 @@ class TokenOrder:
         if counts.numel() != 2 or runs.numel() != tokens.numel():
             raise LongerError("counts must hold two values, and runs as many as tokens")
         self.tokens, self.runs, self.rows, self.counts = tokens, runs, rows, counts
+        self.batch = None                                                # (tokens, table's rows) that longer_sort_ids had last
         self.struct = COrder(tokens.data_ptr(), runs.data_ptr(), rows.data_ptr(), counts.data_ptr())
 
     @classmethod
@@ -766,6 +768,11 @@ class TokenOrder:
         import torch
         make = lambda n: torch.empty(n, dtype=torch.int32, device=device)
         return cls(make(B * L), make(B * L), make(min(B * L, table_rows)), make(2))
+
+    def _most_rows(self, n=None):
+        """Distinct items that a batch of n tokens (None: the last one) may have."""
+        last, table_rows = self.batch or (self.rows.numel(), self.rows.numel())
+        return min(last if n is None else n, table_rows)
 
     def _holds(self, n, rows):
         if self.tokens.numel() < n or self.rows.numel() < min(n, rows):
@@ -857,6 +864,7 @@ def longer_sort_ids(ids, lens, table_rows, order: TokenOrder, ws, stream=None):
     order._holds(B * L, table_rows)
     _check(load_library().longer_sort_ids(ctypes.byref(i), _lens(lens, B), B, L, table_rows, ctypes.byref(order.struct), _ptr(ws),
                                           ws.numel() * ws.element_size(), _stream(stream, device)), "longer_sort_ids")
+    order.batch = (B * L, table_rows)
 
 
 def longer_embedding_backward_workspace_bytes(B: int, L: int, d: int) -> int:
@@ -877,8 +885,8 @@ def longer_embedding_backward(order: TokenOrder, dE, scale, drop: Optional[Dropo
         raise LongerError("grads_out must be a float32 tensor [rows, %d]" % d)
     device = _here(dE, grads_out, norms_out, ws, order.tokens, None if drop is None else drop.key)
     order._holds(B * L, 0)
-    if not dense and grads_out.shape[0] < min(order.rows.numel(), B * L):
-        raise LongerError("grads_out must have a row for each of the order's %d" % min(order.rows.numel(), B * L))
+    if not dense and grads_out.shape[0] < order._most_rows(B * L):
+        raise LongerError("grads_out must have a row for each of the order's %d" % order._most_rows(B * L))
     norms = None if norms_out is None else _vector(norms_out, grads_out.shape[0], torch.float32, "norms_out")
     _check(load_library().longer_embedding_backward(ctypes.byref(order.struct), ctypes.byref(de), B, L, d, scale, _mask(drop), int(bool(dense)),
                                                     grads_out.shape[0], _ptr(grads_out), norms, _ptr(ws), ws.numel() * ws.element_size(),
@@ -887,16 +895,18 @@ def longer_embedding_backward(order: TokenOrder, dE, scale, drop: Optional[Dropo
 
 def longer_adamw_rows(table: AdamWRows, order: TokenOrder, g, norm, lr, beta1, beta2, eps, step, stream=None):
     """longer_adamw_step on the rows of a table that order names, and no other; g float32 [., d]: their gradients, as
-    longer_embedding_backward (not dense) leaves them."""
+    longer_embedding_backward (not dense) leaves them, in as many rows as it asks for, or more."""
     import torch
     _require_gpu()
     if g.dim() != 2 or g.shape[1] != table.d or g.dtype != torch.float32:
         raise LongerError("g must be a float32 tensor [rows, %d]" % table.d)
     device = _here(table.tensors[0], order.rows, g, norm)
-    most = min(order.rows.numel(), table.rows)
-    if g.shape[0] < most:
-        raise LongerError("g must have a row for each of the order's %d" % most)
+    least = min(order._most_rows(), table.rows)
+    if g.shape[0] < least:
+        raise LongerError("g must have a row for each of the order's %d" % least)
+    # (as many rows as order and g both have places for, not the last batch's: a replayed graph may have left the order of another one)
+    most = min(order.rows.numel(), g.shape[0])
     how = CAdamW(lr, beta1, beta2, eps, step)
-    _check(load_library().longer_adamw_rows(ctypes.byref(table.struct), ctypes.byref(order.struct), 1, order.rows.numel(), _ptr(g), ctypes.byref(how),
+    _check(load_library().longer_adamw_rows(ctypes.byref(table.struct), ctypes.byref(order.struct), 1, most, _ptr(g), ctypes.byref(how),
                                             None if norm is None else _vector(norm, 2, torch.float32, "norm"), _stream(stream, device)),
            "longer_adamw_rows")
