@@ -28,7 +28,7 @@ struct GradParams {
   Mask mask;
   longer_order order;
   int dense;
-  uint32_t out_rows, blocks, zero_rows;              // blocks: workgroups with tokens; the others write zeros, zero_rows of a dense gradient each
+  uint32_t out_rows, blocks, zero_rows, zero_shares; // blocks: workgroups with tokens; the others write zeros, in shares of zero_rows of a dense gradient
   float *grads, *norms;
   float* part;                                       // [workgroups][2][d]
   Border* borders;                                   // [workgroups]
@@ -128,12 +128,12 @@ __device__ __forceinline__ uint32_t lower_bound(const int32_t* rows, uint32_t co
   return lo;
 }
 
-// Zeros in the rows of a dense gradient that no token names, and in their norms, beside the workgroups that add up the others': the named rows of this
-// workgroup's share come from the order.  16 KB to a workgroup (300007 rows of 96, 256000 tokens, shares of 4 / 16 / 32 / 64 KB: 47 / 30 / 35 / 36 us
+// Zeros in the rows of a dense gradient that no token names, and in their norms, beside the workgroups that add up the others': the named rows of a
+// share come from the order.  16 KB to a share, a workgroup each while the grid has room for them (300007 rows of 96, 256000 tokens, shares of 4 / 16 / 32 / 64 KB: 47 / 30 / 35 / 36 us
 // in all; zeros in a launch of their own: 35 and that launch's time; 1000003 rows of 128: 103 us for 97 and the launch).
 constexpr uint32_t kMostZeroRows = 2048;
-__device__ __forceinline__ void zero_rows(const GradParams& p, uint32_t part, uint8_t* named) {
-  const uint32_t a = part * p.zero_rows, b = min(a + p.zero_rows, p.out_rows), count = min(runs_of(p), p.out_rows);
+__device__ __forceinline__ void zero_rows(const GradParams& p, uint32_t share, uint8_t* named) {
+  const uint32_t a = share * p.zero_rows, b = min(a + p.zero_rows, p.out_rows), count = min(runs_of(p), p.out_rows);
   for (uint32_t i = threadIdx.x; i < p.zero_rows; i += kThreads) named[i] = 0;
   const uint32_t first = lower_bound(p.order.rows, count, a);
   __syncthreads();
@@ -174,7 +174,11 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   uint32_t *runs = (uint32_t*)(from + p.block) + 1, *rows = runs + p.block + 1, *tokens = rows + p.block;
   if (blockIdx.x >= p.blocks) {
     static_assert(kMostZeroRows <= sizeof(lead), "a byte for each row");
-    if (blockIdx.y == 0) zero_rows(p, blockIdx.x - p.blocks, (uint8_t*)lead);
+    if (blockIdx.y == 0)
+      for (uint32_t share = blockIdx.x - p.blocks; share < p.zero_shares; share += gridDim.x - p.blocks) {
+        zero_rows(p, share, (uint8_t*)lead);
+        __syncthreads();                             // (the next share's marks go where this one's are read)
+      }
     return;
   }
   const Lane me = lane_of<KIND, V>(p, p.shift);
@@ -553,11 +557,13 @@ int longer_embedding_backward(const longer_order* order, const longer_rows* de, 
   hipStream_t st = (hipStream_t)stream;
   uint32_t zero_rows = std::max(4096u / (uint32_t)d, 1u);
   if (d % 4) zero_rows = (zero_rows + 3) & ~3u;                       // (shares begin where pieces of 16 bytes do)
-  while (out_rows / zero_rows >= 1 << 23) zero_rows *= 2;              // (a grid counts threads in 32 bits)
   zero_rows = std::min(zero_rows, emb::kMostZeroRows);
+  const uint32_t zero_shares = dense ? ((uint32_t)out_rows + zero_rows - 1) / zero_rows : 0;
   const emb::GradParams p = {emb::rows_of(de, B, L), emb::divider(L), emb::divider(d), (uint32_t)B * L, (uint32_t)L, d, g.shift, g.chunks, g.range, g.block, (float)factor,
-                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, g.blocks, zero_rows, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares), g.part_bits, (uint32_t*)((char*)ws + g.arrivals), (double*)((char*)ws + g.part_squares)};
-  const dim3 grid(g.blocks + (dense ? (p.out_rows + p.zero_rows - 1) / p.zero_rows : 0), g.chunks);
+                             emb::mask_of(drop), *order, dense, (uint32_t)out_rows, g.blocks, zero_rows, zero_shares, grads_out, norms_out, (float*)ws, (emb::Border*)((char*)ws + g.borders), (double*)((char*)ws + g.squares), g.part_bits, (uint32_t*)((char*)ws + g.arrivals), (double*)((char*)ws + g.part_squares)};
+  // (a grid counts threads in 32 bits; at most 2^24 - 2^14 workgroups have tokens)
+  static_assert(emb::kThreads == 256, "2^24 workgroups");
+  const dim3 grid(g.blocks + std::min(zero_shares, (1u << 24) - 1 - g.blocks), g.chunks);
   if (de->dtype == LONGER_F32) emb::grad<float>(p, grid, st);
   else emb::grad<__bf16>(p, grid, st);
   if (g.blocks > 1) d <= 64 ? emb::join<4, 128>(p, st) : d <= 256 ? emb::join<4, 512>(p, st) : emb::join<emb::kValues, 512>(p, st);

@@ -90,3 +90,49 @@ def test_rows_update_of_tables_off_the_memory_lines(d, which, off):
     for x, y, s, (buf, before, a) in zip(views, other, start, bufs):
         assert torch.equal(x[hit], y[hit]) and torch.equal(x[~hit], s[~hit])
         assert torch.equal(buf[:a], before[:a]) and torch.equal(buf[a + R * d:], before[a + R * d:])
+
+
+def test_as_many_tokens_as_a_call_takes():
+    """2^31 - 2^21 - 1 places: 2^28 tokens of one user name row 0, 700 row 7, three the last row, the others are padding or name no row.  All places of a user
+    share one row of dE, of whole numbers: every sum is exact, in any order that adds 128 tokens of row 0 at a time.  The dense gradient has
+    more shares of zeros than the workgroups that its grid has left."""
+    B, d = 5, 257
+    n = (1 << 31) - (1 << 21) - 1
+    L, R = n // B, 16 * (1 << 15) + 1003
+    assert B * L == n and (1 << 24) - 1 - -(-n // 128) == (1 << 14) - 1
+    ids = torch.tensor([7, R - 1, -1, 3, 0], device=DEV)[:, None].expand(B, L)
+    count = torch.tensor([700, 3, L, 0, 1 << 28], dtype=torch.int32, device=DEV)
+    torch.manual_seed(1)
+    base = torch.randint(-3, 4, (B, 1, d), device=DEV).float()
+    de = base.to(torch.bfloat16).expand(B, L, d)
+    need = [lg.longer_sort_ids_workspace_bytes(B, L, R), lg.longer_embedding_backward_workspace_bytes(B, L, d)]
+    ws, o = torch.empty(max(need), dtype=torch.uint8, device=DEV), lg.TokenOrder.empty(B, L, R, DEV)
+    lg.longer_sort_ids(ids, count, R, o, ws)
+    valid = (1 << 28) + 703
+    assert o.counts.tolist() == [3, valid] and o.rows[:3].tolist() == [0, 7, R - 1]
+    assert bool((o.runs[:1 << 28] == 0).all()) and bool((o.runs[1 << 28:valid - 3] == 1).all()) and o.runs[valid - 3:valid].tolist() == [2] * 3
+    assert torch.equal(o.tokens[:1 << 28], torch.arange(4 * L, 4 * L + (1 << 28), dtype=torch.int32, device=DEV))
+    assert o.tokens[1 << 28:valid].tolist() == list(range(700)) + [L, L + 1, L + 2]
+    want = base[[4, 0, 1], 0].double() * torch.tensor([[1 << 28], [700], [3]], device=DEV) * 0.5
+    norm = want.square().sum(1).sqrt()
+    for dense in (False, True):
+        grads, norms = torch.full((R, d), -77.0, device=DEV), torch.full((R,), -77.0, device=DEV)
+        lg.longer_embedding_backward(o, de, 0.5, None, dense, grads, norms, ws)
+        at = torch.tensor([0, 7, R - 1] if dense else [0, 1, 2], device=DEV)
+        assert torch.equal(grads[at].double(), want)
+        assert bool(((norms[at].double() - norm).abs() <= 1.01 * U * norm).all())
+        grads[at], norms[at] = (0.0 if dense else -77.0), 0.0
+        assert bool((grads == (0.0 if dense else -77.0)).all()) and bool((norms == 0).all())
+    del ws, o
+    E, table = torch.empty(B, L, 1, dtype=torch.bfloat16, device=DEV), torch.randn(R, 1, device=DEV).to(torch.bfloat16)
+    lg.longer_embedding(table, ids, count, 2.0, None, E)
+    place = torch.arange(L, device=DEV)
+    for b, item in enumerate((7, R - 1, None, 3, 0)):
+        assert torch.equal(E[b, :, 0], torch.where(place < count[b], 0.0 if item is None else table[item, 0] * 2, 0.0).to(torch.bfloat16))
+    drop, f = mask(0.5)
+    E.fill_(1.0)
+    lg.longer_dropout(E, None, None, drop, E)
+    at = np.r_[0:4, (1 << 30) - 3:(1 << 30) + 3, n - 2000:n]
+    assert np.array_equal(E.view(-1, 1)[torch.from_numpy(at).to(DEV)].double().cpu().numpy(), f(at, 1))
+    del E, place
+    torch.cuda.empty_cache()
