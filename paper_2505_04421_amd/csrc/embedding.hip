@@ -28,7 +28,8 @@ __device__ __forceinline__ int64_t item(const Ids& ids, uint32_t b, uint32_t l) 
 }
 
 // Values of a lane's piece: 16 bytes of what is written, so that a store of the wave is one stretch without holes (fp32 rows in two stores of 16 bytes a lane,
-// every other 16 to each: 512000 rows of 128 in 83 to 107 us for 47 to 56).
+// every other 16 to each: 512000 rows of 128 from a bf16 table in 110 us for 49, from one of 500009 fp32 rows 71 for 57, dropout 102 for 91; from 1000003
+// fp32 rows, whose reads bound it, 74 for 76).
 template <typename O> constexpr int kPiece = 16 / sizeof(O);
 
 // E[r] = factor * mask * table[id of r], zeros where r is padding or names no row.  A thread finds where a row's values come from and go to, for all

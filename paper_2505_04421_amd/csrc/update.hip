@@ -261,9 +261,9 @@ __global__ __launch_bounds__(kStepPiece / 4) void step_kernel(StepArgs a) {
 }
 
 // The rows of a table that a batch names: row i of g is the gradient of row rows[i].  A lane holds four values of a row.
-// Bound by memory: 400 thousand rows of 128 in 292 us, 5.3 TB/s, p, m, v and w past the caches (305 with ordinary accesses), g, which the gradient's pass
-// has left there, not.  The grid is as large as
-// pays where the count, which is on the GPU, turns out small (2048 / 16384 / 65536 workgroups: 140 thousand rows 113 / 105 / 114).
+// Bound by memory: 400 thousand rows of 128 in 301 us, 5.1 TB/s, p, m, v and w past the caches (312 with ordinary accesses), g, which the gradient's pass
+// has left there, not.  The grid is as large as pays where the count, which is on the GPU, turns out small (2048 / 16384 / 65536 workgroups: 138 thousand rows
+// of a batch of 512000 tokens 99.5 / 95.6 / 102 us; 400 thousand 312 / 301 / 294).
 struct RowsArgs {
   float *p, *m, *v;
   void* w;
@@ -580,11 +580,11 @@ int longer_adamw_rows(const longer_adamw_table* t, const longer_order* order, in
   const upd::RowsArgs a = {t->p, t->m, t->v, t->w, g, order->rows, order->counts, norm, most, (uint32_t)t->rows, t->d, emb::deal((t->d + 3) / 4),
                            (float)(how->lr * t->decay), h};
   const unsigned groups = std::min((most + a.deal.per_turn - 1) / a.deal.per_turn, 16384u);
-  // Few rows of several turns: a workgroup for each turn (300 rows of 8192 in 9.2 us for 12.3, 4606 of 3486 in 38 for 41; 16000 of 4096 in 263 for 255).
+  // Few rows of several turns: a workgroup for each turn (300 rows of 8192 in 17.1 us for 19.1; 4606 of 3486 in 115 either way; 12000 of 4096 in 294 for 284).
   const unsigned parts = most <= 8192 ? (t->d + 1023) / 1024 : 1;
   hipStream_t st = (hipStream_t)stream;
-  // Whole lines of 128 bytes go past the caches; rows of other widths through them, where the lines that two rows share may meet (140 thousand rows of
-  // 33 / 40 / 100 / 129 values, 16000 of 4099: 97 / 64 / 127 / 170 / 311 us past, 53 / 42 / 135 / 166 / 296 through).
+  // Whole lines of 128 bytes go past the caches; rows of other widths through them, where the lines that two rows share may meet (138 thousand rows of
+  // 33 / 40 / 100 / 129 values, 12397 of 4099: 98.6 / 67.3 / 126 / 190 / 365 us past, 63.7 / 65 / 135 / 174 / 353 through; of 128 95.4, 113).
   const bool past = t->d % 32 == 0 && !(((uintptr_t)t->p | (uintptr_t)t->m | (uintptr_t)t->v) & 127);
   auto go = [&](auto kernel) { kernel<<<dim3(groups, parts), 256, 0, st>>>(a); };
   if (!t->w) past ? go(upd::rows_kernel<float, false, true>) : go(upd::rows_kernel<float, false, false>);
