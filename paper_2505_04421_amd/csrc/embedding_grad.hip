@@ -174,11 +174,13 @@ __global__ __launch_bounds__(kThreads, 4) void grad_kernel(GradParams p) {
   uint32_t *runs = (uint32_t*)(from + p.block) + 1, *rows = runs + p.block + 1, *tokens = rows + p.block;
   if (blockIdx.x >= p.blocks) {
     static_assert(kMostZeroRows <= sizeof(lead), "a byte for each row");
-    if (blockIdx.y == 0)
-      for (uint32_t share = blockIdx.x - p.blocks; share < p.zero_shares; share += gridDim.x - p.blocks) {
-        zero_rows(p, share, (uint8_t*)lead);
-        __syncthreads();                             // (the next share's marks go where this one's are read)
-      }
+    if (blockIdx.y) return;
+    uint32_t share = blockIdx.x - p.blocks;
+    zero_rows(p, share, (uint8_t*)lead);
+    while ((share += gridDim.x - p.blocks) < p.zero_shares) {
+      __syncthreads();                               // (a share's marks go where the last one's are read; behind the last share nobody waits)
+      zero_rows(p, share, (uint8_t*)lead);
+    }
     return;
   }
   const Lane me = lane_of<KIND, V>(p, p.shift);
