@@ -771,8 +771,9 @@ class TokenOrder:
 
     def _most_rows(self, n=None):
         """Distinct items that a batch of n tokens (None: the last one) may have."""
-        last, table_rows = self.batch or (self.rows.numel(), self.rows.numel())
-        return min(last if n is None else n, table_rows)
+        most = self.rows.numel()
+        last, table_rows = self.batch or (most, most)
+        return min(most, table_rows, last if n is None else n)
 
     def _holds(self, n, rows):
         if self.tokens.numel() < n or self.rows.numel() < min(n, rows):

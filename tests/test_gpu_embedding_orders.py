@@ -75,3 +75,17 @@ def test_two_graphs_that_share_an_order():
         lg.longer_adamw_rows(lg.AdamWRows(p, m, v, None, 0.0), o, grads, None, 1e-2, 0.9, 0.99, 1e-8, 1)
         torch.cuda.synchronize()
         assert torch.equal((p != start).any(1).nonzero()[:, 0], distinct)
+
+
+def test_an_order_never_asks_for_more_rows_than_it_holds():
+    """Whatever batch it is used with: no more than its rows, and of an order that was never filled, all that it has room for."""
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)
+    o = lg.TokenOrder(i32(300), i32(300), i32(40), i32(2))
+    assert o._most_rows() == 40 and o._most_rows(30) == 30 and o._most_rows(300) == 40
+    fill(o, np.arange(40)[None] % 7, 1000)
+    assert o.counts.tolist() == [7, 40] and o._most_rows() == 40 and o._most_rows(300) == 40
+    fill(o, np.arange(300)[None] % 7, 9)
+    assert o._most_rows() == 9 and o._most_rows(300) == 9 and o._most_rows(4) == 4
+    with pytest.raises(lg.LongerError):
+        fill(o, np.arange(300)[None] % 7, 41)
+    assert o._most_rows() == 9                                            # (a refused call leaves the last batch's)
